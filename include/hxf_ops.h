@@ -158,6 +158,82 @@ int hxf_op_prefill_attention(const void* q, const void* k_pool, const void* v_po
                              const int32_t* n_host, void* out, int32_t S, int32_t Hq, int32_t Hkv, int32_t head_dim,
                              void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ---- The 8-bit KV cache: e4m3 pages with a scale for each block of 16 tokens and head, and the
+ * operators of a step whose lengths are known on the device alone.  None of them waits for the stream or
+ * reads device values on the host, so a step can be captured into a graph and replayed with other lengths.
+ *
+ * K pool [Hkv][n_blocks][dh/16][16][16] bytes: element (token t, dim d) of a page at
+ * ((d/16)*16 + t)*16 + d%16.  V pool [Hkv][n_blocks][4][dh][4]: element (t, d) at ((t/4)*dh + d)*4 + t%4.
+ * Scales: fp32 [Hkv][n_blocks] for K and for V; an element stands for its e4m3 value (OCP: largest 448, NaN, no
+ * infinity) times the scale of its page.  A scale is a POWER OF TWO in [2^-100, 2^120] (hxf_op_rope_kv8_write
+ * makes no other; of any other value the attention uses the exponent alone), so a dequantised element is
+ * exactly a bf16 value and a page whose scale grows keeps its codes up to their exponents.
+ * k and v must be 16-byte aligned; 0 < n_blocks < 2^27.  The struct is read during the call only. */
+typedef struct hxf_kv8_pool {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int64_t n_blocks;
+} hxf_kv8_pool;
+
+/* Block tables, positions and slots of a batch from its lengths: sequence s has start[s] tokens in the
+ * cache and gets n_new[s] (0: none) more.  Its pages past the ceil(start/16) it holds are taken from the front
+ * of free_pages, sequence by sequence, and entered into bt [S, bt_stride] (its other entries stay as they
+ * are).  free_pages holds *n_free (device; at most free_cap) page numbers.  Outputs:
+ *   row0 [S+1]  first row of each sequence, and the number of rows
+ *   pos, slot [T]  of row row0[s] + i: start[s] + i and its place bt[s][pos/16]*16 + pos%16 in the cache;
+ *                rows from row0[S] on: pos 0, slot -1 (so a batch may be padded to T rows)
+ *   ctx [S]     start + n_new
+ *   status [2]  pages taken, rows
+ * All or nothing: when the pages or the T rows do not suffice, a sequence needs more than bt_stride pages,
+ * or a length is negative, status is {-1, 0}, bt is left as it is, row0 is 0, ctx is start (0 for a negative one)
+ * and every row is {pos 0, slot -1}.  S <= HXF_SLOT_MAP_MAX_SEQS.  All arrays are on the device; the outputs must not
+ * overlap the inputs or each other. */
+#define HXF_SLOT_MAP_MAX_SEQS 4096
+int hxf_op_slot_map(const int32_t* start, const int32_t* n_new, int32_t S, const int32_t* free_pages,
+                    const int32_t* n_free, int32_t free_cap, int32_t* bt, int32_t bt_stride, int32_t* row0,
+                    int32_t* pos, int32_t* slot, int32_t T, int32_t* ctx, int32_t* status, void* stream);
+
+/* RoPE and the quantised KV write.  qkv bf16, T rows of qkv_stride elements (q heads, k heads, v heads; left as it
+ * is): rotate-half RoPE of q and k at pos[t] in fp32 (rope_table: max_pos rows of hxf_op_rope_table; NULL: no
+ * rotation, pos unused); rotated q to q_out (bf16, rows of q_stride elements; NULL: not wanted), k and v to
+ * slot[t] of the pools as e4m3 (nearest even, of the unrounded fp32 value).  A page's scale is the least power of two s with
+ * max|x| <= 448 s over the finite values written to it (no less than 2^-100); values that are not finite become NaN.
+ * Rows of one call that go to one page must be successive rows with successive slots (hxf_op_slot_map makes
+ * them so).  When they begin at the page's first token the page starts afresh; otherwise the tokens
+ * before them stay: the scale is the larger of the page's and the new rows', and where it grows the old codes
+ * are requantised.  Tokens behind the new rows are left as they are.  A row whose slot is not in [0, 16 n_blocks), or
+ * (with a table) whose pos is not in [0, max_pos), is skipped, its q_out row included.
+ * qkv and q_out 16-byte aligned, strides multiples of 8; no buffer may overlap another. */
+int hxf_op_rope_kv8_write(const void* qkv, int64_t qkv_stride, const int32_t* pos, const int32_t* slot,
+                          const void* rope_table, int32_t max_pos, void* q_out, int64_t q_stride,
+                          const hxf_kv8_pool* pool, int32_t T, int32_t Hq, int32_t Hkv, int32_t head_dim, void* stream);
+
+/* Decode attention over the 8-bit cache: one query per sequence, q bf16 (row b at b*q_stride, heads of
+ * head_dim), attends to positions [0, ctx[b]) (ctx on the device, taken as in [0, 16 bt_stride]) through
+ * bt [B, bt_stride]; out bf16 rows of out_stride elements.  ctx 0 (an empty place of a padded batch):
+ * zeros.  Tokens of a block-table entry that is no page of the pool are not read and have no weight.  Entries past
+ * the context are not read.  workspace: hxf_op_decode_attention_kv8_workspace_bytes bytes, 16-byte aligned, whose
+ * contents need not be kept between calls; calls that may overlap need one each. */
+int64_t hxf_op_decode_attention_kv8_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t head_dim);
+int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_pool* pool, const int32_t* bt,
+                                int32_t bt_stride, const int32_t* ctx, void* out, int64_t out_stride, int32_t B,
+                                int32_t Hq, int32_t Hkv, int32_t head_dim, void* workspace, int64_t workspace_bytes,
+                                void* stream);
+
+/* Causal prefill attention over the 8-bit cache: sequence s's queries are the rows row0[s] .. row0[s+1] - 1 of q
+ * (row0 [S+1] ascending, on the device, as hxf_op_slot_map makes it; taken as in [0, T]) at positions
+ * pos0[s], pos0[s]+1, ... (pos0 on the device); each attends to the positions up to its own through bt[s],
+ * whose keys are in the cache already.  Rows of no sequence are left as they are in out.  Positions from
+ * 16 bt_stride on are not in the cache: no key there is seen.  Bad entries, strides and workspace as for
+ * hxf_op_decode_attention_kv8. */
+int64_t hxf_op_prefill_attention_kv8_workspace_bytes(int32_t S, int32_t T, int32_t Hq, int32_t Hkv, int32_t head_dim);
+int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_pool* pool, const int32_t* bt,
+                                 int32_t bt_stride, const int32_t* row0, const int32_t* pos0, void* out,
+                                 int64_t out_stride, int32_t S, int32_t T, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                                 void* workspace, int64_t workspace_bytes, void* stream);
+
 /* out[r] = argmax over v of logits fp32 [R, V]; the lowest index wins ties. */
 int hxf_op_argmax(const float* logits, int32_t* out, int32_t R, int32_t V, void* stream);
 

@@ -33,6 +33,8 @@ SOURCES = [
     "kernels/norm.hip",
     "kernels/rope_kv.hip",
     "kernels/attention.hip",
+    "kernels/kv8.hip",
+    "kernels/kv8_attention.hip",
     "kernels/misc.hip",
 ]
 

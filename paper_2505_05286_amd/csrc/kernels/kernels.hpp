@@ -233,6 +233,74 @@ hipError_t prefill_attn_launch(const PrefillAttnArgs& a, hipStream_t st, hipEven
 // Queries covered by one prefill work item for a given GQA group size.
 int prefill_queries_per_item(int group);
 
+// ------------------------------------------------------------------ 8-bit KV cache
+// Per layer, kv-head major like the bf16 pools, one byte per element (e4m3) and one power-of-two
+// scale per (kv-head, page) of each pool:
+//   K: [Hkv][n_blocks][dh/16][16 tokens][16]  (a lane's 16-byte load is 16 dimensions of one token)
+//   V: [Hkv][n_blocks][4][dh][4 tokens]       (a dimension's tokens in groups of four, as a lane of the
+//                                              score tile holds them)
+struct Kv8Pool {
+  uint8_t* k;
+  uint8_t* v;
+  float* ks;
+  float* vs;
+  int64_t n_blocks;
+};
+// Offset of (dimension d, token t) inside a page of K, and of V
+__host__ __device__ inline int k8_offset(int d, int t) { return ((d >> 4) * kPage + t) * 16 + (d & 15); }
+__host__ __device__ inline int v8_offset(int d, int t, int dh) { return ((t >> 2) * dh + d) * 4 + (t & 3); }
+
+constexpr int kSlotMapMaxSeqs = 4096;
+struct SlotMapArgs {
+  const int32_t* start;
+  const int32_t* n_new;
+  const int32_t* free_pages;
+  const int32_t* n_free;
+  int32_t* bt;
+  int32_t* row0;
+  int32_t* pos;
+  int32_t* slot;
+  int32_t* ctx;
+  int32_t* status;
+  int S, T, free_cap, bt_stride;
+};
+hipError_t slot_map_launch(const SlotMapArgs& a, hipStream_t st);
+
+struct Kv8WriteArgs {
+  const uint16_t* qkv;
+  int64_t qkv_stride;
+  const int32_t* pos;
+  const int32_t* slot;
+  const float2* cs;      // may be null: no rotation
+  int max_pos;
+  uint16_t* q_out;       // may be null
+  int64_t q_stride;
+  Kv8Pool pool;
+  int T, Hq, Hkv, dh;
+};
+hipError_t kv8_write_launch(const Kv8WriteArgs& a, hipStream_t st);
+
+struct Kv8AttnArgs {
+  const uint16_t* q;
+  int64_t q_stride;
+  Kv8Pool pool;
+  const int32_t* bt;
+  int bt_stride;
+  const int32_t* ctx;    // decode: [B]
+  const int32_t* row0;   // prefill: [S + 1]
+  const int32_t* pos0;   // prefill: [S]
+  uint16_t* out;
+  int64_t out_stride;
+  int S, T;              // sequences; prefill: rows
+  int Hq, Hkv, dh;
+  float scale_log2;      // log2(e) / sqrt(dh)
+  uint8_t* ws;
+};
+int64_t kv8_decode_ws_bytes(int B, int Hq, int Hkv, int dh);
+hipError_t kv8_decode_launch(const Kv8AttnArgs& a, hipStream_t st);
+int64_t kv8_prefill_ws_bytes(int S, int T, int Hq, int Hkv, int dh);
+hipError_t kv8_prefill_launch(const Kv8AttnArgs& a, hipStream_t st);
+
 // ------------------------------------------------------------------ sampling / misc
 // out[r] = argmax_v logits[r][v], the lowest index among equal maxima.
 hipError_t argmax_launch(const float* logits, int32_t* out, int R, int V, hipStream_t st);

@@ -428,6 +428,144 @@ int hxf_op_prefill_attention(const void* q, const void* k_pool, const void* v_po
   return ok ? dev_rc(done) : HXF_EDEVICE;
 }
 
+namespace {
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+bool pool_ok(const hxf_kv8_pool* p) {
+  return p && p->k && p->v && p->k_scale && p->v_scale && p->n_blocks > 0 && p->n_blocks < (int64_t(1) << 27) &&
+         aligned16(p->k) && aligned16(p->v);
+}
+
+Kv8Pool pool_of(const hxf_kv8_pool* p) {
+  return Kv8Pool{(uint8_t*)p->k, (uint8_t*)p->v, p->k_scale, p->v_scale, p->n_blocks};
+}
+
+// rows of bf16 heads that the kernels read and write 16 bytes at a time
+bool rows_ok(const void* p, int64_t stride, int64_t width) {
+  return p && aligned16(p) && stride >= width && stride % 8 == 0;
+}
+
+bool table_ok(const int32_t* bt, int32_t bt_stride) { return bt && bt_stride > 0 && bt_stride < (1 << 27); }
+
+}  // namespace
+
+int hxf_op_slot_map(const int32_t* start, const int32_t* n_new, int32_t S, const int32_t* free_pages,
+                    const int32_t* n_free, int32_t free_cap, int32_t* bt, int32_t bt_stride, int32_t* row0,
+                    int32_t* pos, int32_t* slot, int32_t T, int32_t* ctx, int32_t* status, void* stream) {
+  if (S < 0 || S > HXF_SLOT_MAP_MAX_SEQS || T < 0 || free_cap < 0 || !row0 || !status || !n_free ||
+      (free_cap > 0 && !free_pages) || (T > 0 && (!pos || !slot)))
+    return HXF_EINVAL;
+  if (S > 0 && (!start || !n_new || !ctx || !table_ok(bt, bt_stride))) return HXF_EINVAL;
+  static_assert(HXF_SLOT_MAP_MAX_SEQS == kSlotMapMaxSeqs, "sequence limit");
+  SlotMapArgs a{};
+  a.start = start;
+  a.n_new = n_new;
+  a.free_pages = free_pages;
+  a.n_free = n_free;
+  a.bt = bt;
+  a.row0 = row0;
+  a.pos = pos;
+  a.slot = slot;
+  a.ctx = ctx;
+  a.status = status;
+  a.S = S;
+  a.T = T;
+  a.free_cap = free_cap;
+  a.bt_stride = bt_stride;
+  return dev_rc(slot_map_launch(a, (hipStream_t)stream));
+}
+
+int hxf_op_rope_kv8_write(const void* qkv, int64_t qkv_stride, const int32_t* pos, const int32_t* slot,
+                          const void* rope_table, int32_t max_pos, void* q_out, int64_t q_stride,
+                          const hxf_kv8_pool* pool, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh, void* stream) {
+  if (T < 0 || !shapes_ok(Hq, Hkv, dh) || !pool_ok(pool) || !slot) return HXF_EINVAL;
+  if (!rows_ok(qkv, qkv_stride, (int64_t)(Hq + 2 * Hkv) * dh) || (q_out && !rows_ok(q_out, q_stride, (int64_t)Hq * dh)))
+    return HXF_EINVAL;
+  if (rope_table && (!pos || max_pos <= 0 || !aligned16(rope_table))) return HXF_EINVAL;
+  if (T == 0) return HXF_OK;
+  Kv8WriteArgs a{};
+  a.qkv = (const uint16_t*)qkv;
+  a.qkv_stride = qkv_stride;
+  a.pos = pos;
+  a.slot = slot;
+  a.cs = (const float2*)rope_table;
+  a.max_pos = max_pos;
+  a.q_out = (uint16_t*)q_out;
+  a.q_stride = q_stride;
+  a.pool = pool_of(pool);
+  a.T = T;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.dh = dh;
+  return dev_rc(kv8_write_launch(a, (hipStream_t)stream));
+}
+
+int64_t hxf_op_decode_attention_kv8_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t dh) {
+  if (B < 0 || !shapes_ok(Hq, Hkv, dh)) return -1;
+  return kv8_decode_ws_bytes(B, Hq, Hkv, dh);
+}
+
+int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_pool* pool, const int32_t* bt,
+                                int32_t bt_stride, const int32_t* ctx, void* out, int64_t out_stride, int32_t B,
+                                int32_t Hq, int32_t Hkv, int32_t dh, void* workspace, int64_t ws_bytes, void* stream) {
+  if (B < 0 || !shapes_ok(Hq, Hkv, dh) || !pool_ok(pool) || !table_ok(bt, bt_stride) || !ctx ||
+      !rows_ok(q, q_stride, (int64_t)Hq * dh) || !rows_ok(out, out_stride, (int64_t)Hq * dh))
+    return HXF_EINVAL;
+  if (B == 0) return HXF_OK;
+  if (!workspace || !aligned16(workspace) || ws_bytes < kv8_decode_ws_bytes(B, Hq, Hkv, dh)) return HXF_ENOMEM;
+  Kv8AttnArgs a{};
+  a.q = (const uint16_t*)q;
+  a.q_stride = q_stride;
+  a.pool = pool_of(pool);
+  a.bt = bt;
+  a.bt_stride = bt_stride;
+  a.ctx = ctx;
+  a.out = (uint16_t*)out;
+  a.out_stride = out_stride;
+  a.S = B;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.dh = dh;
+  a.scale_log2 = 1.4426950408889634f / std::sqrt((float)dh);
+  a.ws = (uint8_t*)workspace;
+  return dev_rc(kv8_decode_launch(a, (hipStream_t)stream));
+}
+
+int64_t hxf_op_prefill_attention_kv8_workspace_bytes(int32_t S, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh) {
+  if (S < 0 || T < 0 || !shapes_ok(Hq, Hkv, dh)) return -1;
+  return kv8_prefill_ws_bytes(S, T, Hq, Hkv, dh);
+}
+
+int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_pool* pool, const int32_t* bt,
+                                 int32_t bt_stride, const int32_t* row0, const int32_t* pos0, void* out,
+                                 int64_t out_stride, int32_t S, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh,
+                                 void* workspace, int64_t ws_bytes, void* stream) {
+  if (S < 0 || T < 0 || !shapes_ok(Hq, Hkv, dh) || !pool_ok(pool) || !table_ok(bt, bt_stride) || !row0 || !pos0 ||
+      !rows_ok(q, q_stride, (int64_t)Hq * dh) || !rows_ok(out, out_stride, (int64_t)Hq * dh))
+    return HXF_EINVAL;
+  if (S == 0 || T == 0) return HXF_OK;
+  if (!workspace || !aligned16(workspace) || ws_bytes < kv8_prefill_ws_bytes(S, T, Hq, Hkv, dh)) return HXF_ENOMEM;
+  Kv8AttnArgs a{};
+  a.q = (const uint16_t*)q;
+  a.q_stride = q_stride;
+  a.pool = pool_of(pool);
+  a.bt = bt;
+  a.bt_stride = bt_stride;
+  a.row0 = row0;
+  a.pos0 = pos0;
+  a.out = (uint16_t*)out;
+  a.out_stride = out_stride;
+  a.S = S;
+  a.T = T;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.dh = dh;
+  a.scale_log2 = 1.4426950408889634f / std::sqrt((float)dh);
+  a.ws = (uint8_t*)workspace;
+  return dev_rc(kv8_prefill_launch(a, (hipStream_t)stream));
+}
+
 int hxf_op_argmax(const float* logits, int32_t* out, int32_t R, int32_t V, void* stream) {
   if (!logits || !out || R < 0 || V <= 0 || V % 4) return HXF_EINVAL;
   return dev_rc(argmax_launch(logits, out, R, V, (hipStream_t)stream));

@@ -100,6 +100,12 @@ class Profile(C.Structure):
                 ("prefill_attn_ms", C.c_double)]
 
 
+class Kv8Pool(C.Structure):
+    """hxf_kv8_pool: device addresses of the e4m3 K and V pools and of their scales, and their pages."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("n_blocks", C.c_int64)]
+
+
 _lib = None
 
 # name -> (restype, argtypes)
@@ -169,6 +175,21 @@ _SIGS = {
                                            C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32),
                                            C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                            C.c_int64, C.c_void_p]),
+    "hxf_op_slot_map": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                  C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
+                                  C.c_void_p]),
+    "hxf_op_rope_kv8_write": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                        C.c_void_p, C.c_int64, C.POINTER(Kv8Pool), C.c_int32, C.c_int32, C.c_int32,
+                                        C.c_int32, C.c_void_p]),
+    "hxf_op_decode_attention_kv8_workspace_bytes": (C.c_int64, [C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
+    "hxf_op_decode_attention_kv8": (C.c_int, [C.c_void_p, C.c_int64, C.POINTER(Kv8Pool), C.c_void_p, C.c_int32,
+                                              C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
+                                              C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]),
+    "hxf_op_prefill_attention_kv8_workspace_bytes": (C.c_int64, [C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                                                 C.c_int32]),
+    "hxf_op_prefill_attention_kv8": (C.c_int, [C.c_void_p, C.c_int64, C.POINTER(Kv8Pool), C.c_void_p, C.c_int32,
+                                               C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_int32,
+                                               C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]),
     "hxf_op_argmax": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]),
     "hxf_op_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "hxf_op_read": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
@@ -532,6 +553,44 @@ def op_prefill_attention(q, k_pool, v_pool, n_blocks, bt, bt_stride, row0, pos0,
     m, mp = _i32(n)
     _op(lib().hxf_op_prefill_attention(q, k_pool, v_pool, n_blocks, bt, bt_stride, rp, pp, mp, out, S, Hq, Hkv, dh,
                                        ws, ws_bytes, stream or None), "hxf_op_prefill_attention")
+
+
+SLOT_MAP_MAX_SEQS = 4096
+
+
+def op_slot_map(start, n_new, S, free_pages, n_free, free_cap, bt, bt_stride, row0, pos, slot, T, ctx, status,
+                stream=0):
+    """Block tables, positions and slots of a batch from its lengths; every array is a device address."""
+    _op(lib().hxf_op_slot_map(start, n_new, S, free_pages, n_free, free_cap, bt, bt_stride, row0, pos, slot, T, ctx,
+                              status, stream or None), "hxf_op_slot_map")
+
+
+def op_rope_kv8_write(qkv, qkv_stride, pos, slot, table, max_pos, q_out, q_stride, pool, T, Hq, Hkv, dh, stream=0):
+    """RoPE of q and k, and the e4m3 write of k and v into pool (a Kv8Pool); table 0: no rotation."""
+    _op(lib().hxf_op_rope_kv8_write(qkv, qkv_stride, pos or None, slot, table or None, max_pos, q_out or None,
+                                    q_stride, pool, T, Hq, Hkv, dh, stream or None), "hxf_op_rope_kv8_write")
+
+
+def op_decode_attention_kv8_workspace_bytes(B, Hq, Hkv, dh):
+    return lib().hxf_op_decode_attention_kv8_workspace_bytes(B, Hq, Hkv, dh)
+
+
+def op_decode_attention_kv8(q, q_stride, pool, bt, bt_stride, ctx, out, out_stride, B, Hq, Hkv, dh, ws, ws_bytes,
+                            stream=0):
+    """Decode attention over the 8-bit cache; ctx is a device address."""
+    _op(lib().hxf_op_decode_attention_kv8(q, q_stride, pool, bt, bt_stride, ctx, out, out_stride, B, Hq, Hkv, dh, ws,
+                                          ws_bytes, stream or None), "hxf_op_decode_attention_kv8")
+
+
+def op_prefill_attention_kv8_workspace_bytes(S, T, Hq, Hkv, dh):
+    return lib().hxf_op_prefill_attention_kv8_workspace_bytes(S, T, Hq, Hkv, dh)
+
+
+def op_prefill_attention_kv8(q, q_stride, pool, bt, bt_stride, row0, pos0, out, out_stride, S, T, Hq, Hkv, dh, ws,
+                             ws_bytes, stream=0):
+    """Causal prefill attention over the 8-bit cache; row0 and pos0 are device addresses."""
+    _op(lib().hxf_op_prefill_attention_kv8(q, q_stride, pool, bt, bt_stride, row0, pos0, out, out_stride, S, T, Hq,
+                                           Hkv, dh, ws, ws_bytes, stream or None), "hxf_op_prefill_attention_kv8")
 
 
 def op_argmax(logits, out, R, V, stream=0):

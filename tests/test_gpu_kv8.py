@@ -1,0 +1,474 @@
+"""The operators of the 8-bit KV cache against a plain model in float64 (tests/kv8_util.py): tables and
+codes to the last bit, attention within the roundings it makes."""
+import numpy as np
+import pytest
+
+import synth
+from paper_2505_05286_amd import hxf
+
+from . import kv8_util as U
+from .gpu_util import dev_bits, host_f64, i32, log, rand_bf16, torch
+
+pytestmark = pytest.mark.gpu
+
+HEADS = [(4, 2, 64), (32, 8, 128), (40, 8, 128), (16, 1, 64), (3, 3, 128), (13, 1, 128), (14, 2, 64)]
+
+
+class DevCache:
+    """A Cache in HBM."""
+
+    def __init__(self, c):
+        t = torch()
+        self.c = c
+        put = lambda a: t.from_numpy(np.ascontiguousarray(a)).to("cuda:0")
+        self.k, self.v = (put(U.pack(c.codes[x], x)) for x in "kv")
+        self.ks, self.vs = put(c.scale["k"]), put(c.scale["v"])
+        self.pool = hxf.Kv8Pool(self.k.data_ptr(), self.v.data_ptr(), self.ks.data_ptr(), self.vs.data_ptr(), c.nb)
+
+    def check(self, what):
+        for kind, codes, scale in (("k", self.k, self.ks), ("v", self.v, self.vs)):
+            got = U.unpack(codes.cpu().numpy(), kind, self.c.dh)
+            np.testing.assert_array_equal(scale.cpu().numpy(), self.c.scale[kind], err_msg=f"{what}: {kind} scales")
+            assert U.same_codes(got, self.c.codes[kind]), (
+                f"{what}: {kind} codes differ at {np.argwhere(got != self.c.codes[kind])[:5].tolist()}")
+
+
+def _dev_slot_map(start, n_new, free, n_free, bt, T, stream=0):
+    t = torch()
+    S, stride = bt.shape
+    guard = 7                                    # words past each output that stay as they are
+    new = lambda n: t.full((n + guard,), 77, dtype=t.int32, device="cuda:0")
+    o = {"bt": i32(bt), "row0": new(S + 1), "pos": new(T), "slot": new(T), "ctx": new(S), "status": new(2)}
+    a, b, f, nf = i32(start), i32(n_new), i32(np.append(free, [0])), i32([n_free])
+    hxf.op_slot_map(a.data_ptr(), b.data_ptr(), S, f.data_ptr(), nf.data_ptr(), len(free), o["bt"].data_ptr(), stride,
+                    o["row0"].data_ptr(), o["pos"].data_ptr(), o["slot"].data_ptr(), T, o["ctx"].data_ptr(),
+                    o["status"].data_ptr(), stream=stream)
+    t.cuda.synchronize()
+    out = {k: v.cpu().numpy() for k, v in o.items()}
+    for k, n in (("row0", S + 1), ("pos", T), ("slot", T), ("ctx", S), ("status", 2)):
+        assert np.all(out[k][n:] == 77), k
+        out[k] = out[k][:n]
+    return out
+
+
+def _check_slot_map(start, n_new, free, bt, T, what, n_free=None):
+    start, n_new = np.asarray(start, np.int64), np.asarray(n_new, np.int64)
+    n_free = len(free) if n_free is None else n_free
+    log(f"slot map {what}: S={len(start)} T={T}")
+    got = _dev_slot_map(start, n_new, np.asarray(free), n_free, bt, T)
+    ref = U.slot_map(start, n_new, free[:max(0, min(n_free, len(free)))], bt, T)
+    for k, r in zip(("bt", "row0", "pos", "slot", "ctx", "status"), ref):
+        np.testing.assert_array_equal(got[k], r, err_msg=f"{what}: {k}")
+    return got
+
+
+def _batch(rng, S, hi_start, hi_new):
+    start = rng.integers(0, hi_start + 1, S)
+    n_new = rng.integers(0, hi_new + 1, S)
+    old, end = -(-start // 16), -(-(start + n_new) // 16)
+    stride = int(end.max(initial=0)) + 2
+    order = rng.permutation(int(end.sum()) + 9)
+    bt = np.full((S, stride), -5, np.int64)
+    at = 0
+    for s in range(S):
+        bt[s, :old[s]] = order[at:at + old[s]]
+        at += old[s]
+    return start, n_new, order[at:], bt
+
+
+@pytest.mark.parametrize("S,hi_start,hi_new", [(0, 0, 0), (1, 0, 1), (1, 100, 1), (2, 0, 40), (63, 50, 3), (64, 300, 1),
+                                               (65, 31, 33), (257, 64, 17), (1000, 500, 30), (1025, 3, 2),
+                                               (4096, 90, 5), (5, 3000, 5000)])
+def test_slot_map(S, hi_start, hi_new):
+    rng = np.random.default_rng(S * 1000 + hi_start + hi_new)
+    start, n_new, free, bt = _batch(rng, S, hi_start, hi_new)
+    for pad in (0, 1, 45):
+        _check_slot_map(start, n_new, free, bt, int(n_new.sum()) + pad, f"pad {pad}")
+
+
+def test_slot_map_page_borders():
+    """Lengths on both sides of a page's end; sequences that get nothing between ones that do."""
+    start = np.array([0, 15, 16, 17, 0, 31, 32, 48, 15, 16])
+    n_new = np.array([16, 1, 0, 15, 17, 1, 1, 0, 2, 16])
+    end = -(-(start + n_new) // 16)
+    old = -(-start // 16)
+    bt = np.full((10, int(end.max())), -1, np.int64)
+    for s in range(10):
+        bt[s, :old[s]] = 100 + 10 * s + np.arange(old[s])
+    need = int((end - old).sum())
+    got = _check_slot_map(start, n_new, np.arange(500, 500 + need), bt, int(n_new.sum()), "borders")
+    assert got["status"][0] == need       # the last free page is taken, and no more
+
+
+@pytest.mark.parametrize("why", ["pages", "n_free", "n_free negative", "rows", "stride", "held pages", "start", "new"])
+def test_slot_map_that_does_not_fit_changes_nothing(why):
+    rng = np.random.default_rng(7)
+    start, n_new, free, bt = _batch(rng, 70, 100, 40)
+    need = int((-(-(start + n_new) // 16) - -(-start // 16)).sum())
+    free, T, n_free = free[:need], int(n_new.sum()), None
+    if why == "pages":
+        free = free[:-1]
+    elif why.startswith("n_free"):
+        n_free = need - 1 if why == "n_free" else -3
+    elif why == "rows":
+        T -= 1
+    elif why == "stride":
+        bt = bt[:, :int((-(-(start + n_new) // 16)).max()) - 1].copy()
+    elif why == "held pages":
+        start[3], n_new[3] = 16 * bt.shape[1] + 1, 0
+    elif why == "start":
+        start[69] = -1
+    else:
+        n_new[0] = -1
+    got = _check_slot_map(start, n_new, free, bt, T, why, n_free)
+    assert got["status"].tolist() == [-1, 0]
+
+
+def test_slot_map_counts_beyond_the_free_list():
+    """n_free larger than the list's capacity counts as the capacity; sums beyond 32 bits do not wrap."""
+    bt = np.full((3, 5), -1, np.int64)
+    _check_slot_map([0, 0, 0], [20, 1, 7], np.arange(9, 13), bt, 28, "capacity", n_free=1000)
+    _check_slot_map([0, 0, 0], [2 ** 31 - 1, 2 ** 31 - 1, 2], np.arange(4), bt, 10, "wrap")
+    _check_slot_map([2 ** 31 - 1, 0, 0], [2 ** 31 - 1, 1, 1], np.arange(4), bt, 10, "wrap of one")
+
+
+def _write(cache, dev, rng, slot, pos, hq, table, scale=1.0, bits=None, pad_cols=0, q_pad=0):
+    """One call of the write against the model, q_out included; bits: the rows to take."""
+    t = torch()
+    T, hkv, dh = len(slot), cache.hkv, cache.dh
+    width = (hq + 2 * hkv) * dh
+    if bits is None:
+        bits = rand_bf16(rng, (T, width), scale)[0]
+    rows = np.full((T, width + pad_cols), 0x7FC0, np.uint16)
+    rows[:, :width] = bits
+    d_rows, d_pos, d_slot = dev_bits(rows), i32(pos), i32(slot)
+    before = rows.copy()
+    q = dev_bits(np.full((T, hq * dh + q_pad), 0x1234, np.uint16))
+    tab = t.from_numpy(table).to("cuda:0") if table is not None else None
+    hxf.op_rope_kv8_write(d_rows.data_ptr(), width + pad_cols, d_pos.data_ptr(), d_slot.data_ptr(),
+                          tab.data_ptr() if tab is not None else 0, len(table) if tab is not None else 0,
+                          q.data_ptr(), hq * dh + q_pad, dev.pool, T, hq, hkv, dh)
+    t.cuda.synchronize()
+    x = U.f32_of(bits).reshape(T, hq + 2 * hkv, dh)
+    live = (slot >= 0) & (slot < cache.nb * 16)
+    qk = x[:, :hq + hkv]
+    if table is not None:
+        live &= (pos >= 0) & (pos < len(table))
+        qk = U.rotate(qk, table[np.where(live, pos, 0)])
+    cache.write(qk[:, hq:], x[:, hq + hkv:], np.where(live, slot, -1))
+    dev.check(f"T={T}")
+    got = q.cpu().numpy().view(np.uint16)
+    ref = np.full_like(got, 0x1234)
+    ref[live, :hq * dh] = synth.f32_to_bf16_bits(qk[live, :hq].reshape(-1, hq * dh))
+    fin = np.ones_like(got, bool)
+    fin[live, :hq * dh] = np.isfinite(qk[live, :hq].reshape(-1, hq * dh))
+    np.testing.assert_array_equal(np.where(fin, got, 0), np.where(fin, ref, 0))
+    assert np.all(~np.isfinite(U.f32_of(got)[~fin]))
+    np.testing.assert_array_equal(d_rows.cpu().numpy().view(np.uint16), before)
+
+
+@pytest.mark.parametrize("hq,hkv,dh", HEADS)
+def test_write_in_pieces(hq, hkv, dh):
+    """A sequence in chunks of many lengths with values that grow and shrink: codes, scales, requantised pages
+    and untouched places after every call."""
+    rng = np.random.default_rng(hq * 100 + hkv + dh)
+    cache = U.Cache(hkv, 23, dh)
+    dev = DevCache(cache)
+    blocks = rng.permutation(23)
+    table = U.rope_table(400, dh)
+    p = 0
+    for i, n in enumerate([1, 1, 14, 5, 1, 27, 16, 33, 1, 1, 2, 64, 1, 3, 100]):
+        pos = np.arange(p, p + n)
+        slot = blocks[pos // 16] * 16 + pos % 16
+        log(f"write {hq}/{hkv}x{dh}: {n} rows at {p}")
+        _write(cache, dev, rng, slot, pos, hq, table, scale=[1.0, 6.0, 0.1, 40.0, 900.0][i % 5], pad_cols=8 * (i % 3),
+               q_pad=8 * (i % 2))
+        p += n
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(4, 2, 64), (32, 8, 128), (5, 1, 128)])
+@pytest.mark.parametrize("with_table", [True, False])
+def test_write_of_many_sequences(hq, hkv, dh, with_table):
+    """Decode rows, chunks that begin and continue, dead rows between them and behind them."""
+    rng = np.random.default_rng(hq + dh + with_table)
+    nb = 150
+    cache = U.Cache(hkv, nb, dh)
+    cache.fill(rng, np.arange(nb))
+    order = iter(rng.permutation(nb))
+    slot, pos = [], []
+    for first, n in [(5, 1), (0, 1), (15, 1), (0, 16), (3, 13), (8, 30), (0, 57), (1, 1), (15, 2), (0, 200), (7, 1)]:
+        p = np.arange(first, first + n)
+        pages = np.array([next(order) for _ in range(p[-1] // 16 + 1)])
+        slot += list(pages[p // 16] * 16 + p % 16)
+        pos += list(p + 64)
+        if n == 13:
+            slot += [-1, nb * 16, 2 ** 31 - 1, -2 ** 31]
+            pos += [1, 2, 3, 4]
+    table = U.rope_table(300, dh) if with_table else None
+    slot, pos = np.array(slot), np.array(pos)
+    if with_table:
+        pos[3], pos[-2] = -1, 300     # rows without a rotation are skipped, wherever they stand in a run
+    dev = DevCache(cache)
+    _write(cache, dev, rng, slot, pos, hq, table, scale=3.0)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_write_values(dh):
+    """Every rounding: all bf16 values near the codes and their midpoints, the ends of the range, subnormal codes,
+    zeros of both signs, pages of zeros, tiny and huge pages, infinities and NaN."""
+    rng = np.random.default_rng(dh)
+    hkv, hq, nb = 2, 2, 40
+    cache = U.Cache(hkv, nb, dh)
+    dev = DevCache(cache)
+    width = (hq + 2 * hkv) * dh
+    for i in range(nb - 1):
+        bits = rng.integers(0, 1 << 16, (16, width)).astype(np.uint16)
+        x = U.f32_of(bits)
+        top = [448.0, 449.0, 480.0, 1e-30, 1e-38, 3e38, 0.0, 1.0][i % 8]
+        if i < 8:
+            bits = np.where(np.abs(x) <= top, bits, bits & 0x8000)          # (NaN and infinity too)
+        elif i < 24:
+            # significands on and next to the midpoints of three-bit ones, exponents around the code's
+            m = rng.choice([0, 7, 8, 9, 15, 16, 17, 24, 64, 120, 127], (16, width))
+            e = rng.integers(127 - 12, 127 + 9, (16, width))
+            bits = ((rng.integers(0, 2, (16, width)) << 15) | (e << 7) | m).astype(np.uint16)
+        elif i < 32:
+            bits = np.where(rng.random((16, width)) < 0.02, np.uint16(0x7F80 if i % 2 else 0xFFC0),
+                            rand_bf16(rng, (16, width))[0])
+        n = 16 if i % 3 else 9
+        slot = i * 16 + np.arange(n)
+        log(f"write values {i}")
+        _write(cache, dev, rng, slot, slot, hq, None, bits=bits[:n].astype(np.uint16))
+        if n == 9:                                                           # and the page's rest, at another size
+            slot = i * 16 + np.arange(9, 16)
+            _write(cache, dev, rng, slot, slot, hq, None, scale=2.0 ** rng.integers(-20, 20))
+
+
+def _attention_case(rng, ctx, hq, hkv, dh, spare=5):
+    """A cache with these contexts behind a permuted table: NaN past every context, unused pages and their scales
+    NaN, table entries past the context out of range."""
+    ctx = np.asarray(ctx)
+    pages = -(-ctx // 16)
+    nb = int(pages.sum()) + spare
+    cache = U.Cache(hkv, nb, dh)
+    order = rng.permutation(nb)
+    stride = max(1, int(pages.max(initial=0)) + 2)
+    bt = rng.choice([-1, nb, 2 ** 31 - 1, -2 ** 31], (len(ctx), stride))
+    at = 0
+    for s, n in enumerate(pages):
+        bt[s, :n] = order[at:at + n]
+        at += n
+    cache.fill(rng, order[:at])
+    for s, n in enumerate(ctx):
+        if n % 16:
+            cache.poison(bt[s, n // 16], n % 16)
+    return cache, bt
+
+
+def _decode(cache, bt, ctx, hq, rng, q_pad=0, o_pad=0, what="", ws_fill=0xFF, q_scale=1.0):
+    t = torch()
+    B, hkv, dh = len(ctx), cache.hkv, cache.dh
+    dev = DevCache(cache)
+    bits, _ = rand_bf16(rng, (B, hq * dh + q_pad), q_scale)
+    if q_pad:
+        bits[:, hq * dh:] = 0x7FC0
+    qf = U.f32_of(bits)[:, :hq * dh].astype(np.float64).reshape(B, hq, dh)
+    q, d_bt, d_ctx = dev_bits(bits), i32(bt), i32(ctx)
+    out = dev_bits(np.full((B + 1, hq * dh + o_pad), 0x1234, np.uint16))
+    n = hxf.op_decode_attention_kv8_workspace_bytes(B, hq, hkv, dh)
+    ws = t.full((n,), ws_fill, dtype=t.uint8, device="cuda:0")
+    log(f"decode kv8 {what}: B={B} {hq}/{hkv}x{dh} ctx max {int(np.max(ctx))}")
+    hxf.op_decode_attention_kv8(q.data_ptr(), hq * dh + q_pad, dev.pool, d_bt.data_ptr(), bt.shape[1],
+                                d_ctx.data_ptr(), out.data_ptr(), hq * dh + o_pad, B, hq, hkv, dh, ws.data_ptr(), n)
+    t.cuda.synchronize()
+    raw = out.cpu().numpy().view(np.uint16).reshape(B + 1, -1)
+    assert np.all(raw[B] == 0x1234) and np.all(raw[:, hq * dh:] == 0x1234), what
+    got = host_f64(out).reshape(B + 1, -1)[:B, :hq * dh].reshape(B, hq, dh)
+    dev.check(what)
+    for b in range(B):
+        ref, size = U.attend(qf[b:b + 1], cache, bt[b], min(max(int(ctx[b]), 0), 16 * bt.shape[1]), hq)
+        U.assert_attention(got[b:b + 1], ref, size, f"{what} sequence {b} (ctx {ctx[b]})")
+    return raw
+
+
+@pytest.mark.parametrize("hq,hkv,dh", HEADS)
+def test_decode_lengths(hq, hkv, dh):
+    rng = np.random.default_rng(hq + 10 * hkv + dh)
+    for i, ctx in enumerate([[1], [0], [0, 5, 0, 33, 0], [15, 16, 17, 31, 32, 33, 47, 48, 49, 63, 64, 65],
+                             [127, 128, 129, 255, 256, 257, 258, 511, 513], [1000, 1, 2], [2500]]):
+        cache, bt = _attention_case(rng, ctx, hq, hkv, dh)
+        _decode(cache, bt, np.array(ctx), hq, rng, q_pad=8 * (i % 3), o_pad=8 * (i % 2), what=f"lengths {i}")
+
+
+@pytest.mark.parametrize("B,hi,heads", [(63, 300, (4, 2, 64)), (64, 200, (32, 8, 128)), (65, 500, (8, 8, 128)),
+                                        (130, 90, (16, 1, 64)), (300, 40, (4, 2, 64)), (1100, 20, (2, 1, 64)),
+                                        (2, 9000, (8, 1, 128)), (17, 3000, (4, 2, 64))])
+def test_decode_batches(B, hi, heads):
+    """Batches around the wavefront's width and beyond it, very uneven, some places empty."""
+    hq, hkv, dh = heads
+    rng = np.random.default_rng(B + hi)
+    ctx = np.rint(np.exp(rng.uniform(0, np.log(hi), B))).astype(np.int64)
+    ctx[rng.random(B) < 0.1] = 0
+    ctx[B // 2] = hi
+    cache, bt = _attention_case(rng, ctx, hq, hkv, dh)
+    _decode(cache, bt, ctx, hq, rng, what="batch")
+
+
+def test_decode_entries_that_are_no_page():
+    """Entries out of range inside a context are neither read nor weighted; a context of nothing else is empty; a
+    context longer than the table's row, or negative, is cut."""
+    rng = np.random.default_rng(3)
+    ctx = [100, 600, 40, 33, 16]
+    cache, bt = _attention_case(rng, ctx, 8, 2, 128)
+    bt[0, 0], bt[0, 5], bt[0, 6] = -1, cache.nb, 2 ** 31 - 1
+    bt[1, 10:30] = -7
+    bt[2, :3] = [-1, cache.nb + 5, -2 ** 31]
+    bt[3, 2] = -1
+    _decode(cache, bt, np.array(ctx), 8, rng, what="bad entries")
+    stride = bt.shape[1]
+    bt[1, 38:] = bt[1, 0]
+    ctx = np.array([100, 2 ** 31 - 1, -5, -2 ** 31, 16])
+    cache.fill(rng, bt[1, 37:38])
+    assert stride * 16 > 600
+    _decode(cache, bt, ctx, 8, rng, what="cut contexts")
+
+
+def test_decode_extreme_scores():
+    """One key far above the others, large and tiny scales: no overflow, and the same result for any split."""
+    rng = np.random.default_rng(4)
+    for q_scale in (0.0, 2.0 ** -20, 6.0):
+        cache, bt = _attention_case(rng, [700, 3], 8, 2, 128)
+        cache.scale["k"][:] = np.minimum(cache.scale["k"], 2.0 ** -4)
+        _decode(cache, bt, np.array([700, 3]), 8, rng, what=f"q {q_scale}", q_scale=q_scale)
+    for s in (2.0 ** -90, 2.0 ** 60):
+        cache, bt = _attention_case(rng, [90], 4, 1, 64)
+        cache.scale["v"][:] *= s
+        cache.scale["k"][:] *= 2.0 ** -40
+        _decode(cache, bt, np.array([90]), 4, rng, what=f"v {s}")
+
+
+def test_decode_offsets_beyond_32_bits():
+    """A pool of more than 4 GiB per tensor, pages at its far end."""
+    t = torch()
+    rng = np.random.default_rng(5)
+    hq, hkv, dh, nb = 4, 2, 128, (1 << 20) + 50_000
+    small = U.Cache(hkv, 40, dh)
+    small.fill(rng, np.arange(40))
+    at = np.concatenate([np.arange(5), nb - 35 + np.arange(35)])
+    k = t.full((hkv, nb, 16 * dh), 0x7F, dtype=t.uint8, device="cuda:0")
+    v = t.full((hkv, nb, 16 * dh), 0x7F, dtype=t.uint8, device="cuda:0")
+    ks = t.full((hkv, nb), float("nan"), device="cuda:0")
+    vs = t.full((hkv, nb), float("nan"), device="cuda:0")
+    ix = t.from_numpy(at).to("cuda:0")
+    for kind, codes, scale in (("k", k, ks), ("v", v, vs)):
+        codes[:, ix] = t.from_numpy(U.pack(small.codes[kind], kind)).to("cuda:0")
+        scale[:, ix] = t.from_numpy(small.scale[kind]).to("cuda:0")
+    pool = hxf.Kv8Pool(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), nb)
+    order = rng.permutation(40)
+    bits, qf = rand_bf16(rng, (1, hq, dh))
+    q, bt, ctx, out = dev_bits(bits), i32(at[order][None]), i32([640]), dev_bits(np.zeros((1, hq, dh), np.uint16))
+    n = hxf.op_decode_attention_kv8_workspace_bytes(1, hq, hkv, dh)
+    ws = t.empty(n, dtype=t.uint8, device="cuda:0")
+    hxf.op_decode_attention_kv8(q.data_ptr(), hq * dh, pool, bt.data_ptr(), 40, ctx.data_ptr(), out.data_ptr(),
+                                hq * dh, 1, hq, hkv, dh, ws.data_ptr(), n)
+    n = hxf.op_prefill_attention_kv8_workspace_bytes(1, 1, hq, hkv, dh)
+    ws2, row0, pos0 = t.empty(n, dtype=t.uint8, device="cuda:0"), i32([0, 1]), i32([639])
+    out2 = dev_bits(np.zeros((1, hq, dh), np.uint16))
+    hxf.op_prefill_attention_kv8(q.data_ptr(), hq * dh, pool, bt.data_ptr(), 40, row0.data_ptr(), pos0.data_ptr(),
+                                 out2.data_ptr(), hq * dh, 1, 1, hq, hkv, dh, ws2.data_ptr(), n)
+    t.cuda.synchronize()
+    ref, size = U.attend(qf, small, order, 640, hq)
+    U.assert_attention(host_f64(out).reshape(1, hq, dh), ref, size, "decode")
+    U.assert_attention(host_f64(out2).reshape(1, hq, dh), ref, size, "prefill")
+
+
+def _prefill(cache, bt, pos0, n, hq, rng, pad=0, lead=0, q_pad=0, o_pad=0, what="", row0=None):
+    """lead: rows before the first sequence; pad: rows behind the last one."""
+    t = torch()
+    S, hkv, dh = len(n), cache.hkv, cache.dh
+    dev = DevCache(cache)
+    if row0 is None:
+        row0 = lead + np.concatenate([[0], np.cumsum(n)])
+    T = int(max(row0)) + pad
+    bits, _ = rand_bf16(rng, (T, hq * dh + q_pad))
+    qf = U.f32_of(bits)[:, :hq * dh].astype(np.float64).reshape(T, hq, dh)
+    q, d_bt, d_row0, d_pos0 = dev_bits(bits), i32(bt), i32(row0), i32(pos0)
+    out = dev_bits(np.full((T + 1, hq * dh + o_pad), 0x1234, np.uint16))
+    m = hxf.op_prefill_attention_kv8_workspace_bytes(S, T, hq, hkv, dh)
+    ws = t.full((m,), 0xFF, dtype=t.uint8, device="cuda:0")
+    log(f"prefill kv8 {what}: S={S} T={T} {hq}/{hkv}x{dh}")
+    hxf.op_prefill_attention_kv8(q.data_ptr(), hq * dh + q_pad, dev.pool, d_bt.data_ptr(), bt.shape[1],
+                                 d_row0.data_ptr(), d_pos0.data_ptr(), out.data_ptr(), hq * dh + o_pad, S, T, hq, hkv,
+                                 dh, ws.data_ptr(), m)
+    t.cuda.synchronize()
+    raw = out.cpu().numpy().view(np.uint16).reshape(T + 1, -1)
+    assert np.all(raw[:, hq * dh:] == 0x1234), what
+    got = host_f64(out).reshape(T + 1, -1)[:T, :hq * dh].reshape(T, hq, dh)
+    dev.check(what)
+    seen = np.zeros(T + 1, bool)
+    for s in range(S):
+        r = slice(int(row0[s]), int(row0[s]) + int(n[s]))
+        seen[r] = True
+        ref, size = U.attend(qf[r], cache, bt[s], min(int(pos0[s] + n[s]), 16 * bt.shape[1]), hq, first=int(pos0[s]))
+        U.assert_attention(got[r], ref, size, f"{what} sequence {s} (pos {pos0[s]}, {n[s]} rows)")
+    assert np.all(raw[~seen] == 0x1234), f"{what}: rows of no sequence"
+    return raw
+
+
+@pytest.mark.parametrize("hq,hkv,dh", HEADS)
+def test_prefill_lengths(hq, hkv, dh):
+    rng = np.random.default_rng(hq + 10 * hkv + dh)
+    for i, (pos0, n) in enumerate([([0], [1]), ([0], [37]), ([5, 0, 16, 31], [1, 0, 33, 1]), ([100, 15], [70, 17]),
+                                   ([0, 300, 7], [129, 2, 0]), ([1000], [3]), ([2300], [40]), ([0], [257]),
+                                   ([31, 32, 33, 47], [32, 31, 33, 17])]):
+        cache, bt = _attention_case(rng, np.add(pos0, n), hq, hkv, dh)
+        _prefill(cache, bt, np.array(pos0), np.array(n), hq, rng, pad=3 * (i % 2), lead=2 * (i % 3), q_pad=8 * (i % 2),
+                 o_pad=8 * (i % 3), what=f"lengths {i}")
+
+
+@pytest.mark.parametrize("S,hi_pos,hi_n,heads", [(33, 200, 20, (4, 2, 64)), (70, 60, 9, (32, 8, 128)),
+                                                 (8, 700, 300, (8, 2, 128)), (300, 33, 3, (2, 1, 64)),
+                                                 (2, 3000, 400, (10, 2, 128)), (1100, 9, 2, (4, 2, 64))])
+def test_prefill_batches(S, hi_pos, hi_n, heads):
+    hq, hkv, dh = heads
+    rng = np.random.default_rng(S + hi_pos)
+    pos0, n = rng.integers(0, hi_pos + 1, S), rng.integers(0, hi_n + 1, S)
+    n[S // 2] = hi_n
+    cache, bt = _attention_case(rng, pos0 + n, hq, hkv, dh)
+    _prefill(cache, bt, pos0, n, hq, rng, pad=5, what="batch")
+
+
+def test_prefill_entries_that_are_no_page():
+    rng = np.random.default_rng(13)
+    pos0, n = np.array([80, 0, 300, 0]), np.array([40, 33, 9, 16])
+    cache, bt = _attention_case(rng, pos0 + n, 8, 2, 128)
+    bt[0, 2], bt[0, 3], bt[0, 4] = -1, cache.nb, -2 ** 31
+    bt[1, 1] = 2 ** 31 - 1
+    bt[2, :12] = -1
+    bt[3, 0] = -3                       # a sequence none of whose keys is there
+    raw = _prefill(cache, bt, pos0, n, 8, rng, what="bad entries")
+    assert np.all(raw[82:98] == 0)
+
+
+def test_prefill_rows_past_the_table_and_row0_out_of_range():
+    """Positions past the table's row see the keys it holds; row0 beyond T counts as T."""
+    t = torch()
+    rng = np.random.default_rng(14)
+    cache, bt = _attention_case(rng, [64, 40], 4, 2, 64)
+    bt = bt[:, :4].copy()
+    cache.fill(rng, bt[0])
+    _prefill(cache, bt, np.array([50, 30]), np.array([30, 10]), 4, rng, what="past the table")
+    dev = DevCache(cache)
+    bits, qf = rand_bf16(rng, (20, 4, 64))
+    q, d_bt, row0, pos0 = dev_bits(bits), i32(bt), i32([0, 12, 50]), i32([20, 12])
+    out = dev_bits(np.full((24, 4, 64), 0x1234, np.uint16))
+    m = hxf.op_prefill_attention_kv8_workspace_bytes(2, 20, 4, 2, 64)
+    ws = t.empty(m, dtype=t.uint8, device="cuda:0")
+    hxf.op_prefill_attention_kv8(q.data_ptr(), 256, dev.pool, d_bt.data_ptr(), 4, row0.data_ptr(), pos0.data_ptr(),
+                                 out.data_ptr(), 256, 2, 20, 4, 2, 64, ws.data_ptr(), m)
+    t.cuda.synchronize()
+    got = host_f64(out).reshape(24, 4, 64)
+    for r, s, p in ((slice(0, 12), 0, 20), (slice(12, 20), 1, 12)):
+        ref, size = U.attend(qf[r], cache, bt[s], p + r.stop - r.start, 4, first=p)
+        U.assert_attention(got[r], ref, size, f"sequence {s}")
+    assert np.all(out.cpu().numpy().view(np.uint16).reshape(24, -1)[20:] == 0x1234)
