@@ -47,7 +47,7 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
 DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # The attention kernels rescale their MFMA accumulators with VALU every tile: with
 # accumulators in VGPRs the compiler stops copying them to and from AGPRs.
-EXTRA = {"kernels/attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+EXTRA = {f"kernels/{f}.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("attention", "kv8_attention")}
 
 
 def _compile(src, build_dir=BUILD, host_flags=()):

@@ -46,6 +46,13 @@ __device__ __forceinline__ f32x4 mfma16x16x32(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// Four e4m3 codes times a power of two (the exponent of `scale`) as bf16, exactly
+__device__ __forceinline__ uint2 e4m3x4_to_bf16(uint32_t c, float scale) {
+  const auto lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false);
+  const auto hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true);
+  return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+}
+
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // 32x32x16 bf16 MFMA: A lane l holds row l%32, k (l/32)*8..+8; B lane l holds
@@ -106,6 +113,23 @@ template <int N>
 __device__ __forceinline__ void wait_vmcnt_lgkm0() {
   static_assert(N >= 0 && N < 64, "vmcnt range");
   __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((N >> 4) << 14));
+}
+
+// Inclusive sum over the wavefront's lanes, by DPP moves (rows of 16 lanes, then the rows)
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31 into rows 2 and 3
+  return x;
+}
+
+// max(v, v of lane l ^ 16), likewise by a swap of odd and even rows of 16 lanes
+__device__ __forceinline__ float row_swap_max(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 // max(v, v of lane l ^ 32) in every lane, by a VALU swap of the wavefront's halves

@@ -295,7 +295,35 @@ struct Kv8AttnArgs {
   int Hq, Hkv, dh;
   float scale_log2;      // log2(e) / sqrt(dh)
   uint8_t* ws;
+  int64_t ws_ml;         // offset of the partials' (maximum, sum) pairs
 };
+// Decode work split, made by the kernels themselves from the contexts in device memory.  As for the bf16
+// cache, each (sequence, kv-head) stream of pages is cut into equal parts no longer than an even share of
+// all the pages over the wavefronts the chip holds at once, at least kKv8MinPages pages; with fewer streams than
+// those wavefronts the parts just fill them.
+constexpr int kKv8Resident = 2048;
+constexpr int kKv8MinPages = 8;
+__host__ __device__ inline int64_t kv8_target_pages(int64_t total_pages, int64_t n_seqs, int hkv) {
+  const int64_t pairs = n_seqs * hkv;
+  const int64_t slots = pairs < kKv8Resident ? kKv8Resident - pairs : kKv8Resident;
+  const int64_t t = (total_pages * hkv + slots - 1) / slots;
+  return t > kKv8MinPages ? t : kKv8MinPages;
+}
+// Length of a part of a stream of `pages` pages, and the number of them: at most ceil(pages / target)
+__host__ __device__ inline int kv8_part_pages(int pages, int target) {
+  const int n = (pages + target - 1) / target;
+  return n > 0 ? (pages + n - 1) / n : 1;
+}
+__host__ __device__ inline int kv8_parts(int pages, int target) {
+  const int len = kv8_part_pages(pages, target);
+  return (pages + len - 1) / len;
+}
+// Wavefronts that hold every part whatever the contexts are: with fewer streams than resident wavefronts,
+// sum ceil(p / t) <= sum p / t + streams <= (resident - streams) + streams; otherwise resident + streams.
+inline int64_t kv8_decode_items(int64_t n_seqs, int hkv) {
+  const int64_t pairs = n_seqs * hkv;
+  return pairs < kKv8Resident ? kKv8Resident : kKv8Resident + pairs;
+}
 int64_t kv8_decode_ws_bytes(int B, int Hq, int Hkv, int dh);
 hipError_t kv8_decode_launch(const Kv8AttnArgs& a, hipStream_t st);
 int64_t kv8_prefill_ws_bytes(int S, int T, int Hq, int Hkv, int dh);

@@ -446,6 +446,9 @@ bool rows_ok(const void* p, int64_t stride, int64_t width) {
   return p && aligned16(p) && stride >= width && stride % 8 == 0;
 }
 
+// (wavefront and grid indices are 32 bits wide)
+bool batch_ok(int64_t n, int Hq) { return n * Hq < (int64_t(1) << 29); }
+
 bool table_ok(const int32_t* bt, int32_t bt_stride) { return bt && bt_stride > 0 && bt_stride < (1 << 27); }
 
 }  // namespace
@@ -502,7 +505,7 @@ int hxf_op_rope_kv8_write(const void* qkv, int64_t qkv_stride, const int32_t* po
 }
 
 int64_t hxf_op_decode_attention_kv8_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t dh) {
-  if (B < 0 || !shapes_ok(Hq, Hkv, dh)) return -1;
+  if (B < 0 || !shapes_ok(Hq, Hkv, dh) || !batch_ok(B, Hq)) return -1;
   return kv8_decode_ws_bytes(B, Hq, Hkv, dh);
 }
 
@@ -510,7 +513,7 @@ int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_p
                                 int32_t bt_stride, const int32_t* ctx, void* out, int64_t out_stride, int32_t B,
                                 int32_t Hq, int32_t Hkv, int32_t dh, void* workspace, int64_t ws_bytes, void* stream) {
   if (B < 0 || !shapes_ok(Hq, Hkv, dh) || !pool_ok(pool) || !table_ok(bt, bt_stride) || !ctx ||
-      !rows_ok(q, q_stride, (int64_t)Hq * dh) || !rows_ok(out, out_stride, (int64_t)Hq * dh))
+      !rows_ok(q, q_stride, (int64_t)Hq * dh) || !rows_ok(out, out_stride, (int64_t)Hq * dh) || !batch_ok(B, Hq))
     return HXF_EINVAL;
   if (B == 0) return HXF_OK;
   if (!workspace || !aligned16(workspace) || ws_bytes < kv8_decode_ws_bytes(B, Hq, Hkv, dh)) return HXF_ENOMEM;
