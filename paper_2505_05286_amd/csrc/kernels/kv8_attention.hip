@@ -6,47 +6,6 @@ namespace hxf {
 
 namespace {
 
-// One wavefront per (query row, head): 64 tokens at a time, a lane scoring one of them, then
-// each lane summing its dimensions over the 64 weights.
-template <int DH>
-__device__ void attend(const Kv8AttnArgs& a, int seq, int row, int head, int n, float* qs) {
-  const int lane = threadIdx.x;
-  const int kvh = head / (a.Hq / a.Hkv);
-  const uint16_t* q = a.q + row * a.q_stride + head * DH;
-  for (int d = lane; d < DH; d += 64) qs[d] = bf2f(q[d]);
-  __syncthreads();
-  const int32_t* bt = a.bt + (size_t)seq * a.bt_stride;
-  float m = -1e30f, l = 0.f, acc[DH / 64] = {};
-  for (int t0 = 0; t0 < n; t0 += 64) {
-    const int t = t0 + lane;
-    const int blk = t < n ? bt[t / kPage] : -1;
-    const bool ok = blk >= 0 && blk < a.pool.n_blocks;
-    float x = -__builtin_huge_valf(), vs = 0.f;
-    if (ok) {
-      const uint8_t* k = a.pool.k + kv_tile(kvh, a.pool.n_blocks, blk, DH);
-      float s = 0.f;
-      for (int d = 0; d < DH; ++d) s += qs[d] * __builtin_amdgcn_cvt_f32_fp8(k[k8_offset(d, t % kPage)], 0);
-      x = s * a.pool.ks[kvh * a.pool.n_blocks + blk] * a.scale_log2;
-      vs = a.pool.vs[kvh * a.pool.n_blocks + blk];
-    }
-    const float m_new = fmaxf(m, wave_max(x));
-    const float alpha = exp2f(m - m_new), p = exp2f(x - m_new);
-    l = l * alpha + wave_sum(p);
-    m = m_new;
-    for (int j = 0; j < DH / 64; ++j) acc[j] *= alpha;
-    for (int u = 0; u < 64; ++u) {
-      const int b = __shfl(ok ? blk : -1, u, kWave);
-      const float w = __shfl(p, u, kWave), sc = __shfl(vs, u, kWave);
-      if (b < 0) continue;
-      const uint8_t* v = a.pool.v + kv_tile(kvh, a.pool.n_blocks, b, DH);
-      for (int j = 0; j < DH / 64; ++j)
-        acc[j] += w * sc * __builtin_amdgcn_cvt_f32_fp8(v[v8_offset(j * 64 + lane, (t0 + u) % kPage, DH)], 0);
-    }
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  for (int j = 0; j < DH / 64; ++j) a.out[row * a.out_stride + head * DH + j * 64 + lane] = f2bf(acc[j] * inv);
-}
-
 constexpr float kNegInf = -__builtin_huge_valf();
 
 // Pages of sequence b that its context reaches, and its tokens
@@ -281,19 +240,62 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
   if (rq == 0) reinterpret_cast<float2*>(a.ws + a.ws_ml)[slot] = make_float2(S.m, S.l);
 }
 
-// Joins the parts of one (sequence, head) per wavefront; zeros for an empty context.
+// Joins the parts of a sequence's heads, H (4 or 1) heads a workgroup; zeros for an empty context.  A thread owns
+// four dimensions and every R-th part, four of them in flight, with a running maximum.  With four heads and up to
+// kMergeAlone parts each wavefront joins a head of its own; otherwise the workgroup takes its heads in turn and its
+// streams meet in LDS.  H is 1 where four heads a workgroup would leave CUs without one and the
+// tables are long enough for more parts than that.  64 sequences of up to 11
+// parts: 4.7 us (H = 1: 7.7); a lone context of 64 parts: 4.7 us with H = 1, 9.5 with 4, 17.2 with a wavefront for
+// each head.
+constexpr int kCus = 256;
+constexpr int kMergeAlone = 16;
 template <int DH>
+struct MergeState {
+  float M = -1e30f, L = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  __device__ __forceinline__ void fold(float2 v, float4 x) {
+    const float m = fmaxf(M, v.x);
+    const float sc = __builtin_amdgcn_exp2f(M - m), w = __builtin_amdgcn_exp2f(v.x - m);
+    M = m;
+    L = L * sc + w * v.y;
+    acc.x = acc.x * sc + w * x.x;
+    acc.y = acc.y * sc + w * x.y;
+    acc.z = acc.z * sc + w * x.z;
+    acc.w = acc.w * sc + w * x.w;
+  }
+  // parts r, r + R, ... of n; part j at ml[j * G] and o + j * G * DH
+  __device__ __forceinline__ void take(const float2* ml, const float* o, int G, int n, int r, int R) {
+    for (int j0 = r; j0 < n; j0 += 4 * R) {
+      float2 v[4];
+      float4 x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const size_t j = (size_t)min(j0 + u * R, n - 1) * G;
+        v[u] = ml[j];
+        x[u] = *reinterpret_cast<const float4*>(o + j * DH);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (j0 + u * R < n) fold(v[u], x[u]);
+    }
+  }
+  __device__ __forceinline__ void write(uint16_t* out) const {
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf2(acc.x * inv, acc.y * inv), pack_bf2(acc.z * inv, acc.w * inv));
+  }
+};
+
+template <int DH, int H>
 __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int job = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (job >= a.S * a.Hq) return;
-  const int b = job / a.Hq, head = job - b * a.Hq;
-  constexpr int PER = DH / 64;   // dimensions a lane
-  uint16_t* out = a.out + b * a.out_stride + head * DH + lane * PER;
+  constexpr int C = DH / 4, R = 256 / C;   // threads across a row, streams of parts in a workgroup
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = (a.Hq + H - 1) / H;
+  const int b = blockIdx.x / groups, h0 = (blockIdx.x - b * groups) * H;
+  const int c = threadIdx.x % C;
+  uint16_t* out = a.out + b * a.out_stride + c * 4;
   const int n_pages = pages_of(ctx_of(a, b));
   if (n_pages == 0) {
-#pragma unroll
-    for (int k = 0; k < PER; ++k) out[k] = 0;
+    if (w < H && lane < C && h0 + w < a.Hq) *reinterpret_cast<uint2*>(out + (h0 + w) * DH) = make_uint2(0, 0);
     return;
   }
   const int target = decode_target(a, lane);
@@ -303,37 +305,520 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a) {
   for (int i0 = 0; i0 < b; i0 += kWave)
     before += __builtin_amdgcn_readlane(
         wave_scan(i0 + lane < b ? kv8_parts(pages_of(ctx_of(a, i0 + lane)), target) : 0), 63);
-  const int G = a.Hq / a.Hkv, kvh = head / G;
-  const size_t first = ((size_t)before * a.Hkv + (size_t)kvh * n) * G + head - kvh * G;
-  const float2* ml = reinterpret_cast<const float2*>(a.ws + a.ws_ml) + first;
-  const float* o = reinterpret_cast<const float*>(a.ws) + first * DH + lane * PER;
-  float M = -1e30f;
-  for (int j = lane; j < n; j += kWave) M = fmaxf(M, ml[(size_t)j * G].x);
-  M = wave_max(M);
-  float L = 0.f, acc[PER] = {};
-  for (int j = 0; j < n; ++j) {
-    const float2 v = ml[(size_t)j * G];
-    const float w = __builtin_amdgcn_exp2f(v.x - M);
-    L += w * v.y;
+  const int G = a.Hq / a.Hkv;
+  const float2* ml = reinterpret_cast<const float2*>(a.ws + a.ws_ml);
+  const float* o = reinterpret_cast<const float*>(a.ws) + c * 4;
+  auto first = [&](int head) { return ((size_t)before * a.Hkv + (size_t)(head / G) * n) * G + head % G; };
+  if (H == 4 && n <= kMergeAlone) {
+    if (h0 + w >= a.Hq) return;
+    const size_t f = first(h0 + w);
+    MergeState<DH> S;
+    S.take(ml + f, o + f * DH, G, n, lane / C, kWave / C);
 #pragma unroll
-    for (int k = 0; k < PER; ++k) acc[k] += w * o[(size_t)j * G * DH + k];
-  }
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  if constexpr (PER == 2) *reinterpret_cast<uint32_t*>(out) = pack_bf2(acc[0] * inv, acc[1] * inv);
-  else out[0] = f2bf(acc[0] * inv);
-}
-
-template <int DH>
-__global__ __launch_bounds__(64) void kv8_prefill_kernel(Kv8AttnArgs a) {
-  __shared__ float qs[DH];
-  const int row = blockIdx.x;
-  for (int s = 0; s < a.S; ++s) {
-    const int r0 = max(a.row0[s], 0), r1 = min(a.row0[s + 1], a.T);
-    if (row < r0 || row >= r1) continue;
-    const int64_t n = (int64_t)a.pos0[s] + (row - a.row0[s]) + 1;
-    attend<DH>(a, s, row, blockIdx.y, (int)min(max(n, (int64_t)0), (int64_t)a.bt_stride * kPage), qs);
+    for (int x = C; x < kWave; x *= 2) {
+      const float2 v = make_float2(__shfl_xor(S.M, x, kWave), __shfl_xor(S.L, x, kWave));
+      const float4 y = make_float4(__shfl_xor(S.acc.x, x, kWave), __shfl_xor(S.acc.y, x, kWave),
+                                   __shfl_xor(S.acc.z, x, kWave), __shfl_xor(S.acc.w, x, kWave));
+      S.fold(v, y);
+    }
+    if (lane < C) S.write(out + (h0 + w) * DH);
     return;
   }
+  __shared__ float2 s_ml[H][R];
+  __shared__ float4 s_acc[H][R][C];
+  const int r = threadIdx.x / C;
+  for (int i = 0; i < H && h0 + i < a.Hq; ++i) {
+    const size_t f = first(h0 + i);
+    MergeState<DH> S;
+    S.take(ml + f, o + f * DH, G, n, r, R);
+    if (c == 0) s_ml[i][r] = make_float2(S.M, S.L);
+    s_acc[i][r][c] = S.acc;
+  }
+  __syncthreads();
+  if (w >= H || h0 + w >= a.Hq || lane >= C) return;
+  MergeState<DH> S;
+  for (int j = 0; j < R; ++j) S.fold(s_ml[w][j], s_acc[w][j][lane]);
+  S.write(out + (h0 + w) * DH);
+}
+
+// ------------------------------------------------------------------ prefill
+// One block of queries of a sequence (up to 128 / G of them), or one part of its keys: rows [row, row + nq) at positions
+// pos .. over the key tiles [t0, t1) of 32 positions.  slot < 0: the whole block, whose output it writes; otherwise the
+// partial slot.  Every kv-head runs the same units.
+struct PrefillUnit {
+  int32_t seq, row, nq, pos;
+  int32_t t0, t1, slot, pad;
+};
+// Partial slots [slot0, slot0 + n_part) of a block that was cut
+struct PrefillJob {
+  int32_t row, nq, slot0, n_part;
+};
+struct PrefillHead {
+  int32_t n_units, n_jobs, pad[14];
+};
+struct PrefillWs {
+  int64_t units, jobs, part_o, part_ml, total;   // byte offsets
+  int32_t unit_cap, slots;                       // units; partial slots of a kv-head
+};
+// A block is cut only where the whole blocks are fewer than the CUs: then blocks * Hkv < kCus, and the parts, no longer
+// than an even share of all key tiles over the resident workgroups, number at most kCus + kPrefillResident over all heads.
+// Otherwise sum ceil(n / q) <= T / q + S.
+PrefillWs prefill_ws(int S, int T, int Hq, int Hkv, int dh) {
+  PrefillWs w;
+  const int64_t split = (kCus + kPrefillResident) / Hkv;
+  const int64_t whole = (int64_t)T / prefill_queries_per_item(Hq / Hkv) + S;
+  w.unit_cap = (int32_t)(std::max(split, whole) + 1);
+  w.slots = (int32_t)std::min<int64_t>(split, whole + kPrefillResident / Hkv) + 1;
+  auto al = [](int64_t x) { return (x + 255) & ~int64_t(255); };
+  w.units = sizeof(PrefillHead);
+  w.jobs = al(w.units + w.unit_cap * (int64_t)sizeof(PrefillUnit));
+  w.part_o = al(w.jobs + (kCus + 1) * (int64_t)sizeof(PrefillJob));
+  const int64_t rows = (int64_t)w.slots * Hkv * kPrefillPairs;
+  w.part_ml = al(w.part_o + rows * dh * 4);
+  w.total = w.part_ml + rows * 8;
+  return w;
+}
+
+struct Kv8PrefillArgs {
+  Kv8AttnArgs a;
+  PrefillHead* head;
+  PrefillUnit* units;
+  PrefillJob* jobs;
+  float* part_o;    // [Hkv][slots][128 pairs][dh]: unnormalized
+  float* part_ml;   // [Hkv][slots][128 pairs][2]: (maximum in log2 units, sum)
+  int unit_cap, slots, qpi;
+};
+
+// The units of a batch from row0 and pos0 in device memory, longest first; one workgroup.
+__global__ __launch_bounds__(1024) void kv8_prefill_plan_kernel(Kv8PrefillArgs p) {
+  constexpr int kBins = 1024;
+  __shared__ int32_t pre[1025], wave_sums[16], bins[kBins];
+  const Kv8AttnArgs& a = p.a;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int kcap = a.bt_stride * kPage;
+  auto scan = [&](int v, int& total) {   // exclusive, over the workgroup
+    const int x = wave_scan(v);
+    __syncthreads();
+    if (lane == 63) wave_sums[w] = x;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int i = 0; i < 16; ++i) {
+      if (i < w) before += wave_sums[i];
+      all += wave_sums[i];
+    }
+    total = all;
+    return before + x - v;
+  };
+  auto rows_of = [&](int s, int& r0) {
+    r0 = min(max(a.row0[s], 0), a.T);
+    return max(min(a.row0[s + 1], a.T) - r0, 0);
+  };
+  // f(s, row0 of s, its rows, block j of s, number of the block) for every block; the number of blocks
+  auto blocks = [&](auto&& f) {
+    int base = 0;
+    for (int s0 = 0; s0 < a.S; s0 += 1024) {
+      int r0, total;
+      const int n = s0 + tid < a.S ? rows_of(s0 + tid, r0) : 0;
+      const int before = scan((n + p.qpi - 1) / p.qpi, total);
+      pre[tid] = before;
+      __syncthreads();
+      for (int i = tid; i < total; i += 1024) {
+        int lo = 0, hi = 1024;   // the last sequence whose blocks begin at or before i (empty ones before it)
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (pre[mid] <= i) lo = mid;
+          else hi = mid;
+        }
+        int r;
+        const int m = rows_of(s0 + lo, r);
+        f(s0 + lo, r, m, i - pre[lo], base + i);
+      }
+      base += total;
+    }
+    return base;
+  };
+  auto unit_of = [&](int s, int r0, int n, int j) {
+    PrefillUnit u;
+    u.seq = s;
+    u.row = r0 + j * p.qpi;
+    u.nq = min(p.qpi, n - j * p.qpi);
+    u.pos = min(max(a.pos0[s], -(1 << 30)), kcap) + j * p.qpi;
+    u.t0 = 0;
+    u.t1 = (max(min(u.pos + u.nq, kcap), 0) + 31) / 32;
+    u.slot = -1;
+    u.pad = 0;
+    return u;
+  };
+  for (int i = tid; i < kBins; i += 1024) bins[i] = 0;
+  __syncthreads();
+  // bin of a tile count, so that longer units come first (with under kBins tiles: in exact order)
+  const int shift = max(0, 32 - __clz((kcap + 31) / 32) - 10);
+  auto bin_of = [&](int tiles) { return kBins - 1 - min(tiles >> shift, kBins - 1); };
+  uint32_t mine = 0;   // half the tiles: under 256 blocks of up to 2^25 tiles stay in 32 bits
+  const int n_blocks = blocks([&](int s, int r0, int n, int j, int) {
+    const int t = unit_of(s, r0, n, j).t1;
+    mine += t >> 1;
+    atomicAdd(&bins[bin_of(t)], 1);
+  });
+  __syncthreads();
+  if ((int64_t)n_blocks * a.Hkv >= kCus) {
+    int total;
+    const int at = scan(bins[tid], total);
+    __syncthreads();
+    bins[tid] = at;
+    __syncthreads();
+    blocks([&](int s, int r0, int n, int j, int) {
+      const PrefillUnit u = unit_of(s, r0, n, j);
+      const int i = atomicAdd(&bins[bin_of(u.t1)], 1);
+      if (i < p.unit_cap) p.units[i] = u;
+    });
+    if (tid == 0) {
+      p.head->n_units = min(n_blocks, p.unit_cap);
+      p.head->n_jobs = 0;
+    }
+    return;
+  }
+  // few blocks (under 256, so a thread has one at most): cut the long ones
+  int halves;
+  scan((int)mine, halves);
+  const int64_t tiles = ((int64_t)(uint32_t)halves + n_blocks) * 2;   // no less than their sum
+  const int share = (int)max((tiles * a.Hkv + kPrefillResident - 1) / kPrefillResident, (int64_t)kPrefillMinTiles);
+  PrefillUnit u;
+  int n_part = 0;
+  blocks([&](int s, int r0, int n, int j, int) {
+    u = unit_of(s, r0, n, j);
+    n_part = max(1, (u.t1 + share - 1) / share);
+    n_part = max(1, (u.t1 + (u.t1 + n_part - 1) / n_part - 1) / max(1, (u.t1 + n_part - 1) / n_part));
+  });
+  int n_units, n_slots, n_jobs;
+  const int at = scan(n_part, n_units), slot0 = scan(n_part > 1 ? n_part : 0, n_slots);
+  const int job = scan(n_part > 1 ? 1 : 0, n_jobs);
+  if (n_part > 0) {
+    const int t1 = u.t1, len = (t1 + n_part - 1) / n_part;
+    for (int k = 0; k < n_part; ++k) {
+      u.t0 = k * len;
+      u.t1 = min(t1, u.t0 + len);
+      u.slot = n_part > 1 ? slot0 + k : -1;
+      if (at + k < p.unit_cap && u.slot < p.slots) p.units[at + k] = u;
+    }
+    if (n_part > 1 && job < kCus) p.jobs[job] = PrefillJob{u.row, u.nq, slot0, n_part};
+  }
+  if (tid == 0) {
+    p.head->n_units = min(n_units, p.unit_cap);
+    p.head->n_jobs = min(n_jobs, kCus);
+  }
+}
+
+// Causal attention of a unit and kv-head, as the bf16 cache's prefill kernel computes it: the (query, head) pairs
+// of the block are the columns of
+//   S^T[32 keys x 32 pairs] = K[32 x dh] . Q^T[dh x 32]       (v_mfma_f32_32x32x16_bf16)
+//   O^T[32 dims x 32 pairs] += V^T[32 x 32 keys] . P^T[32 x 32]
+// with 32 pairs per wavefront.  Every wavefront multiplies every key, so a tile of 32 keys is turned into bf16 once
+// for the workgroup, on its way into LDS: a thread loads DH/8 bytes of K and of V, three tiles ahead, into registers,
+// and writes them as exact bf16 (the page's power of two is applied by the conversion) in the order of the matrix
+// operands.  LDS holds three tiles: V of the one multiplied, K of the next, and the one being written; a
+// step multiplies K of tile t + 1 and V of tile t, so that the scores of the next tile and the exponentials of this
+// one run side by side.
+template <int DH>
+__global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
+  constexpr int KS = DH / 16;      // 16-dim steps of QK^T
+  constexpr int DT = DH / 32;      // 32-dim tiles of O^T
+  constexpr int KT = 32 * DH;      // elements of a K (or V) tile of 32 keys
+  constexpr int STAGE = 2 * KT;    // K tile then V tile
+  constexpr int NS = 3;            // tiles in LDS, and tiles in registers on their way
+  __shared__ __attribute__((aligned(1024))) bf16_t L0[STAGE], L1[STAGE], L2[STAGE];
+  auto stage = [&](auto ic) -> bf16_t* {
+    constexpr int I = decltype(ic)::value % NS;
+    if constexpr (I == 0) return L0; else if constexpr (I == 1) return L1; else return L2;
+  };
+  const Kv8AttnArgs& a = p.a;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Workgroup -> (unit, head): heads innermost, so that with 8 of them an XCD works on one head's keys; and among the
+  // first resident workgroups the second half of the units in reverse, so that a CU gets a long one and a short one
+  const int n_units = p.head->n_units;
+  int ui = blockIdx.x / a.Hkv;
+  const int kvh = blockIdx.x - ui * a.Hkv;
+  if (ui >= n_units) return;
+  {
+    const int half = kPrefillResident / 2 / a.Hkv, window = min(n_units, kPrefillResident / a.Hkv);
+    if (ui >= half && ui < window) ui = half + window - 1 - ui;
+  }
+  const PrefillUnit it = p.units[ui];
+  const int G = a.Hq / a.Hkv;
+  const int npairs = it.nq * G;
+  const int kend = min(it.pos + it.nq, a.bt_stride * kPage);   // keys [0, kend) are visible to some pair
+  const int tbase = it.t0, ntiles = it.t1 - it.t0;
+  const int last_page = max(kend - 1, 0) / kPage;
+  // read through the constant address space: uniform loads by the scalar unit, counted apart from the others
+  typedef const __attribute__((address_space(4))) int32_t* cint_t;
+  typedef const __attribute__((address_space(4))) float* cfloat_t;
+  const cint_t bt = (cint_t)(a.bt + (size_t)it.seq * a.bt_stride);
+  const cfloat_t ksp = (cfloat_t)(a.pool.ks + kvh * a.pool.n_blocks);
+  const cfloat_t vsp = (cfloat_t)(a.pool.vs + kvh * a.pool.n_blocks);
+  const int h = lane >> 5;
+
+  const int pair = w * 32 + (lane & 31);
+  const bool pair_ok = pair < npairs;
+  const int qi = pair_ok ? pair / G : 0, hj = pair_ok ? pair % G : 0;
+  const int qpos = pair_ok ? it.pos + qi : -1;   // -1: every key masked
+  const int64_t row = it.row + qi;
+  const int col0 = (kvh * G + hj) * DH;
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)   // (a column past the pairs computes with row 0, fully masked)
+    qf[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(a.q + row * a.q_stride + col0 + ks * 16 + h * 8));
+
+  // What this thread moves of a tile: page pg of its two, half hw of the page's K chunks, and of V the groups of four
+  // tokens hw and hw + 2 (the order in which the keys of the P^T operand lie) of DH/64 dimensions.
+  const int pg = w >> 1, hw = w & 1;
+  struct Raw {
+    uint32_t k[DH / 32], v[DH / 32];
+    float ks, vs;
+  };
+  const int k_src = hw * (DH * 8) + lane * (DH / 8);
+  const int v_src = (hw * DH + lane * (DH / 64)) * 4;
+  uint32_t gone = 0;   // two bits for each of the last 16 tiles: its pages that are no page of the pool
+  auto load = [&](Raw& R, int t) __attribute__((always_inline)) {
+    const int page = (tbase + t) * 2;
+    const int e0 = bt[min(page, last_page)], e1 = bt[min(page + 1, last_page)];
+    const bool ok0 = (uint32_t)e0 < (uint64_t)a.pool.n_blocks, ok1 = (uint32_t)e1 < (uint64_t)a.pool.n_blocks;
+    const int sh = (t & 15) * 2;
+    gone = (gone & ~(3u << sh)) | ((ok0 ? 0u : 1u) | (ok1 ? 0u : 2u)) << sh;
+    const bool ok = pg ? ok1 : ok0;
+    const int e = ok ? (pg ? e1 : e0) : 0;
+    const float ks = ksp[e], vs = vsp[e];   // (entry 0 exists: a load without a branch)
+    R.ks = ok ? ks : 1.f;
+    R.vs = ok ? vs : 1.f;
+    const size_t tile = kv_tile(kvh, a.pool.n_blocks, e, DH);
+    const uint8_t* k = a.pool.k + tile + k_src;
+    const uint8_t* v = a.pool.v + tile + v_src;
+    if constexpr (DH == 128) {
+      const uint4 x = *reinterpret_cast<const uint4*>(k);
+      R.k[0] = x.x; R.k[1] = x.y; R.k[2] = x.z; R.k[3] = x.w;
+      const uint2 y = *reinterpret_cast<const uint2*>(v), z = *reinterpret_cast<const uint2*>(v + 8 * DH);
+      R.v[0] = y.x; R.v[1] = y.y; R.v[2] = z.x; R.v[3] = z.y;
+    } else {
+      const uint2 x = *reinterpret_cast<const uint2*>(k);
+      R.k[0] = x.x; R.k[1] = x.y;
+      R.v[0] = *reinterpret_cast<const uint32_t*>(v);
+      R.v[1] = *reinterpret_cast<const uint32_t*>(v + 8 * DH);
+    }
+  };
+  // K: DH/64 chunks of 8 dimensions of one token; V: 8 positions of DH/64 dimensions.  The halves of V rows of
+  // dimensions 8..15 (mod 16) change places, so that the 16 lanes of one read of V^T hit distinct banks.
+  const int k_dst = pg * (KT / 2) + (DH == 128 ? ((hw * 8 + (lane >> 4) * 2) * 16 + (lane & 15)) * 8
+                                               : ((hw * 4 + (lane >> 5) * 2 + (lane & 1)) * 16 + ((lane & 31) >> 1)) * 8);
+  auto store = [&](const Raw& R, bf16_t* base, int t) __attribute__((always_inline)) {
+    uint32_t keep_lo = ~0u, keep_hi = ~0u;
+    const int k0 = (tbase + t) * 32;
+    if (k0 + 32 > kend || (gone >> ((t & 15) * 2) & 3)) {   // places that do not count may hold NaN codes
+      const int tok = k0 + pg * kPage + hw * 4;
+      const bool there = !(gone >> ((t & 15) * 2 + pg) & 1);
+      keep_lo = there ? keep_bytes(kend - tok) : 0;
+      keep_hi = there ? keep_bytes(kend - tok - 8) : 0;
+    }
+#pragma unroll
+    for (int c = 0; c < DH / 64; ++c) {
+      const uint2 lo = e4m3x4_to_bf16(R.k[2 * c], R.ks), hi = e4m3x4_to_bf16(R.k[2 * c + 1], R.ks);
+      *reinterpret_cast<uint4*>(base + k_dst + c * 128) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+#pragma unroll
+    for (int c = 0; c < DH / 64; ++c) {
+      const int d = lane * (DH / 64) + c;
+      const uint2 lo = e4m3x4_to_bf16(R.v[c] & keep_lo, R.vs), hi = e4m3x4_to_bf16(R.v[DH / 64 + c] & keep_hi, R.vs);
+      *reinterpret_cast<uint4*>(base + KT + (pg * DH + d) * 16 + (hw ^ ((d >> 3) & 1)) * 8) =
+          make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+  };
+
+  f32x16 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+  float m = -1e30f, l = 0.f;   // finite, so that a fully masked pair keeps zero weights
+  const int k_off = ((lane & 31) >> 4) * (KT / 2) + (lane & 15) * 8 + h * 128;
+  const int v_off = KT + (lane & 31) * 16 + (h ^ ((lane >> 3) & 1)) * 8;
+  bf16x8 kf[KS];
+  auto read_k = [&](const bf16_t* base) __attribute__((always_inline)) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kf[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(base + k_off + ks * 256));
+  };
+  auto scores = [&]() __attribute__((always_inline)) {
+    f32x16 x;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) x = mfma32x32x16(kf[ks], qf[ks], x);
+    return x;
+  };
+  auto score_max = [&](const f32x16& x) __attribute__((always_inline)) {
+    float v = x[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) v = fmaxf(v, x[r]);
+    return half_swap_max(v) * a.scale_log2;
+  };
+  // the mask of a tile that needs one, then the reference maximum, which moves only where a score exceeds it by 2^8
+  auto settle = [&](f32x16& x, float& mx, int t) __attribute__((always_inline)) {
+    const int k0 = (tbase + t) * 32;
+    const uint32_t miss = gone >> ((t & 15) * 2) & 3;
+    if (k0 + 32 > kend || k0 + 31 > it.pos || miss) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = k0 + (r >> 2) * 8 + h * 4 + (r & 3);
+        if (key > qpos || key >= kend || (miss >> (r >> 3) & 1)) x[r] = kNegInf;
+      }
+      mx = score_max(x);
+    }
+    if (__any(mx > m + 8.f)) {
+      const float m_new = fmaxf(m, mx);
+      const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
+    }
+  };
+  uint4 vv[2][DT];
+  auto read_v = [&](const bf16_t* base) __attribute__((always_inline)) {
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) vv[st][dt] = *reinterpret_cast<const uint4*>(base + v_off + (st * DH + dt * 32) * 16);
+  };
+  bf16x8 pf[2];
+  auto probs = [&](const f32x16& x) __attribute__((always_inline)) {
+    float ps = 0.f;
+    float pv[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      pv[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale_log2, -m));
+      ps += pv[r];
+    }
+    l += ps;
+    // rounded to bf16, the type of the matrix operand; the denominator is not
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      bf16x8 v;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = (__bf16)pv[st * 8 + j];
+      pf[st] = v;
+    }
+  };
+  auto accumulate = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32x32x16(as_bf16x8(vv[st][dt]), pf[st], o[dt]);
+  };
+
+  // order of a step's second half: the K reads, the first exponentials, then one MFMA at a time (QK^T of the next
+  // tile, then V^T . P^T) with a V read and softmax work between
+  auto interleave = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_group_barrier(0x100, KS, 0);   // LDS reads
+    __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);    // VALU
+    __builtin_amdgcn_sched_group_barrier(0x400, 4, 0);    // exponentials
+    static_for<KS>([&](auto) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+    });
+    static_for<2 * DT>([&](auto) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+    });
+  };
+
+  if (ntiles > 0) {
+    // Past the last tile a step moves and scores the last one again, which nothing uses: no step has a branch, so
+    // the loads in flight stay counted.
+    Raw R[NS];
+    auto fetch = [&](Raw& r, int t) __attribute__((always_inline)) { load(r, min(t, ntiles - 1)); };
+    static_for<NS>([&](auto ic) { fetch(R[ic], decltype(ic)::value); });
+    static_for<NS - 1>([&](auto ic) {
+      constexpr int J = decltype(ic)::value;
+      store(R[J], stage(ic), J);
+      fetch(R[J], J + NS);
+    });
+    __syncthreads();
+    read_k(L0);
+    f32x16 s = scores();
+    float mx = score_max(s);
+    // a step: tile t + 2 into LDS, tile t + 5 on its way, scores of t + 1, output of t
+    auto step = [&](auto ic, int t) __attribute__((always_inline)) {
+      constexpr int J = decltype(ic)::value;
+      constexpr int W = (J + 2) % NS;
+      store(R[W], stage(std::integral_constant<int, W>{}), t + 2);
+      fetch(R[W], t + 2 + NS);
+      settle(s, mx, t);
+      __builtin_amdgcn_sched_barrier(0);
+      read_k(stage(std::integral_constant<int, J + 1>{}));
+      read_v(stage(ic));
+      probs(s);
+      const f32x16 next = scores();
+      accumulate();
+      mx = score_max(next);
+      s = next;
+      interleave();
+      __builtin_amdgcn_sched_barrier(0);
+      __syncthreads();
+    };
+    for (int t = 0;; t += NS) {
+      step(std::integral_constant<int, 0>{}, t);
+      if (t + 1 >= ntiles) break;
+      step(std::integral_constant<int, 1>{}, t + 1);
+      if (t + 2 >= ntiles) break;
+      step(std::integral_constant<int, 2>{}, t + 2);
+      if (t + 3 >= ntiles) break;
+    }
+  }
+
+  const float lt = l + __shfl_xor(l, 32, kWave);
+  if (!pair_ok) return;
+  if (it.slot >= 0) {
+    const size_t slot = ((size_t)kvh * p.slots + it.slot) * kPrefillPairs + pair;
+    float* po = p.part_o + slot * DH;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4)
+        *reinterpret_cast<float4*>(po + dt * 32 + g4 * 8 + h * 4) =
+            make_float4(o[dt][g4 * 4], o[dt][g4 * 4 + 1], o[dt][g4 * 4 + 2], o[dt][g4 * 4 + 3]);
+    if (h == 0) *reinterpret_cast<float2*>(p.part_ml + slot * 2) = make_float2(m, lt);
+    return;
+  }
+  const float inv = lt == 0.f ? 0.f : 1.f / lt;
+  uint16_t* out = a.out + row * a.out_stride + col0;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4)
+      *reinterpret_cast<uint2*>(out + dt * 32 + g4 * 8 + h * 4) =
+          make_uint2(pack_bf2(o[dt][g4 * 4] * inv, o[dt][g4 * 4 + 1] * inv),
+                     pack_bf2(o[dt][g4 * 4 + 2] * inv, o[dt][g4 * 4 + 3] * inv));
+}
+
+// Joins the parts of cut blocks: DH/4 threads a (query, head) pair, 256 / (DH/4) pairs a workgroup.
+template <int DH>
+__global__ __launch_bounds__(256) void kv8_prefill_merge_kernel(Kv8PrefillArgs p) {
+  constexpr int C = DH / 4, PPB = 256 / C;
+  const Kv8AttnArgs& a = p.a;
+  const int job = blockIdx.x / (kPrefillPairs / PPB);
+  const int jb = job / a.Hkv, kvh = job - jb * a.Hkv;
+  if (jb >= p.head->n_jobs) return;
+  const PrefillJob mg = p.jobs[jb];
+  const int G = a.Hq / a.Hkv;
+  const int pair = (blockIdx.x % (kPrefillPairs / PPB)) * PPB + threadIdx.x / C, c = threadIdx.x % C;
+  if (pair >= mg.nq * G) return;
+  const size_t slot = ((size_t)kvh * p.slots + mg.slot0) * kPrefillPairs + pair;
+  MergeState<DH> S;
+  S.take(reinterpret_cast<const float2*>(p.part_ml) + slot, p.part_o + slot * DH + c * 4, kPrefillPairs, mg.n_part, 0, 1);
+  const int qi = pair / G, hj = pair - qi * G;
+  S.write(a.out + (int64_t)(mg.row + qi) * a.out_stride + (kvh * G + hj) * DH + c * 4);
 }
 
 }  // namespace
@@ -343,25 +828,50 @@ static int64_t decode_ml_offset(int B, int Hq, int Hkv, int dh) { return kv8_dec
 int64_t kv8_decode_ws_bytes(int B, int Hq, int Hkv, int dh) {
   return decode_ml_offset(B, Hq, Hkv, dh) + kv8_decode_items(B, Hkv) * (Hq / Hkv) * 8;
 }
-int64_t kv8_prefill_ws_bytes(int, int, int, int, int) { return 256; }
+int64_t kv8_prefill_ws_bytes(int S, int T, int Hq, int Hkv, int dh) { return prefill_ws(S, T, Hq, Hkv, dh).total; }
 
 hipError_t kv8_decode_launch(const Kv8AttnArgs& args, hipStream_t st) {
   Kv8AttnArgs a = args;
   a.ws_ml = decode_ml_offset(a.S, a.Hq, a.Hkv, a.dh);
-  const dim3 grid((unsigned)kv8_decode_items(a.S, a.Hkv)), merge((unsigned)(((int64_t)a.S * a.Hq + 3) / 4));
+  const dim3 grid((unsigned)kv8_decode_items(a.S, a.Hkv));
   if (a.dh == 128) hipLaunchKernelGGL(kv8_decode_kernel<128>, grid, dim3(64), 0, st, a);
   else hipLaunchKernelGGL(kv8_decode_kernel<64>, grid, dim3(64), 0, st, a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (a.dh == 128) hipLaunchKernelGGL(kv8_merge_kernel<128>, merge, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(kv8_merge_kernel<64>, merge, dim3(256), 0, st, a);
-  return hipGetLastError();
+  const int64_t quads = (int64_t)a.S * ((a.Hq + 3) / 4);
+  auto merge = [&](auto kernel, int64_t groups) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, st, a);
+    return hipGetLastError();
+  };
+  if (quads < kCus && a.bt_stride > kMergeAlone * kKv8MinPages)
+    return a.dh == 128 ? merge(kv8_merge_kernel<128, 1>, (int64_t)a.S * a.Hq) : merge(kv8_merge_kernel<64, 1>, (int64_t)a.S * a.Hq);
+  return a.dh == 128 ? merge(kv8_merge_kernel<128, 4>, quads) : merge(kv8_merge_kernel<64, 4>, quads);
 }
 
 hipError_t kv8_prefill_launch(const Kv8AttnArgs& a, hipStream_t st) {
-  const dim3 grid(a.T, a.Hq);
-  if (a.dh == 128) hipLaunchKernelGGL(kv8_prefill_kernel<128>, grid, dim3(64), 0, st, a);
-  else hipLaunchKernelGGL(kv8_prefill_kernel<64>, grid, dim3(64), 0, st, a);
-  return hipGetLastError();
+  const PrefillWs w = prefill_ws(a.S, a.T, a.Hq, a.Hkv, a.dh);
+  Kv8PrefillArgs p{};
+  p.a = a;
+  p.head = reinterpret_cast<PrefillHead*>(a.ws);
+  p.units = reinterpret_cast<PrefillUnit*>(a.ws + w.units);
+  p.jobs = reinterpret_cast<PrefillJob*>(a.ws + w.jobs);
+  p.part_o = reinterpret_cast<float*>(a.ws + w.part_o);
+  p.part_ml = reinterpret_cast<float*>(a.ws + w.part_ml);
+  p.unit_cap = w.unit_cap;
+  p.slots = w.slots;
+  p.qpi = prefill_queries_per_item(a.Hq / a.Hkv);
+  auto go = [&](auto kernel, int64_t grid, int threads) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, st, p);
+    return hipGetLastError();
+  };
+  hipError_t e = go(kv8_prefill_plan_kernel, 1, 1024);
+  if (e != hipSuccess) return e;
+  const int64_t grid = (int64_t)w.unit_cap * a.Hkv;
+  e = a.dh == 128 ? go(kv8_prefill_kernel<128>, grid, 256) : go(kv8_prefill_kernel<64>, grid, 256);
+  if (e != hipSuccess) return e;
+  // cut blocks number under kCus / Hkv, and no more than there are blocks
+  const int64_t jobs = std::min<int64_t>((int64_t)a.T / p.qpi + a.S, (kCus + a.Hkv - 1) / a.Hkv) * a.Hkv;
+  return a.dh == 128 ? go(kv8_prefill_merge_kernel<128>, jobs * (kPrefillPairs / 8), 256)
+                     : go(kv8_prefill_merge_kernel<64>, jobs * (kPrefillPairs / 16), 256);
 }
 
 }  // namespace hxf

@@ -449,7 +449,7 @@ bool rows_ok(const void* p, int64_t stride, int64_t width) {
 // (wavefront and grid indices are 32 bits wide)
 bool batch_ok(int64_t n, int Hq) { return n * Hq < (int64_t(1) << 29); }
 
-bool table_ok(const int32_t* bt, int32_t bt_stride) { return bt && bt_stride > 0 && bt_stride < (1 << 27); }
+bool table_ok(const int32_t* bt, int32_t bt_stride) { return bt && bt_stride > 0 && bt_stride < (1 << 26); }
 
 }  // namespace
 
@@ -536,7 +536,7 @@ int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_p
 }
 
 int64_t hxf_op_prefill_attention_kv8_workspace_bytes(int32_t S, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh) {
-  if (S < 0 || T < 0 || !shapes_ok(Hq, Hkv, dh)) return -1;
+  if (S < 0 || T < 0 || !shapes_ok(Hq, Hkv, dh) || !batch_ok((int64_t)S + T, Hq)) return -1;
   return kv8_prefill_ws_bytes(S, T, Hq, Hkv, dh);
 }
 
@@ -545,7 +545,8 @@ int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_
                                  int64_t out_stride, int32_t S, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh,
                                  void* workspace, int64_t ws_bytes, void* stream) {
   if (S < 0 || T < 0 || !shapes_ok(Hq, Hkv, dh) || !pool_ok(pool) || !table_ok(bt, bt_stride) || !row0 || !pos0 ||
-      !rows_ok(q, q_stride, (int64_t)Hq * dh) || !rows_ok(out, out_stride, (int64_t)Hq * dh))
+      !rows_ok(q, q_stride, (int64_t)Hq * dh) || !rows_ok(out, out_stride, (int64_t)Hq * dh) ||
+      !batch_ok((int64_t)S + T, Hq))
     return HXF_EINVAL;
   if (S == 0 || T == 0) return HXF_OK;
   if (!workspace || !aligned16(workspace) || ws_bytes < kv8_prefill_ws_bytes(S, T, Hq, Hkv, dh)) return HXF_ENOMEM;

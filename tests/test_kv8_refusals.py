@@ -42,7 +42,7 @@ def _slot_map(**k):
 
 @pytest.mark.parametrize("bad", [dict(start=None), dict(n_new=None), dict(S=-1), dict(S=hxf.SLOT_MAP_MAX_SEQS + 1),
                                  dict(free_pages=None), dict(n_free=None), dict(free_cap=-1), dict(bt=None),
-                                 dict(bt_stride=0), dict(bt_stride=1 << 27), dict(row0=None), dict(pos=None),
+                                 dict(bt_stride=0), dict(bt_stride=1 << 26), dict(row0=None), dict(pos=None),
                                  dict(slot=None), dict(T=-1), dict(ctx=None), dict(status=None)])
 def test_slot_map_refuses(bad):
     _refused(hxf.EINVAL, _slot_map, **bad)
@@ -72,7 +72,7 @@ def _decode(**k):
 
 
 @pytest.mark.parametrize("bad", [dict(q=None), dict(q=A + 8), dict(q_stride=511), dict(q_stride=504), dict(bt=None),
-                                 dict(bt_stride=0), dict(bt_stride=1 << 27), dict(ctx=None), dict(out=None),
+                                 dict(bt_stride=0), dict(bt_stride=1 << 26), dict(ctx=None), dict(out=None),
                                  dict(out=A + 2), dict(out_stride=500), dict(B=-1), dict(Hq=6, Hkv=4), dict(Hkv=-2),
                                  dict(Hq=68), dict(dh=32), dict(pool=None)] + [dict(pool=_pool(**p)) for p in BAD_POOLS])
 def test_decode_refuses(bad):
@@ -97,7 +97,7 @@ def _prefill(**k):
 
 
 @pytest.mark.parametrize("bad", [dict(q=None), dict(q=A + 8), dict(q_stride=511), dict(q_stride=504), dict(bt=None),
-                                 dict(bt_stride=0), dict(bt_stride=1 << 27), dict(row0=None), dict(pos0=None),
+                                 dict(bt_stride=0), dict(bt_stride=1 << 26), dict(row0=None), dict(pos0=None),
                                  dict(out=None), dict(out=A + 2), dict(out_stride=500), dict(S=-1), dict(T=-1),
                                  dict(Hq=6, Hkv=4), dict(Hkv=-2), dict(Hq=68), dict(dh=32), dict(pool=None)] +
                          [dict(pool=_pool(**p)) for p in BAD_POOLS])
