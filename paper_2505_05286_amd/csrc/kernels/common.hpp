@@ -99,6 +99,12 @@ template <int CACHE = 0>
 __device__ __forceinline__ uint4 buf_load16(rsrc_t r, int lane_off, int scalar_off) {
   return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_off, scalar_off, CACHE));
 }
+__device__ __forceinline__ uint2 buf_load8(rsrc_t r, int lane_off, int scalar_off) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, lane_off, scalar_off, 0));
+}
+__device__ __forceinline__ uint32_t buf_load4(rsrc_t r, int lane_off, int scalar_off) {
+  return __builtin_amdgcn_raw_buffer_load_b32(r, lane_off, scalar_off, 0);
+}
 
 // s_waitcnt vmcnt(N) with the other counters left alone (gfx9 encoding)
 template <int N>

@@ -343,7 +343,8 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a) {
 
 // ------------------------------------------------------------------ prefill
 // One block of queries of a sequence (up to 128 / G of them), or one part of its keys: rows [row, row + nq) at positions
-// pos .. over the key tiles [t0, t1) of 32 positions.  slot < 0: the whole block, whose output it writes; otherwise the
+// pos .. over the key tiles [t0, t1) of 32 positions, an even
+// number of them.  slot < 0: the whole block, whose output it writes; otherwise the
 // partial slot.  Every kv-head runs the same units.
 struct PrefillUnit {
   int32_t seq, row, nq, pos;
@@ -444,7 +445,7 @@ __global__ __launch_bounds__(1024) void kv8_prefill_plan_kernel(Kv8PrefillArgs p
     u.nq = min(p.qpi, n - j * p.qpi);
     u.pos = min(max(a.pos0[s], -(1 << 30)), kcap) + j * p.qpi;
     u.t0 = 0;
-    u.t1 = (max(min(u.pos + u.nq, kcap), 0) + 31) / 32;
+    u.t1 = (max(min(u.pos + u.nq, kcap), 0) + 63) / 64 * 2;
     u.slot = -1;
     u.pad = 0;
     return u;
@@ -487,14 +488,15 @@ __global__ __launch_bounds__(1024) void kv8_prefill_plan_kernel(Kv8PrefillArgs p
   int n_part = 0;
   blocks([&](int s, int r0, int n, int j, int) {
     u = unit_of(s, r0, n, j);
-    n_part = max(1, (u.t1 + share - 1) / share);
-    n_part = max(1, (u.t1 + (u.t1 + n_part - 1) / n_part - 1) / max(1, (u.t1 + n_part - 1) / n_part));
+    const int pairs = u.t1 / 2;   // pairs of tiles
+    const int len = max(1, (pairs + max(1, (u.t1 + share - 1) / share) - 1) / max(1, (u.t1 + share - 1) / share));
+    n_part = max(1, (pairs + len - 1) / len);
   });
   int n_units, n_slots, n_jobs;
   const int at = scan(n_part, n_units), slot0 = scan(n_part > 1 ? n_part : 0, n_slots);
   const int job = scan(n_part > 1 ? 1 : 0, n_jobs);
   if (n_part > 0) {
-    const int t1 = u.t1, len = (t1 + n_part - 1) / n_part;
+    const int t1 = u.t1, len = (t1 / 2 + n_part - 1) / n_part * 2;
     for (int k = 0; k < n_part; ++k) {
       u.t0 = k * len;
       u.t1 = min(t1, u.t0 + len);
@@ -514,23 +516,16 @@ __global__ __launch_bounds__(1024) void kv8_prefill_plan_kernel(Kv8PrefillArgs p
 //   S^T[32 keys x 32 pairs] = K[32 x dh] . Q^T[dh x 32]       (v_mfma_f32_32x32x16_bf16)
 //   O^T[32 dims x 32 pairs] += V^T[32 x 32 keys] . P^T[32 x 32]
 // with 32 pairs per wavefront.  Every wavefront multiplies every key, so a tile of 32 keys is turned into bf16 once
-// for the workgroup, on its way into LDS: a thread loads DH/8 bytes of K and of V, three tiles ahead, into registers,
+// for the workgroup, on its way into LDS: a thread loads DH/8 bytes of K and of V, two tiles ahead, into registers,
 // and writes them as exact bf16 (the page's power of two is applied by the conversion) in the order of the matrix
-// operands.  LDS holds three tiles: V of the one multiplied, K of the next, and the one being written; a
-// step multiplies K of tile t + 1 and V of tile t, so that the scores of the next tile and the exponentials of this
-// one run side by side.
+// operands.  A step multiplies K of tile t + 1 and V of tile t, so that the scores of the next tile and the
+// exponentials of this one run side by side; the conversions run beside the product with V.
 template <int DH>
 __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   constexpr int KS = DH / 16;      // 16-dim steps of QK^T
   constexpr int DT = DH / 32;      // 32-dim tiles of O^T
   constexpr int KT = 32 * DH;      // elements of a K (or V) tile of 32 keys
-  constexpr int STAGE = 2 * KT;    // K tile then V tile
-  constexpr int NS = 3;            // tiles in LDS, and tiles in registers on their way
-  __shared__ __attribute__((aligned(1024))) bf16_t L0[STAGE], L1[STAGE], L2[STAGE];
-  auto stage = [&](auto ic) -> bf16_t* {
-    constexpr int I = decltype(ic)::value % NS;
-    if constexpr (I == 0) return L0; else if constexpr (I == 1) return L1; else return L2;
-  };
+  __shared__ __attribute__((aligned(1024))) bf16_t K0[KT], K1[KT], V0[KT], V1[KT];
   const Kv8AttnArgs& a = p.a;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Workgroup -> (unit, head): heads innermost, so that with 8 of them an XCD works on one head's keys; and among the
@@ -549,12 +544,9 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   const int kend = min(it.pos + it.nq, a.bt_stride * kPage);   // keys [0, kend) are visible to some pair
   const int tbase = it.t0, ntiles = it.t1 - it.t0;
   const int last_page = max(kend - 1, 0) / kPage;
-  // read through the constant address space: uniform loads by the scalar unit, counted apart from the others
-  typedef const __attribute__((address_space(4))) int32_t* cint_t;
-  typedef const __attribute__((address_space(4))) float* cfloat_t;
-  const cint_t bt = (cint_t)(a.bt + (size_t)it.seq * a.bt_stride);
-  const cfloat_t ksp = (cfloat_t)(a.pool.ks + kvh * a.pool.n_blocks);
-  const cfloat_t vsp = (cfloat_t)(a.pool.vs + kvh * a.pool.n_blocks);
+  const int32_t* bt = a.bt + (size_t)it.seq * a.bt_stride;
+  const float* ksp = a.pool.ks + kvh * a.pool.n_blocks;
+  const float* vsp = a.pool.vs + kvh * a.pool.n_blocks;
   const int h = lane >> 5;
 
   const int pair = w * 32 + (lane & 31);
@@ -571,63 +563,103 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   // What this thread moves of a tile: page pg of its two, half hw of the page's K chunks, and of V the groups of four
   // tokens hw and hw + 2 (the order in which the keys of the P^T operand lie) of DH/64 dimensions.
   const int pg = w >> 1, hw = w & 1;
-  struct Raw {
-    uint32_t k[DH / 32], v[DH / 32];
-    float ks, vs;
-  };
   const int k_src = hw * (DH * 8) + lane * (DH / 8);
   const int v_src = (hw * DH + lane * (DH / 64)) * 4;
-  uint32_t gone = 0;   // two bits for each of the last 16 tiles: its pages that are no page of the pool
-  auto load = [&](Raw& R, int t) __attribute__((always_inline)) {
-    const int page = (tbase + t) * 2;
-    const int e0 = bt[min(page, last_page)], e1 = bt[min(page + 1, last_page)];
-    const bool ok0 = (uint32_t)e0 < (uint64_t)a.pool.n_blocks, ok1 = (uint32_t)e1 < (uint64_t)a.pool.n_blocks;
-    const int sh = (t & 15) * 2;
-    gone = (gone & ~(3u << sh)) | ((ok0 ? 0u : 1u) | (ok1 ? 0u : 2u)) << sh;
-    const bool ok = pg ? ok1 : ok0;
-    const int e = ok ? (pg ? e1 : e0) : 0;
-    const float ks = ksp[e], vs = vsp[e];   // (entry 0 exists: a load without a branch)
-    R.ks = ok ? ks : 1.f;
-    R.vs = ok ? vs : 1.f;
-    const size_t tile = kv_tile(kvh, a.pool.n_blocks, e, DH);
-    const uint8_t* k = a.pool.k + tile + k_src;
-    const uint8_t* v = a.pool.v + tile + v_src;
-    if constexpr (DH == 128) {
-      const uint4 x = *reinterpret_cast<const uint4*>(k);
-      R.k[0] = x.x; R.k[1] = x.y; R.k[2] = x.z; R.k[3] = x.w;
-      const uint2 y = *reinterpret_cast<const uint2*>(v), z = *reinterpret_cast<const uint2*>(v + 8 * DH);
-      R.v[0] = y.x; R.v[1] = y.y; R.v[2] = z.x; R.v[3] = z.y;
-    } else {
-      const uint2 x = *reinterpret_cast<const uint2*>(k);
-      R.k[0] = x.x; R.k[1] = x.y;
-      R.v[0] = *reinterpret_cast<const uint32_t*>(v);
-      R.v[1] = *reinterpret_cast<const uint32_t*>(v + 8 * DH);
+  // Tables of 64 pages (32 tiles), one page a lane: the pages being loaded and the 64 after them, and the scales of the
+  // pages being loaded and of those being stored.  A scale of 0 marks an entry that is no page.  (Scalar loads of each
+  // tile's entries would leave no LDS read's wait without theirs.)
+  auto entries = [&](int r0) { return bt[min(tbase * 2 + r0 + lane, last_page)]; };
+  int blk = 0, blk_next = 0;
+  float ks_next = 0.f, vs_next = 0.f, ks_now = 0.f, vs_now = 0.f;
+  auto scales = [&]() {
+    const bool there = (uint32_t)blk < (uint32_t)a.pool.n_blocks;
+    blk = there ? blk : 0;
+    const float ks = ksp[blk], vs = vsp[blk];
+    ks_next = there ? ks : 0.f;
+    vs_next = there ? vs : 0.f;
+  };
+  // before K of tile t, a multiple of 32, is loaded; before K of any tile t is stored
+  auto turn_loads = [&](int t) __attribute__((always_inline)) {
+    blk = blk_next;
+    blk_next = entries(t * 2 + kWave);
+    scales();
+  };
+  auto turn_stores = [&](int t) __attribute__((always_inline)) {
+    if ((t & 31) == 0) {
+      ks_now = ks_next;
+      vs_now = vs_next;
     }
   };
+  // V of a tile is loaded and stored a step after its K, with the page and the scale that K looked up
+  typedef uint32_t words_t[DH / 32];
+  int e_last = 0, keep_lo = 0, keep_hi = 0;
+  float vs_last = 1.f;
+  // (one buffer descriptor for each page: scalar work only, and the pools may exceed 4 GiB)
+  auto page_rsrc = [&](const uint8_t* pool) __attribute__((always_inline)) {
+    return make_rsrc(pool + kv_tile(kvh, a.pool.n_blocks, __builtin_amdgcn_readfirstlane(e_last), DH), kPage * DH);
+  };
+  auto load_k = [&](words_t& R, int t) __attribute__((always_inline)) {
+    e_last = __builtin_amdgcn_readlane(blk, (t & 31) * 2 + pg);
+    const rsrc_t rs = page_rsrc(a.pool.k);
+    if constexpr (DH == 128) {
+      const uint4 x = buf_load16(rs, k_src, 0);
+      R[0] = x.x; R[1] = x.y; R[2] = x.z; R[3] = x.w;
+    } else {
+      const uint2 x = buf_load8(rs, k_src, 0);
+      R[0] = x.x; R[1] = x.y;
+    }
+  };
+  auto load_v = [&](words_t& R) __attribute__((always_inline)) {
+    const rsrc_t rs = page_rsrc(a.pool.v);
+    if constexpr (DH == 128) {
+      const uint2 y = buf_load8(rs, v_src, 0), z = buf_load8(rs, v_src, 8 * DH);
+      R[0] = y.x; R[1] = y.y; R[2] = z.x; R[3] = z.y;
+    } else {
+      R[0] = buf_load4(rs, v_src, 0);
+      R[1] = buf_load4(rs, v_src, 8 * DH);
+    }
+  };
+  uint32_t gone = 0;   // two bits for each of the last 16 tiles stored: its pages that are no page of the pool
   // K: DH/64 chunks of 8 dimensions of one token; V: 8 positions of DH/64 dimensions.  The halves of V rows of
   // dimensions 8..15 (mod 16) change places, so that the 16 lanes of one read of V^T hit distinct banks.
   const int k_dst = pg * (KT / 2) + (DH == 128 ? ((hw * 8 + (lane >> 4) * 2) * 16 + (lane & 15)) * 8
                                                : ((hw * 4 + (lane >> 5) * 2 + (lane & 1)) * 16 + ((lane & 31) >> 1)) * 8);
-  auto store = [&](const Raw& R, bf16_t* base, int t) __attribute__((always_inline)) {
-    uint32_t keep_lo = ~0u, keep_hi = ~0u;
-    const int k0 = (tbase + t) * 32;
-    if (k0 + 32 > kend || (gone >> ((t & 15) * 2) & 3)) {   // places that do not count may hold NaN codes
-      const int tok = k0 + pg * kPage + hw * 4;
-      const bool there = !(gone >> ((t & 15) * 2 + pg) & 1);
-      keep_lo = there ? keep_bytes(kend - tok) : 0;
-      keep_hi = there ? keep_bytes(kend - tok - 8) : 0;
-    }
-#pragma unroll
-    for (int c = 0; c < DH / 64; ++c) {
-      const uint2 lo = e4m3x4_to_bf16(R.k[2 * c], R.ks), hi = e4m3x4_to_bf16(R.k[2 * c + 1], R.ks);
-      *reinterpret_cast<uint4*>(base + k_dst + c * 128) = make_uint4(lo.x, lo.y, hi.x, hi.y);
-    }
+  auto store_v = [&](const words_t& R, bf16_t* base) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < DH / 64; ++c) {
       const int d = lane * (DH / 64) + c;
-      const uint2 lo = e4m3x4_to_bf16(R.v[c] & keep_lo, R.vs), hi = e4m3x4_to_bf16(R.v[DH / 64 + c] & keep_hi, R.vs);
-      *reinterpret_cast<uint4*>(base + KT + (pg * DH + d) * 16 + (hw ^ ((d >> 3) & 1)) * 8) =
-          make_uint4(lo.x, lo.y, hi.x, hi.y);
+      const uint2 lo = e4m3x4_to_bf16(R[c] & keep_lo, vs_last), hi = e4m3x4_to_bf16(R[DH / 64 + c] & keep_hi, vs_last);
+      *reinterpret_cast<uint4*>(base + (pg * DH + d) * 16 + (hw ^ ((d >> 3) & 1)) * 8) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+  };
+  // scales and masks of tile t, before its K is stored (in a step: ahead of the matrix work, which waits for nothing
+  // scalar then)
+  float ks_here = 1.f, vs_here = 1.f;
+  int lo_here = 0, hi_here = 0;
+  auto look_up = [&](int t) __attribute__((always_inline)) {
+    const int r = (t & 31) * 2;
+    const int s0 = __builtin_amdgcn_readlane(__float_as_int(ks_now), r), s1 = __builtin_amdgcn_readlane(__float_as_int(ks_now), r + 1);
+    // (selects by arithmetic: branches here would cut the step into pieces that are scheduled apart)
+    const uint32_t there0 = min((uint32_t)s0, 1u), there1 = min((uint32_t)s1, 1u);
+    const int sh = (t & 15) * 2;
+    gone = (gone & ~(3u << sh)) | (3u - there0 - there1 * 2) << sh;
+    const int sk = pg ? s1 : s0, none = (int)(pg ? there1 : there0) - 1;   // none: all ones where the page is none
+    ks_here = __int_as_float(sk | (none & 0x3F800000));
+    const int sv = __builtin_amdgcn_readlane(__float_as_int(vs_now), r + pg);
+    vs_here = __int_as_float(sv | (none & 0x3F800000));
+    // places of V that do not count may hold NaN codes, and zero times NaN is NaN
+    const int left = (kend - ((tbase + t) * 32 + pg * kPage + hw * 4)) & ~none;
+    lo_here = keep_bytes(left);
+    hi_here = keep_bytes(left - 8);
+  };
+  auto store_k = [&](const words_t& R, bf16_t* base) __attribute__((always_inline)) {
+    vs_last = vs_here;
+    keep_lo = lo_here;
+    keep_hi = hi_here;
+#pragma unroll
+    for (int c = 0; c < DH / 64; ++c) {
+      const uint2 lo = e4m3x4_to_bf16(R[2 * c], ks_here), hi = e4m3x4_to_bf16(R[2 * c + 1], ks_here);
+      *reinterpret_cast<uint4*>(base + k_dst + c * 128) = make_uint4(lo.x, lo.y, hi.x, hi.y);
     }
   };
 
@@ -638,7 +670,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
   float m = -1e30f, l = 0.f;   // finite, so that a fully masked pair keeps zero weights
   const int k_off = ((lane & 31) >> 4) * (KT / 2) + (lane & 15) * 8 + h * 128;
-  const int v_off = KT + (lane & 31) * 16 + (h ^ ((lane >> 3) & 1)) * 8;
+  const int v_off = (lane & 31) * 16 + (h ^ ((lane >> 3) & 1)) * 8;
   bf16x8 kf[KS];
   auto read_k = [&](const bf16_t* base) __attribute__((always_inline)) {
 #pragma unroll
@@ -714,66 +746,92 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
       for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32x32x16(as_bf16x8(vv[st][dt]), pf[st], o[dt]);
   };
 
-  // order of a step's second half: the K reads, the first exponentials, then one MFMA at a time (QK^T of the next
-  // tile, then V^T . P^T) with a V read and softmax work between
+  // order of a step's matrix work: the K reads, then QK^T of the next tile one MFMA at a time with a V read and the
+  // exponentials between, then V^T . P^T with the conversions of the tiles to come, their LDS writes and the sums
   auto interleave = [&]() __attribute__((always_inline)) {
     __builtin_amdgcn_sched_group_barrier(0x100, KS, 0);   // LDS reads
     __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);    // VALU
-    __builtin_amdgcn_sched_group_barrier(0x400, 4, 0);    // exponentials
+    __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);    // exponentials
     static_for<KS>([&](auto) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
-      __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 16 * 3 / KS / 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, 16 / KS, 0);
     });
-    static_for<2 * DT>([&](auto) {
+    static_for<2 * DT>([&](auto ic) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
-      __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+      if (decltype(ic)::value % 2) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);   // LDS write
     });
   };
 
   if (ntiles > 0) {
     // Past the last tile a step moves and scores the last one again, which nothing uses: no step has a branch, so
     // the loads in flight stay counted.
-    Raw R[NS];
-    auto fetch = [&](Raw& r, int t) __attribute__((always_inline)) { load(r, min(t, ntiles - 1)); };
-    static_for<NS>([&](auto ic) { fetch(R[ic], decltype(ic)::value); });
-    static_for<NS - 1>([&](auto ic) {
-      constexpr int J = decltype(ic)::value;
-      store(R[J], stage(ic), J);
-      fetch(R[J], J + NS);
-    });
+    // Past the last tile a step moves and scores the last page again, which nothing uses: no step has a branch around
+    // its loads, so that those in flight stay counted.
+    words_t RK0, RK1, RV0, RV1;   // tiles on their way: K of two, V of two
+    blk_next = entries(0);
+    turn_loads(0);
+    turn_stores(0);
+    auto in_order = [] { __builtin_amdgcn_sched_barrier(0); };   // (the loads' order is what the waits count)
+    load_k(RK0, 0);
+    load_v(RV0);
+    load_k(RK1, 1);
+    in_order();
+    load_v(RV1);
+    in_order();
+    look_up(0);
+    store_k(RK0, K0);
+    load_k(RK0, 2);
+    in_order();
+    store_v(RV0, V0);
+    load_v(RV0);
+    in_order();
+    look_up(1);
+    store_k(RK1, K1);
+    load_k(RK1, 3);
+    in_order();
     __syncthreads();
-    read_k(L0);
+    read_k(K0);
     f32x16 s = scores();
     float mx = score_max(s);
-    // a step: tile t + 2 into LDS, tile t + 5 on its way, scores of t + 1, output of t
-    auto step = [&](auto ic, int t) __attribute__((always_inline)) {
-      constexpr int J = decltype(ic)::value;
-      constexpr int W = (J + 2) % NS;
-      store(R[W], stage(std::integral_constant<int, W>{}), t + 2);
-      fetch(R[W], t + 2 + NS);
+    __syncthreads();
+    // a step: V of tile t + 1 and K of t + 2 into LDS, V of t + 3 and K of t + 4 on their way, scores of t + 1, output of t.
+    // Past the last tile it moves and scores the last page again, which nothing uses: no step has a branch around
+    // its loads, so that those in flight stay counted.
+    auto step = [&](words_t& rk, words_t& rv, bf16_t* k_now, bf16_t* k_next, bf16_t* v_now, bf16_t* v_next, int t)
+        __attribute__((always_inline)) {
+      turn_stores(t + 2);
+      look_up(t + 2);
       settle(s, mx, t);
       __builtin_amdgcn_sched_barrier(0);
-      read_k(stage(std::integral_constant<int, J + 1>{}));
-      read_v(stage(ic));
+      read_k(k_next);
+      read_v(v_now);
       probs(s);
       const f32x16 next = scores();
       accumulate();
+      store_v(rv, v_next);
+      store_k(rk, k_now);
       mx = score_max(next);
       s = next;
       interleave();
       __builtin_amdgcn_sched_barrier(0);
+      load_v(rv);
+      load_k(rk, t + 4);
       __syncthreads();
     };
-    for (int t = 0;; t += NS) {
-      step(std::integral_constant<int, 0>{}, t);
-      if (t + 1 >= ntiles) break;
-      step(std::integral_constant<int, 1>{}, t + 1);
-      if (t + 2 >= ntiles) break;
-      step(std::integral_constant<int, 2>{}, t + 2);
-      if (t + 3 >= ntiles) break;
+    // (the tables turn outside of the loop over steps, whose loads stay counted)
+    // (the tables turn outside of the loop over steps, whose loads stay counted; ntiles is even)
+    for (int t = 0;;) {
+      const int stop = min(ntiles, ((t + 4) | 31) - 3);   // the next t with t + 4 a multiple of 32
+      do {
+        step(RK0, RV1, K0, K1, V0, V1, t);
+        step(RK1, RV0, K1, K0, V1, V0, t + 1);
+        t += 2;
+      } while (t < stop);
+      if (t >= ntiles) break;
+      turn_loads(t + 4);
     }
   }
 
