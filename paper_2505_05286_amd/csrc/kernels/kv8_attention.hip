@@ -479,35 +479,49 @@ __global__ __launch_bounds__(1024) void kv8_prefill_plan_kernel(Kv8PrefillArgs p
     }
     return;
   }
-  // few blocks (under 256, so a thread has one at most): cut the long ones
+  // few blocks, under kCus: cut the long ones
   int halves;
   scan((int)mine, halves);
   const int64_t tiles = ((int64_t)(uint32_t)halves + n_blocks) * 2;   // no less than their sum
   const int share = (int)max((tiles * a.Hkv + kPrefillResident - 1) / kPrefillResident, (int64_t)kPrefillMinTiles);
-  PrefillUnit u;
-  int n_part = 0;
-  blocks([&](int s, int r0, int n, int j, int) {
-    u = unit_of(s, r0, n, j);
-    const int pairs = u.t1 / 2;   // pairs of tiles
-    const int len = max(1, (pairs + max(1, (u.t1 + share - 1) / share) - 1) / max(1, (u.t1 + share - 1) / share));
+  __shared__ PrefillUnit whole[kCus];
+  __shared__ int32_t first[kCus];   // a block's first unit
+  blocks([&](int s, int r0, int n, int j, int i) { whole[i] = unit_of(s, r0, n, j); });
+  __syncthreads();
+  int n_part = 0;   // of block tid
+  if (tid < n_blocks) {
+    const int pairs = whole[tid].t1 / 2;   // pairs of tiles
+    const int len = max(1, (pairs + max(1, (2 * pairs + share - 1) / share) - 1) / max(1, (2 * pairs + share - 1) / share));
     n_part = max(1, (pairs + len - 1) / len);
-  });
+  }
   int n_units, n_slots, n_jobs;
   const int at = scan(n_part, n_units), slot0 = scan(n_part > 1 ? n_part : 0, n_slots);
   const int job = scan(n_part > 1 ? 1 : 0, n_jobs);
-  if (n_part > 0) {
-    const int t1 = u.t1, len = (t1 / 2 + n_part - 1) / n_part * 2;
-    for (int k = 0; k < n_part; ++k) {
-      u.t0 = k * len;
-      u.t1 = min(t1, u.t0 + len);
-      u.slot = n_part > 1 ? slot0 + k : -1;
-      if (at + k < p.unit_cap && u.slot < p.slots) p.units[at + k] = u;
+  if (tid < n_blocks) {
+    first[tid] = at;
+    whole[tid].t0 = n_part;
+    whole[tid].slot = slot0;
+    if (n_part > 1) p.jobs[job] = PrefillJob{whole[tid].row, whole[tid].nq, slot0, n_part};
+  }
+  __syncthreads();
+  n_units = min(n_units, p.unit_cap);
+  for (int i = tid; i < n_units; i += 1024) {
+    int lo = 0, hi = n_blocks;   // the last block whose units begin at or before i
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= i) lo = mid;
+      else hi = mid;
     }
-    if (n_part > 1 && job < kCus) p.jobs[job] = PrefillJob{u.row, u.nq, slot0, n_part};
+    PrefillUnit u = whole[lo];
+    const int parts = u.t0, k = i - first[lo], len = (u.t1 / 2 + parts - 1) / parts * 2;
+    u.t0 = k * len;
+    u.t1 = min(u.t1, u.t0 + len);
+    u.slot = parts > 1 ? u.slot + k : -1;
+    p.units[i] = u;
   }
   if (tid == 0) {
-    p.head->n_units = min(n_units, p.unit_cap);
-    p.head->n_jobs = min(n_jobs, kCus);
+    p.head->n_units = n_units;
+    p.head->n_jobs = n_jobs;
   }
 }
 
@@ -860,23 +874,37 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
                      pack_bf2(o[dt][g4 * 4 + 2] * inv, o[dt][g4 * 4 + 3] * inv));
 }
 
-// Joins the parts of cut blocks: DH/4 threads a (query, head) pair, 256 / (DH/4) pairs a workgroup.
+// Joins the parts of cut blocks: DH/4 threads a (query, head) pair and one of R streams of parts, P pairs a
+// workgroup; the workgroups walk the pairs of all jobs, so that a launch with nothing to join (the host does not know)
+// is short.
 template <int DH>
 __global__ __launch_bounds__(256) void kv8_prefill_merge_kernel(Kv8PrefillArgs p) {
-  constexpr int C = DH / 4, PPB = 256 / C;
+  constexpr int C = DH / 4, R = 4, P = 256 / C / R;
   const Kv8AttnArgs& a = p.a;
-  const int job = blockIdx.x / (kPrefillPairs / PPB);
-  const int jb = job / a.Hkv, kvh = job - jb * a.Hkv;
-  if (jb >= p.head->n_jobs) return;
-  const PrefillJob mg = p.jobs[jb];
   const int G = a.Hq / a.Hkv;
-  const int pair = (blockIdx.x % (kPrefillPairs / PPB)) * PPB + threadIdx.x / C, c = threadIdx.x % C;
-  if (pair >= mg.nq * G) return;
-  const size_t slot = ((size_t)kvh * p.slots + mg.slot0) * kPrefillPairs + pair;
-  MergeState<DH> S;
-  S.take(reinterpret_cast<const float2*>(p.part_ml) + slot, p.part_o + slot * DH + c * 4, kPrefillPairs, mg.n_part, 0, 1);
-  const int qi = pair / G, hj = pair - qi * G;
-  S.write(a.out + (int64_t)(mg.row + qi) * a.out_stride + (kvh * G + hj) * DH + c * 4);
+  const int c = threadIdx.x % C, r = threadIdx.x / C % R, pl = threadIdx.x / C / R;
+  __shared__ float2 s_ml[P][R];
+  __shared__ float4 s_acc[P][R][C];
+  const int items = p.head->n_jobs * a.Hkv * (kPrefillPairs / P);
+  for (int i = blockIdx.x; i < items; i += gridDim.x) {
+    const int job = i / (kPrefillPairs / P), jb = job / a.Hkv, kvh = job - jb * a.Hkv;
+    const PrefillJob mg = p.jobs[jb];
+    const int pair0 = i % (kPrefillPairs / P) * P;
+    if (pair0 >= mg.nq * G) continue;   // (uniform over the workgroup)
+    const int pair = pair0 + pl;        // a pair past the block's: its slot exists, its row is not written
+    const size_t slot = ((size_t)kvh * p.slots + mg.slot0) * kPrefillPairs + pair;
+    MergeState<DH> S;
+    S.take(reinterpret_cast<const float2*>(p.part_ml) + slot, p.part_o + slot * DH + c * 4, kPrefillPairs, mg.n_part, r, R);
+    __syncthreads();
+    if (c == 0) s_ml[pl][r] = make_float2(S.M, S.L);
+    s_acc[pl][r][c] = S.acc;
+    __syncthreads();
+    if (r == 0 && pair < mg.nq * G) {
+      for (int j = 1; j < R; ++j) S.fold(s_ml[pl][j], s_acc[pl][j][c]);
+      const int qi = pair / G, hj = pair - qi * G;
+      S.write(a.out + (int64_t)(mg.row + qi) * a.out_stride + (kvh * G + hj) * DH + c * 4);
+    }
+  }
 }
 
 }  // namespace
@@ -926,10 +954,10 @@ hipError_t kv8_prefill_launch(const Kv8AttnArgs& a, hipStream_t st) {
   const int64_t grid = (int64_t)w.unit_cap * a.Hkv;
   e = a.dh == 128 ? go(kv8_prefill_kernel<128>, grid, 256) : go(kv8_prefill_kernel<64>, grid, 256);
   if (e != hipSuccess) return e;
-  // cut blocks number under kCus / Hkv, and no more than there are blocks
+  // cut blocks number under kCus / Hkv, and no more than there are blocks; 256 / (dh / 4) / 4 pairs a workgroup
   const int64_t jobs = std::min<int64_t>((int64_t)a.T / p.qpi + a.S, (kCus + a.Hkv - 1) / a.Hkv) * a.Hkv;
-  return a.dh == 128 ? go(kv8_prefill_merge_kernel<128>, jobs * (kPrefillPairs / 8), 256)
-                     : go(kv8_prefill_merge_kernel<64>, jobs * (kPrefillPairs / 16), 256);
+  const int64_t groups = std::min<int64_t>(jobs * kPrefillPairs / (256 / a.dh), 4 * kCus);
+  return a.dh == 128 ? go(kv8_prefill_merge_kernel<128>, groups, 256) : go(kv8_prefill_merge_kernel<64>, groups, 256);
 }
 
 }  // namespace hxf

@@ -438,6 +438,17 @@ def test_prefill_batches(S, hi_pos, hi_n, heads):
     _prefill(cache, bt, pos0, n, hq, rng, pad=5, what="batch")
 
 
+def test_prefill_few_chunks_among_many_places():
+    """A batch of more than 1024 places of which few have queries, whose long contexts are cut."""
+    rng = np.random.default_rng(15)
+    S = 2300
+    n, pos0 = np.zeros(S, np.int64), np.zeros(S, np.int64)
+    for s, p, m in ((3, 900, 5), (1027, 1500, 2), (1028, 0, 40), (2051, 64, 1), (2299, 700, 33)):
+        pos0[s], n[s] = p, m
+    cache, bt = _attention_case(rng, pos0 + n, 4, 2, 64)
+    _prefill(cache, bt, pos0, n, 4, rng, pad=2, what="places")
+
+
 def test_prefill_entries_that_are_no_page():
     rng = np.random.default_rng(13)
     pos0, n = np.array([80, 0, 300, 0]), np.array([40, 33, 9, 16])
