@@ -200,8 +200,8 @@ int hxf_op_slot_map(const int32_t* start, const int32_t* n_new, int32_t S, const
  * rotation, pos unused); rotated q to q_out (bf16, rows of q_stride elements; NULL: not wanted), k and v to
  * slot[t] of the pools as e4m3 (nearest even, of the unrounded fp32 value).  A page's scale is the least power of two s with
  * max|x| <= 448 s over the finite values written to it (no less than 2^-100); values that are not finite become NaN.
- * Rows of one call that go to one page must be successive rows with successive slots (hxf_op_slot_map makes
- * them so).  When they begin at the page's first token the page starts afresh; otherwise the tokens
+ * Rows of one call that go to one page must be successive rows with successive slots, none of them skipped
+ * (hxf_op_slot_map makes them so).  When they begin at the page's first token the page starts afresh; otherwise the tokens
  * before them stay: the scale is the larger of the page's and the new rows', and where it grows the old codes
  * are requantised.  Tokens behind the new rows are left as they are.  A row whose slot is not in [0, 16 n_blocks), or
  * (with a table) whose pos is not in [0, max_pos), is skipped, its q_out row included.

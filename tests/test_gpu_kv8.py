@@ -212,6 +212,27 @@ def test_write_of_many_sequences(hq, hkv, dh, with_table):
     _write(cache, dev, rng, slot, pos, hq, table, scale=3.0)
 
 
+@pytest.mark.parametrize("hq,hkv,dh", [(4, 2, 64), (8, 8, 128), (40, 8, 128)])
+def test_write_of_decode_rows(hq, hkv, dh):
+    """Many rows that each continue a page of their own, some of which must grow, between chunks and dead rows."""
+    rng = np.random.default_rng(hq + hkv)
+    nb = 130
+    cache = U.Cache(hkv, nb, dh)
+    cache.fill(rng, np.arange(nb), spread=8)
+    dev = DevCache(cache)
+    table = U.rope_table(50, dh)
+    first = np.arange(100) % 16
+    slot = rng.permutation(nb - 30)[:100] * 16 + first
+    slot[rng.permutation(100)[:12]] = -1
+    chunk = (nb - 30 + np.arange(3)) * 16
+    slot = np.concatenate([slot[:37], chunk[0] + np.arange(5), slot[37:70], chunk[1] + np.arange(2), slot[70:],
+                           chunk[2] + 9 + np.arange(7)])
+    pos = rng.integers(0, 50, len(slot))
+    for scale in (0.01, 1.0, 30.0):
+        log(f"write decode rows {hq}/{hkv}x{dh} scale {scale}")
+        _write(cache, dev, rng, slot, pos, hq, table, scale=scale)
+
+
 @pytest.mark.parametrize("dh", [64, 128])
 def test_write_values(dh):
     """Every rounding: all bf16 values near the codes and their midpoints, the ends of the range, subnormal codes,
