@@ -390,10 +390,13 @@ struct Kv8PrefillArgs {
   int unit_cap, slots, qpi;
 };
 
-// The units of a batch from row0 and pos0 in device memory, longest first; one workgroup.
-__global__ __launch_bounds__(1024) void kv8_prefill_plan_kernel(Kv8PrefillArgs p) {
-  constexpr int kBins = 1024;
-  __shared__ int32_t pre[1025], wave_sums[16], bins[kBins];
+// The units of a batch from row0 and pos0 in device memory, longest first; one workgroup, of four wavefronts because
+// most of its time is barriers (@PLAN@ us for 16 chunks; with 16 wavefronts 4.8).
+constexpr int kPlanThreads = 256;
+static_assert(kPlanThreads >= kCus, "a thread for each block of a batch that is cut");
+__global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8PrefillArgs p) {
+  constexpr int kBins = 1024, kWaves = kPlanThreads / kWave, kPer = kBins / kPlanThreads;
+  __shared__ int32_t pre[kPlanThreads], wave_sums[kWaves], bins[kBins];
   const Kv8AttnArgs& a = p.a;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int kcap = a.bt_stride * kPage;
@@ -403,7 +406,7 @@ __global__ __launch_bounds__(1024) void kv8_prefill_plan_kernel(Kv8PrefillArgs p
     if (lane == 63) wave_sums[w] = x;
     __syncthreads();
     int before = 0, all = 0;
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < kWaves; ++i) {
       if (i < w) before += wave_sums[i];
       all += wave_sums[i];
     }
@@ -415,16 +418,21 @@ __global__ __launch_bounds__(1024) void kv8_prefill_plan_kernel(Kv8PrefillArgs p
     return max(min(a.row0[s + 1], a.T) - r0, 0);
   };
   // f(s, row0 of s, its rows, block j of s, number of the block) for every block; the number of blocks
+  int total = 0;
+  bool scanned = false;   // pre and total are those of the only kPlanThreads sequences
   auto blocks = [&](auto&& f) {
     int base = 0;
-    for (int s0 = 0; s0 < a.S; s0 += 1024) {
-      int r0, total;
-      const int n = s0 + tid < a.S ? rows_of(s0 + tid, r0) : 0;
-      const int before = scan((n + p.qpi - 1) / p.qpi, total);
-      pre[tid] = before;
-      __syncthreads();
-      for (int i = tid; i < total; i += 1024) {
-        int lo = 0, hi = 1024;   // the last sequence whose blocks begin at or before i (empty ones before it)
+    for (int s0 = 0; s0 < a.S; s0 += kPlanThreads) {
+      if (!scanned) {
+        int r0;
+        const int n = s0 + tid < a.S ? rows_of(s0 + tid, r0) : 0;
+        const int before = scan((n + p.qpi - 1) / p.qpi, total);
+        pre[tid] = before;
+        scanned = a.S <= kPlanThreads;
+        __syncthreads();
+      }
+      for (int i = tid; i < total; i += kPlanThreads) {
+        int lo = 0, hi = min(kPlanThreads, a.S - s0);   // the last sequence whose blocks begin at or before i (empty ones before it)
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
           if (pre[mid] <= i) lo = mid;
@@ -450,7 +458,7 @@ __global__ __launch_bounds__(1024) void kv8_prefill_plan_kernel(Kv8PrefillArgs p
     u.pad = 0;
     return u;
   };
-  for (int i = tid; i < kBins; i += 1024) bins[i] = 0;
+  for (int i = tid; i < kBins; i += kPlanThreads) bins[i] = 0;
   __syncthreads();
   // bin of a tile count, so that longer units come first (with under kBins tiles: in exact order)
   const int shift = max(0, 32 - __clz((kcap + 31) / 32) - 10);
@@ -463,10 +471,14 @@ __global__ __launch_bounds__(1024) void kv8_prefill_plan_kernel(Kv8PrefillArgs p
   });
   __syncthreads();
   if ((int64_t)n_blocks * a.Hkv >= kCus) {
-    int total;
-    const int at = scan(bins[tid], total);
-    __syncthreads();
-    bins[tid] = at;
+    int all, sum = 0;
+    for (int k = 0; k < kPer; ++k) sum += bins[tid * kPer + k];
+    int at = scan(sum, all);
+    for (int k = 0; k < kPer; ++k) {
+      const int n = bins[tid * kPer + k];
+      bins[tid * kPer + k] = at;
+      at += n;
+    }
     __syncthreads();
     blocks([&](int s, int r0, int n, int j, int) {
       const PrefillUnit u = unit_of(s, r0, n, j);
@@ -505,7 +517,7 @@ __global__ __launch_bounds__(1024) void kv8_prefill_plan_kernel(Kv8PrefillArgs p
   }
   __syncthreads();
   n_units = min(n_units, p.unit_cap);
-  for (int i = tid; i < n_units; i += 1024) {
+  for (int i = tid; i < n_units; i += kPlanThreads) {
     int lo = 0, hi = n_blocks;   // the last block whose units begin at or before i
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -634,16 +646,19 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     }
   };
   uint32_t gone = 0;   // two bits for each of the last 16 tiles stored: its pages that are no page of the pool
-  // K: DH/64 chunks of 8 dimensions of one token; V: 8 positions of DH/64 dimensions.  The halves of V rows of
-  // dimensions 8..15 (mod 16) change places, so that the 16 lanes of one read of V^T hit distinct banks.
+  // K: DH/64 chunks of 8 dimensions of one token; V: 8 positions of DH/64 dimensions.  Among 32 dimensions of V the even
+  // ones come first, and the halves of rows change places by bits 3 and 4 of the row, so that the 16 lanes of a read
+  // (successive dimensions) and of a write (every second one at dh 128) hit distinct banks.
+  auto v_row = [](int d) { return (d & ~31) | (d >> 1 & 15) | (d & 1) << 4; };
+  auto v_half = [](int row, int half) { return half ^ (row >> 3 & 1) ^ (row >> 4 & 1); };
   const int k_dst = pg * (KT / 2) + (DH == 128 ? ((hw * 8 + (lane >> 4) * 2) * 16 + (lane & 15)) * 8
                                                : ((hw * 4 + (lane >> 5) * 2 + (lane & 1)) * 16 + ((lane & 31) >> 1)) * 8);
   auto store_v = [&](const words_t& R, bf16_t* base) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < DH / 64; ++c) {
-      const int d = lane * (DH / 64) + c;
+      const int row = v_row(lane * (DH / 64) + c);
       const uint2 lo = e4m3x4_to_bf16(R[c] & keep_lo, vs_last), hi = e4m3x4_to_bf16(R[DH / 64 + c] & keep_hi, vs_last);
-      *reinterpret_cast<uint4*>(base + (pg * DH + d) * 16 + (hw ^ ((d >> 3) & 1)) * 8) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+      *reinterpret_cast<uint4*>(base + (pg * DH + row) * 16 + v_half(row, hw) * 8) = make_uint4(lo.x, lo.y, hi.x, hi.y);
     }
   };
   // scales and masks of tile t, before its K is stored (in a step: ahead of the matrix work, which waits for nothing
@@ -684,7 +699,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
   float m = -1e30f, l = 0.f;   // finite, so that a fully masked pair keeps zero weights
   const int k_off = ((lane & 31) >> 4) * (KT / 2) + (lane & 15) * 8 + h * 128;
-  const int v_off = (lane & 31) * 16 + (h ^ ((lane >> 3) & 1)) * 8;
+  const int v_off = v_row(lane & 31) * 16 + v_half(v_row(lane & 31), h) * 8;
   bf16x8 kf[KS];
   auto read_k = [&](const bf16_t* base) __attribute__((always_inline)) {
 #pragma unroll
@@ -774,7 +789,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     });
     static_for<2 * DT>([&](auto ic) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
       if (decltype(ic)::value % 2) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);   // LDS write
     });
   };
@@ -820,6 +835,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
       look_up(t + 2);
       settle(s, mx, t);
       __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);   // over the other workgroup's wavefront while that moves tiles
       read_k(k_next);
       read_v(v_now);
       probs(s);
@@ -831,6 +847,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
       s = next;
       interleave();
       __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(0);
       load_v(rv);
       load_k(rk, t + 4);
       __syncthreads();
@@ -949,14 +966,14 @@ hipError_t kv8_prefill_launch(const Kv8AttnArgs& a, hipStream_t st) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, st, p);
     return hipGetLastError();
   };
-  hipError_t e = go(kv8_prefill_plan_kernel, 1, 1024);
+  hipError_t e = go(kv8_prefill_plan_kernel, 1, kPlanThreads);
   if (e != hipSuccess) return e;
   const int64_t grid = (int64_t)w.unit_cap * a.Hkv;
   e = a.dh == 128 ? go(kv8_prefill_kernel<128>, grid, 256) : go(kv8_prefill_kernel<64>, grid, 256);
   if (e != hipSuccess) return e;
   // cut blocks number under kCus / Hkv, and no more than there are blocks; 256 / (dh / 4) / 4 pairs a workgroup
   const int64_t jobs = std::min<int64_t>((int64_t)a.T / p.qpi + a.S, (kCus + a.Hkv - 1) / a.Hkv) * a.Hkv;
-  const int64_t groups = std::min<int64_t>(jobs * kPrefillPairs / (256 / a.dh), 4 * kCus);
+  const int64_t groups = std::min<int64_t>(jobs * kPrefillPairs / (256 / a.dh), 2 * kCus);
   return a.dh == 128 ? go(kv8_prefill_merge_kernel<128>, groups, 256) : go(kv8_prefill_merge_kernel<64>, groups, 256);
 }
 
