@@ -295,7 +295,8 @@ struct Kv8AttnArgs {
   int Hq, Hkv, dh;
   float scale_log2;      // log2(e) / sqrt(dh)
   uint8_t* ws;
-  int64_t ws_ml;         // offset of the partials' (maximum, sum) pairs
+  int64_t ws_ml;         // decode: offset of the partials' (maximum, sum) pairs
+  int32_t* starts;       // decode: parts before each sequence, where a launch makes them
 };
 // Decode work split, made by the kernels themselves from the contexts in device memory.  As for the bf16
 // cache, each (sequence, kv-head) stream of pages is cut into equal parts no longer than an even share of

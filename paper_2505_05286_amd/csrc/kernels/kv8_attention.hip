@@ -8,12 +8,16 @@ namespace {
 
 constexpr float kNegInf = -__builtin_huge_valf();
 
+constexpr int kKv8DecodeScan = 128;
+
 // Pages of sequence b that its context reaches, and its tokens
 __device__ __forceinline__ int ctx_of(const Kv8AttnArgs& a, int b) { return min(max(a.ctx[b], 0), a.bt_stride * kPage); }
 __device__ __forceinline__ int pages_of(int n) { return (n + kPage - 1) / kPage; }
 
-// The longest part of this batch (kv8_target_pages), found by every wavefront for itself from the contexts:
-// one load and a scan for up to 64 sequences, against a launch and a round trip of a list through memory.
+// The longest part of this batch (kv8_target_pages), found by every wavefront for itself from the contexts: with few
+// sequences a load and a scan or two, against a launch and a round trip through memory.  Above kKv8DecodeScan
+// sequences a launch of its own does it once (a.starts); us for contexts of 64 to 128 tokens, 32 + 8 heads, every
+// wavefront / one launch: 64 sequences 9.4 / 12.2, 128 12.0 / 12.4, 256 20 / 18, 1024 111 / 52, 4096 1016 / 194.
 __device__ __forceinline__ int decode_target(const Kv8AttnArgs& a, int lane) {
   int64_t total = 0;
   for (int i0 = 0; i0 < a.S; i0 += kWave) {
@@ -23,6 +27,54 @@ __device__ __forceinline__ int decode_target(const Kv8AttnArgs& a, int lane) {
     total += (int64_t)__builtin_amdgcn_readlane(wave_scan(p >> 20), 63) << 20;
   }
   return (int)min(kv8_target_pages(total, a.S, a.Hkv), (int64_t)1 << 27);
+}
+
+// starts[b]: parts of a kv-head's streams before sequence b, for b = 0 .. S
+__global__ __launch_bounds__(1024) void kv8_decode_plan_kernel(Kv8AttnArgs a) {
+  __shared__ int64_t sums[16];
+  __shared__ int32_t waves[16];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int64_t mine = 0;
+  for (int b = threadIdx.x; b < a.S; b += 1024) mine += pages_of(ctx_of(a, b));
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) mine += __shfl_xor(mine, x, kWave);
+  if (lane == 0) sums[w] = mine;
+  __syncthreads();
+  int64_t total = 0;
+  for (int i = 0; i < 16; ++i) total += sums[i];
+  const int target = (int)min(kv8_target_pages(total, a.S, a.Hkv), (int64_t)1 << 27);
+  int base = 0;
+  for (int b0 = 0; b0 < a.S; b0 += 1024) {
+    const int b = b0 + threadIdx.x;
+    const int n = b < a.S ? kv8_parts(pages_of(ctx_of(a, b)), target) : 0;
+    const int upto = wave_scan(n);
+    __syncthreads();
+    if (lane == 63) waves[w] = upto;
+    __syncthreads();
+    int before = base;
+    for (int i = 0; i < 16; ++i) {
+      if (i < w) before += waves[i];
+      base += waves[i];
+    }
+    if (b < a.S) a.starts[b] = before + upto - n;
+  }
+  if (threadIdx.x == 0) a.starts[a.S] = base;
+}
+
+// The sequence whose parts, Hkv times each, hold `item` (the last whose parts begin at or before it), or -1 past the
+// last one: 64 entries at a time.
+__device__ __forceinline__ int seq_of_item(const Kv8AttnArgs& a, int item, int lane) {
+  const int part = item / a.Hkv;   // (streams of a sequence are cut alike: Hkv times as many items as parts)
+  int lo = 0, n = a.S + 1;         // entries [lo, lo + n); the answer is in them
+  if (part >= a.starts[a.S]) return -1;
+  while (n > 1) {
+    const int step = (n + kWave - 1) / kWave, i = lane * step;
+    const uint64_t below = __ballot(i < n && a.starts[lo + (i < n ? i : 0)] <= part);
+    const int k = 63 - __builtin_clzll(below);   // (entry 0 is 0: never empty at the first level, nor below it)
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  return lo;
 }
 
 // K and V bytes of a pair of pages: a lane's 16 dimensions of a token for K; for V four dimensions of the
@@ -110,29 +162,37 @@ __device__ __forceinline__ void kv8_pair(Kv8State<DH>& S, const Kv8Pair<DH>& R, 
 }
 
 // Split-K decode: one wavefront per part of a (sequence, kv-head) stream, its 16 columns the heads of the group.
-template <int DH>
+template <int DH, bool PLANNED>
 __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
   const int lane = threadIdx.x;
-  const int target = decode_target(a, lane);
   // this wavefront's sequence: parts come sequence by sequence, then head by head
   int item = blockIdx.x, b = -1, n_parts = 0;
-  for (int i0 = 0; i0 < a.S; i0 += kWave) {
-    const int mine = i0 + lane < a.S ? kv8_parts(pages_of(ctx_of(a, i0 + lane)), target) : 0;
-    const int upto = wave_scan(mine);
-    const int all = __builtin_amdgcn_readlane(upto, 63);
-    if (item < all * a.Hkv) {
-      const int at = __builtin_ctzll(__ballot(item < upto * a.Hkv));
-      n_parts = __builtin_amdgcn_readlane(mine, at);
-      item -= (__builtin_amdgcn_readlane(upto, at) - n_parts) * a.Hkv;
-      b = i0 + at;
-      break;
+  if (PLANNED) {
+    b = seq_of_item(a, item, lane);
+    if (b < 0) return;
+    const int first = a.starts[b];
+    n_parts = a.starts[b + 1] - first;
+    item -= first * a.Hkv;
+  } else {
+    const int target = decode_target(a, lane);
+    for (int i0 = 0; i0 < a.S; i0 += kWave) {
+      const int mine = i0 + lane < a.S ? kv8_parts(pages_of(ctx_of(a, i0 + lane)), target) : 0;
+      const int upto = wave_scan(mine);
+      const int all = __builtin_amdgcn_readlane(upto, 63);
+      if (item < all * a.Hkv) {
+        const int at = __builtin_ctzll(__ballot(item < upto * a.Hkv));
+        n_parts = __builtin_amdgcn_readlane(mine, at);
+        item -= (__builtin_amdgcn_readlane(upto, at) - n_parts) * a.Hkv;
+        b = i0 + at;
+        break;
+      }
+      item -= all * a.Hkv;
     }
-    item -= all * a.Hkv;
+    if (b < 0) return;
   }
-  if (b < 0) return;
   const int kvh = item / n_parts, part = item - kvh * n_parts;
   const int n = ctx_of(a, b), n_pages = pages_of(n);
-  const int len = kv8_part_pages(n_pages, target);
+  const int len = (n_pages + n_parts - 1) / n_parts;   // (what kv8_part_pages made the parts of)
   const int p0 = part * len, np = min(len, n_pages - p0);   // pages [p0, p0 + np)
   const int G = a.Hq / a.Hkv;
   const int col = lane & 15, rq = lane >> 4;
@@ -285,7 +345,7 @@ struct MergeState {
   }
 };
 
-template <int DH, int H>
+template <int DH, int H, bool PLANNED>
 __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a) {
   constexpr int C = DH / 4, R = 256 / C;   // threads across a row, streams of parts in a workgroup
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -298,13 +358,19 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a) {
     if (w < H && lane < C && h0 + w < a.Hq) *reinterpret_cast<uint2*>(out + (h0 + w) * DH) = make_uint2(0, 0);
     return;
   }
-  const int target = decode_target(a, lane);
-  const int n = kv8_parts(n_pages, target);
-  if (n == 1) return;
-  int before = 0;
-  for (int i0 = 0; i0 < b; i0 += kWave)
-    before += __builtin_amdgcn_readlane(
-        wave_scan(i0 + lane < b ? kv8_parts(pages_of(ctx_of(a, i0 + lane)), target) : 0), 63);
+  int n, before = 0;
+  if (PLANNED) {
+    before = a.starts[b];
+    n = a.starts[b + 1] - before;
+    if (n == 1) return;
+  } else {
+    const int target = decode_target(a, lane);
+    n = kv8_parts(n_pages, target);
+    if (n == 1) return;
+    for (int i0 = 0; i0 < b; i0 += kWave)
+      before += __builtin_amdgcn_readlane(
+          wave_scan(i0 + lane < b ? kv8_parts(pages_of(ctx_of(a, i0 + lane)), target) : 0), 63);
+  }
   const int G = a.Hq / a.Hkv;
   const float2* ml = reinterpret_cast<const float2*>(a.ws + a.ws_ml);
   const float* o = reinterpret_cast<const float*>(a.ws) + c * 4;
@@ -926,28 +992,38 @@ __global__ __launch_bounds__(256) void kv8_prefill_merge_kernel(Kv8PrefillArgs p
 
 }  // namespace
 
-// Partial outputs [items][G][dh], then their (maximum, sum) pairs
+// Partial outputs [items][G][dh], then their (maximum, sum) pairs, then the starts of the sequences
 static int64_t decode_ml_offset(int B, int Hq, int Hkv, int dh) { return kv8_decode_items(B, Hkv) * (Hq / Hkv) * dh * 4; }
-int64_t kv8_decode_ws_bytes(int B, int Hq, int Hkv, int dh) {
+static int64_t decode_starts_offset(int B, int Hq, int Hkv, int dh) {
   return decode_ml_offset(B, Hq, Hkv, dh) + kv8_decode_items(B, Hkv) * (Hq / Hkv) * 8;
 }
+int64_t kv8_decode_ws_bytes(int B, int Hq, int Hkv, int dh) {
+  return decode_starts_offset(B, Hq, Hkv, dh) + ((int64_t)B + 1) * 4;
+}
 int64_t kv8_prefill_ws_bytes(int S, int T, int Hq, int Hkv, int dh) { return prefill_ws(S, T, Hq, Hkv, dh).total; }
+
+template <int DH, bool PLANNED>
+static hipError_t decode_launch(const Kv8AttnArgs& a, hipStream_t st) {
+  if (PLANNED) {
+    hipLaunchKernelGGL(kv8_decode_plan_kernel, dim3(1), dim3(1024), 0, st, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((kv8_decode_kernel<DH, PLANNED>), dim3((unsigned)kv8_decode_items(a.S, a.Hkv)), dim3(64), 0, st, a);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  const int64_t quads = (int64_t)a.S * ((a.Hq + 3) / 4);
+  if (quads < kCus && a.bt_stride > kMergeAlone * kKv8MinPages)
+    hipLaunchKernelGGL((kv8_merge_kernel<DH, 1, PLANNED>), dim3((unsigned)(a.S * a.Hq)), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((kv8_merge_kernel<DH, 4, PLANNED>), dim3((unsigned)quads), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
 
 hipError_t kv8_decode_launch(const Kv8AttnArgs& args, hipStream_t st) {
   Kv8AttnArgs a = args;
   a.ws_ml = decode_ml_offset(a.S, a.Hq, a.Hkv, a.dh);
-  const dim3 grid((unsigned)kv8_decode_items(a.S, a.Hkv));
-  if (a.dh == 128) hipLaunchKernelGGL(kv8_decode_kernel<128>, grid, dim3(64), 0, st, a);
-  else hipLaunchKernelGGL(kv8_decode_kernel<64>, grid, dim3(64), 0, st, a);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  const int64_t quads = (int64_t)a.S * ((a.Hq + 3) / 4);
-  auto merge = [&](auto kernel, int64_t groups) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, st, a);
-    return hipGetLastError();
-  };
-  if (quads < kCus && a.bt_stride > kMergeAlone * kKv8MinPages)
-    return a.dh == 128 ? merge(kv8_merge_kernel<128, 1>, (int64_t)a.S * a.Hq) : merge(kv8_merge_kernel<64, 1>, (int64_t)a.S * a.Hq);
-  return a.dh == 128 ? merge(kv8_merge_kernel<128, 4>, quads) : merge(kv8_merge_kernel<64, 4>, quads);
+  a.starts = reinterpret_cast<int32_t*>(a.ws + decode_starts_offset(a.S, a.Hq, a.Hkv, a.dh));
+  if (a.S > kKv8DecodeScan) return a.dh == 128 ? decode_launch<128, true>(a, st) : decode_launch<64, true>(a, st);
+  return a.dh == 128 ? decode_launch<128, false>(a, st) : decode_launch<64, false>(a, st);
 }
 
 hipError_t kv8_prefill_launch(const Kv8AttnArgs& a, hipStream_t st) {
