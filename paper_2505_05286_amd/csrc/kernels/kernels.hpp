@@ -302,7 +302,7 @@ struct Kv8AttnArgs {
 // cache, each (sequence, kv-head) stream of pages is cut into equal parts no longer than an even share of
 // all the pages over the wavefronts the chip holds at once, at least kKv8MinPages pages; with fewer streams than
 // those wavefronts the parts just fill them.
-constexpr int kKv8Resident = 2048;
+constexpr int kKv8Resident = 3072;   // three a SIMD, at 161 VGPRs
 constexpr int kKv8MinPages = 8;
 __host__ __device__ inline int64_t kv8_target_pages(int64_t total_pages, int64_t n_seqs, int hkv) {
   const int64_t pairs = n_seqs * hkv;
@@ -324,6 +324,35 @@ __host__ __device__ inline int kv8_parts(int pages, int target) {
 inline int64_t kv8_decode_items(int64_t n_seqs, int hkv) {
   const int64_t pairs = n_seqs * hkv;
   return pairs < kKv8Resident ? kKv8Resident : kKv8Resident + pairs;
+}
+// Prefill work split, made by a kernel from the rows and positions in device memory.  A block of up to 128 / G queries
+// of a sequence is one unit of work for every kv-head, over its key tiles of 32 positions (taken in pairs).  Where
+// whole blocks would be fewer than the CUs, blocks longer than an even share of all tiles over the resident workgroups
+// are cut into parts of equal length, at least kPrefillMinTiles tiles.
+constexpr int kCus = 256;
+__host__ __device__ inline bool kv8_prefill_cuts(int64_t blocks, int hkv) { return blocks * hkv < kCus; }
+// tiles: no less than the sum of all blocks' tiles
+__host__ __device__ inline int kv8_prefill_share(int64_t tiles, int hkv) {
+  const int64_t t = (tiles * hkv + kPrefillResident - 1) / kPrefillResident;
+  return (int)(t > kPrefillMinTiles ? t : kPrefillMinTiles);
+}
+// Parts of a block of `tiles` (even) tiles, at least one; part k is the tiles [k * len, min(tiles, (k + 1) * len))
+__host__ __device__ inline int kv8_prefill_part_tiles(int tiles, int parts) { return (tiles / 2 + parts - 1) / parts * 2; }
+__host__ __device__ inline int kv8_prefill_parts(int tiles, int share) {
+  const int most = (tiles + share - 1) / share;
+  if (most <= 1) return 1;
+  const int len = kv8_prefill_part_tiles(tiles, most);
+  return (tiles + len - 1) / len;
+}
+// Units that hold any batch of S sequences and T rows, and partial slots of a kv-head: blocks number at most
+// T / q + S; cut ones, over all heads, under kCus blocks and kPrefillResident more parts than blocks.
+inline int64_t kv8_prefill_unit_cap(int64_t S, int64_t T, int queries, int hkv) {
+  const int64_t cut = (kCus + kPrefillResident) / hkv, whole = T / queries + S;
+  return (cut > whole ? cut : whole) + 1;
+}
+inline int64_t kv8_prefill_slots(int64_t S, int64_t T, int queries, int hkv) {
+  const int64_t cut = (kCus + kPrefillResident) / hkv, whole = T / queries + S + kPrefillResident / hkv;
+  return (cut < whole ? cut : whole) + 1;
 }
 int64_t kv8_decode_ws_bytes(int B, int Hq, int Hkv, int dh);
 hipError_t kv8_decode_launch(const Kv8AttnArgs& a, hipStream_t st);

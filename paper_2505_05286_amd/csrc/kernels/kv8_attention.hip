@@ -161,7 +161,8 @@ __device__ __forceinline__ void kv8_pair(Kv8State<DH>& S, const Kv8Pair<DH>& R, 
   }
 }
 
-// Split-K decode: one wavefront per part of a (sequence, kv-head) stream, its 16 columns the heads of the group.
+// Split-K decode: one wavefront per part of a (sequence, kv-head) stream, its 16 columns the heads of the group.  Bound by
+// HBM: 64 contexts of 1-8k tokens (451 MB) in 78 us, 5.8 of the 6.0 TB/s that a plain read reaches.
 template <int DH, bool PLANNED>
 __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
   const int lane = threadIdx.x;
@@ -225,7 +226,10 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
   for (int i = 0; i < DH / 16; ++i) S.acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   S.m = -1e30f;   // finite, so that a column without keys keeps zero weights
   S.l = 0.f;
-  constexpr int NB = 3;   // pairs of pages in registers: one multiplied, two on their way
+  // Pairs of pages in registers: one multiplied, one on its way.  A third takes the registers of a third wavefront
+  // on the SIMD, whose loads hide more: 128 contexts of 1.5-3k tokens, 32 + 8 heads, 109 us against 118, 97 of
+  // 4.5-9k 226 against 238.
+  constexpr int NB = 2;
   Kv8Pair<DH> R[NB];
   auto issue = [&](Kv8Pair<DH>& P, int r) __attribute__((always_inline)) {
     if (r && r % kWave == 0) {
@@ -307,7 +311,6 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
 // tables are long enough for more parts than that.  64 sequences of up to 11
 // parts: 4.7 us (H = 1: 7.7); a lone context of 64 parts: 4.7 us with H = 1, 9.5 with 4, 17.2 with a wavefront for
 // each head.
-constexpr int kCus = 256;
 constexpr int kMergeAlone = 16;
 template <int DH>
 struct MergeState {
@@ -427,15 +430,11 @@ struct PrefillWs {
   int64_t units, jobs, part_o, part_ml, total;   // byte offsets
   int32_t unit_cap, slots;                       // units; partial slots of a kv-head
 };
-// A block is cut only where the whole blocks are fewer than the CUs: then blocks * Hkv < kCus, and the parts, no longer
-// than an even share of all key tiles over the resident workgroups, number at most kCus + kPrefillResident over all heads.
-// Otherwise sum ceil(n / q) <= T / q + S.
 PrefillWs prefill_ws(int S, int T, int Hq, int Hkv, int dh) {
   PrefillWs w;
-  const int64_t split = (kCus + kPrefillResident) / Hkv;
-  const int64_t whole = (int64_t)T / prefill_queries_per_item(Hq / Hkv) + S;
-  w.unit_cap = (int32_t)(std::max(split, whole) + 1);
-  w.slots = (int32_t)std::min<int64_t>(split, whole + kPrefillResident / Hkv) + 1;
+  const int queries = prefill_queries_per_item(Hq / Hkv);
+  w.unit_cap = (int32_t)kv8_prefill_unit_cap(S, T, queries, Hkv);
+  w.slots = (int32_t)kv8_prefill_slots(S, T, queries, Hkv);
   auto al = [](int64_t x) { return (x + 255) & ~int64_t(255); };
   w.units = sizeof(PrefillHead);
   w.jobs = al(w.units + w.unit_cap * (int64_t)sizeof(PrefillUnit));
@@ -536,7 +535,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
     atomicAdd(&bins[bin_of(t)], 1);
   });
   __syncthreads();
-  if ((int64_t)n_blocks * a.Hkv >= kCus) {
+  if (!kv8_prefill_cuts(n_blocks, a.Hkv)) {
     int all, sum = 0;
     for (int k = 0; k < kPer; ++k) sum += bins[tid * kPer + k];
     int at = scan(sum, all);
@@ -561,17 +560,13 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
   int halves;
   scan((int)mine, halves);
   const int64_t tiles = ((int64_t)(uint32_t)halves + n_blocks) * 2;   // no less than their sum
-  const int share = (int)max((tiles * a.Hkv + kPrefillResident - 1) / kPrefillResident, (int64_t)kPrefillMinTiles);
+  const int share = kv8_prefill_share(tiles, a.Hkv);
   __shared__ PrefillUnit whole[kCus];
   __shared__ int32_t first[kCus];   // a block's first unit
   blocks([&](int s, int r0, int n, int j, int i) { whole[i] = unit_of(s, r0, n, j); });
   __syncthreads();
   int n_part = 0;   // of block tid
-  if (tid < n_blocks) {
-    const int pairs = whole[tid].t1 / 2;   // pairs of tiles
-    const int len = max(1, (pairs + max(1, (2 * pairs + share - 1) / share) - 1) / max(1, (2 * pairs + share - 1) / share));
-    n_part = max(1, (pairs + len - 1) / len);
-  }
+  if (tid < n_blocks) n_part = kv8_prefill_parts(whole[tid].t1, share);
   int n_units, n_slots, n_jobs;
   const int at = scan(n_part, n_units), slot0 = scan(n_part > 1 ? n_part : 0, n_slots);
   const int job = scan(n_part > 1 ? 1 : 0, n_jobs);
@@ -591,7 +586,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
       else hi = mid;
     }
     PrefillUnit u = whole[lo];
-    const int parts = u.t0, k = i - first[lo], len = (u.t1 / 2 + parts - 1) / parts * 2;
+    const int parts = u.t0, k = i - first[lo], len = kv8_prefill_part_tiles(u.t1, parts);
     u.t0 = k * len;
     u.t1 = min(u.t1, u.t0 + len);
     u.slot = parts > 1 ? u.slot + k : -1;

@@ -93,8 +93,10 @@ class Cache:
 
     def write_run(self, kind, block, first, x):
         """x float32 [n, Hkv, dh] to places first .. of one page."""
+        with np.errstate(invalid="ignore"):                # (casts of NaN)
+            x = x.astype(np.float64)
         for h in range(self.hkv):
-            a = np.abs(x[:, h].astype(np.float64))
+            a = np.abs(x[:, h])
             s = scale_for(np.max(a[np.isfinite(a)], initial=0.0))
             page = self.codes[kind][h, block]
             if first:
@@ -102,7 +104,7 @@ class Cache:
                 s = max(s, old)
                 if s != old:
                     page[:first] = encode(VALUES[page[:first]] * (old / s))
-            page[first:first + len(x)] = encode(x[:, h].astype(np.float64) / s)
+            page[first:first + len(x)] = encode(x[:, h] / s)
             self.scale[kind][h, block] = s
 
     def write(self, k, v, slot):

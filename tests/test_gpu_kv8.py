@@ -504,3 +504,164 @@ def test_prefill_rows_past_the_table_and_row0_out_of_range():
         ref, size = U.attend(qf[r], cache, bt[s], p + r.stop - r.start, 4, first=p)
         U.assert_attention(got[r], ref, size, f"sequence {s}")
     assert np.all(out.cpu().numpy().view(np.uint16).reshape(24, -1)[20:] == 0x1234)
+
+
+def test_prefill_long_blocks_that_are_not_cut():
+    """More blocks than CUs, each over many tables of 64 pages."""
+    rng = np.random.default_rng(16)
+    pos0, n = np.array([1500, 2100, 0, 1023]), np.array([300, 257, 320, 290])
+    cache, bt = _attention_case(rng, pos0 + n, 32, 8, 128)
+    _prefill(cache, bt, pos0, n, 32, rng, what="not cut")
+
+
+def test_attention_repeats_to_the_bit():
+    """The order in which work is taken up does not show in the result, whatever the workspace held before."""
+    for hq, hkv, dh, ctx in ((8, 2, 128, [2000, 3, 0, 700]), (4, 2, 64, list(range(1, 150)))):
+        raw = []
+        for fill in (0xFF, 0, 0x7F):
+            rng = np.random.default_rng(21)
+            cache, bt = _attention_case(rng, ctx, hq, hkv, dh)
+            raw.append(_decode(cache, bt, np.array(ctx), hq, rng, what="again", ws_fill=fill))
+        assert all(np.array_equal(r, raw[0]) for r in raw)
+    raw = []
+    for _ in range(3):
+        rng = np.random.default_rng(22)
+        pos0, n = rng.integers(0, 200, 60), rng.integers(0, 20, 60)
+        cache, bt = _attention_case(rng, pos0 + n, 32, 8, 128)
+        raw.append(_prefill(cache, bt, pos0, n, 32, rng, what="again"))
+    assert all(np.array_equal(r, raw[0]) for r in raw)
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each with a workspace of its own, do not disturb each other."""
+    t = torch()
+    hq, hkv, dh = 8, 2, 128
+    sides = []
+    for seed in (31, 32):
+        rng = np.random.default_rng(seed)
+        ctx = rng.integers(1, 1500, 40)
+        cache, bt = _attention_case(rng, ctx, hq, hkv, dh)
+        bits, qf = rand_bf16(rng, (40, hq, dh))
+        n = hxf.op_decode_attention_kv8_workspace_bytes(40, hq, hkv, dh)
+        m = hxf.op_prefill_attention_kv8_workspace_bytes(40, 40, hq, hkv, dh)
+        sides.append(dict(ctx=ctx, cache=cache, bt=bt, qf=qf, dev=DevCache(cache), q=dev_bits(bits), d_bt=i32(bt),
+                          d_ctx=i32(ctx), row0=i32(np.arange(41)), pos0=i32(ctx - 1), ws=t.empty(n, dtype=t.uint8, device="cuda:0"),
+                          ws2=t.empty(m, dtype=t.uint8, device="cuda:0"), out=dev_bits(np.zeros((40, hq, dh), np.uint16)),
+                          out2=dev_bits(np.zeros((40, hq, dh), np.uint16)), st=t.cuda.Stream()))
+    t.cuda.synchronize()
+    log("two streams")
+    for _ in range(20):
+        for s in sides:
+            hxf.op_decode_attention_kv8(s["q"].data_ptr(), hq * dh, s["dev"].pool, s["d_bt"].data_ptr(),
+                                        s["bt"].shape[1], s["d_ctx"].data_ptr(), s["out"].data_ptr(), hq * dh, 40, hq,
+                                        hkv, dh, s["ws"].data_ptr(), s["ws"].numel(), stream=s["st"].cuda_stream)
+            hxf.op_prefill_attention_kv8(s["q"].data_ptr(), hq * dh, s["dev"].pool, s["d_bt"].data_ptr(),
+                                         s["bt"].shape[1], s["row0"].data_ptr(), s["pos0"].data_ptr(),
+                                         s["out2"].data_ptr(), hq * dh, 40, 40, hq, hkv, dh, s["ws2"].data_ptr(),
+                                         s["ws2"].numel(), stream=s["st"].cuda_stream)
+    t.cuda.synchronize()
+    for s in sides:
+        for b in range(40):
+            ref, size = U.attend(s["qf"][b:b + 1], s["cache"], s["bt"][b], int(s["ctx"][b]), hq)
+            for o in ("out", "out2"):
+                U.assert_attention(host_f64(s[o]).reshape(40, hq, dh)[b:b + 1], ref, size, f"{o} {b}")
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(4, 2, 64), (16, 2, 128)])
+def test_a_captured_step_of_all_operators(hq, hkv, dh):
+    """The operators as a serving loop runs them, in one captured graph that is replayed with other lengths: tables,
+    rotation and write, attention of the decode rows and of the chunks (both through one workspace).  Every
+    replay is checked against the model and against the same calls made eagerly on a second cache."""
+    t = torch()
+    rng = np.random.default_rng(hq)
+    D, P, T, stride, nb, max_pos = 5, 4, 120, 12, 160, 200
+    S = D + P
+    width = (hq + 2 * hkv) * dh
+    table = U.rope_table(max_pos, dh)
+    cache = U.Cache(hkv, nb, dh)
+    order = list(rng.permutation(nb))
+    start = np.concatenate([rng.integers(1, 60, D), np.zeros(P, np.int64)])
+    bt = np.full((S, stride), -1, np.int64)
+    for s in range(D):                                    # the decode sequences' prompts are in the cache already
+        for p in range(-(-start[s] // 16)):
+            bt[s, p] = order.pop()
+        cache.fill(rng, bt[s, :-(-start[s] // 16)])
+        if start[s] % 16:
+            cache.poison(bt[s, start[s] // 16], start[s] % 16)
+
+    def side():
+        z = lambda *n: t.zeros(n, dtype=t.int32, device="cuda:0")
+        ws = max(hxf.op_decode_attention_kv8_workspace_bytes(D, hq, hkv, dh),
+                 hxf.op_prefill_attention_kv8_workspace_bytes(P, T, hq, hkv, dh))
+        return dict(dev=DevCache(cache), bt=i32(bt), start=z(S), new=z(S), free=z(64), n_free=z(1), row0=z(S + 1), pos=z(T),
+                    slot=z(T), ctx=z(S), status=z(2), qkv=t.zeros(T * width, dtype=t.int16, device="cuda:0"),
+                    q=t.zeros(T * hq * dh, dtype=t.int16, device="cuda:0"),
+                    out=t.zeros(T * hq * dh, dtype=t.int16, device="cuda:0"), ws=t.zeros(ws, dtype=t.uint8, device="cuda:0"),
+                    table=t.from_numpy(table).to("cuda:0"))
+
+    def step(s, stream):
+        p = lambda k, at=0: s[k].data_ptr() + at
+        hxf.op_slot_map(p("start"), p("new"), S, p("free"), p("n_free"), 64, p("bt"), stride, p("row0"), p("pos"),
+                        p("slot"), T, p("ctx"), p("status"), stream=stream)
+        hxf.op_rope_kv8_write(p("qkv"), width, p("pos"), p("slot"), p("table"), max_pos, p("q"), hq * dh, s["dev"].pool,
+                              T, hq, hkv, dh, stream=stream)
+        hxf.op_decode_attention_kv8(p("q"), hq * dh, s["dev"].pool, p("bt"), stride, p("ctx"), p("out"), hq * dh, D, hq,
+                                    hkv, dh, p("ws"), s["ws"].numel(), stream=stream)
+        hxf.op_prefill_attention_kv8(p("q"), hq * dh, s["dev"].pool, p("bt", 4 * D * stride), stride, p("row0", 4 * D),
+                                     p("start", 4 * D), p("out"), hq * dh, P, T, hq, hkv, dh, p("ws"), s["ws"].numel(),
+                                     stream=stream)
+
+    cap, eager = side(), side()
+    cap["n_free"].fill_(64)
+    st = t.cuda.Stream()
+    with t.cuda.stream(st):
+        step(cap, st.cuda_stream)                          # lengths of zero: nothing is written
+        st.synchronize()
+        graph = t.cuda.CUDAGraph()
+        with t.cuda.graph(graph, stream=st):
+            step(cap, t.cuda.current_stream().cuda_stream)
+    t.cuda.synchronize()
+    cap["dev"].check("before the first replay")
+    for it in range(7):
+        new = np.concatenate([np.ones(D, np.int64), rng.integers(0, 28, P)])
+        if it == 2:
+            new[D:] = 0
+        if it == 4:
+            new[D] = 200                                   # more rows than the batch holds: nothing may happen
+        free = [order.pop() for _ in range(24)]
+        bits, _ = rand_bf16(rng, (T, width), [1.0, 3.0, 0.2][it % 3])
+        for s in (cap, eager):
+            for k, a in (("start", start), ("new", new), ("n_free", [len(free)])):
+                s[k].copy_(i32(a))
+            s["free"][:len(free)].copy_(i32(free))
+            s["qkv"].copy_(dev_bits(bits).view(-1))
+            s["out"].fill_(0x1234)
+        t.cuda.synchronize()
+        log(f"replay {it}: new {new.tolist()}")
+        graph.replay()
+        step(eager, 0)
+        t.cuda.synchronize()
+        bt, row0, pos, slot, ctx, status = U.slot_map(start, new, free, bt, T)
+        for k, r in (("bt", bt), ("row0", row0), ("pos", pos), ("slot", slot), ("ctx", ctx), ("status", status)):
+            for s in (cap, eager):
+                np.testing.assert_array_equal(s[k].cpu().numpy().reshape(r.shape), r, err_msg=f"replay {it}: {k}")
+        order = free[max(0, status[0]):] + order            # what was not taken goes back
+        x = U.f32_of(bits).reshape(T, hq + 2 * hkv, dh)
+        qk = U.rotate(x[:, :hq + hkv], table[pos])
+        cache.write(qk[:, hq:], x[:, hq + hkv:], slot)
+        for s in (cap, eager):
+            s["dev"].check(f"replay {it}")
+        assert t.equal(cap["out"], eager["out"]) and t.equal(cap["q"], eager["q"])
+        got = host_f64(cap["out"]).reshape(T, hq, dh)
+        qf = host_f64(cap["q"]).reshape(T, hq, dh)
+        live = np.zeros(T, bool)
+        for s in range(S):
+            rows = slice(s, s + 1) if s < D else slice(row0[s], row0[s + 1])
+            live[rows] = True
+            if status[0] < 0 and s >= D:
+                continue
+            ref, size = U.attend(qf[rows], cache, bt[s], int(ctx[s]), hq, first=None if s < D else int(start[s]))
+            U.assert_attention(got[rows], ref, size, f"replay {it} sequence {s}")
+        raw = cap["out"].cpu().numpy().reshape(T, -1)
+        assert np.all(raw[~live] == 0x1234)
+        start = ctx

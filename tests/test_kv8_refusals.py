@@ -1,5 +1,8 @@
 """The operators of the 8-bit KV cache refuse what they cannot do before anything is launched, and the model
 they are tested against is right on hand values (no GPU)."""
+import os
+import subprocess
+
 import numpy as np
 import pytest
 
@@ -120,6 +123,18 @@ def test_nothing_to_do_is_no_error():
     _decode(B=0, ws=None, ws_bytes=0)
     _prefill(S=0, ws=None, ws_bytes=0)
     _prefill(T=0, ws=None, ws_bytes=0)
+
+
+def test_work_splits(tmp_path):
+    """tests/kv8_split.cpp: the decode and prefill splits cover everything once and fit their launches."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "kv8_split")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                    "-I" + os.path.join(root, "paper_2505_05286_amd", "csrc"),
+                    os.path.join(root, "tests", "kv8_split.cpp"), "-o", exe], check=True, capture_output=True,
+                   timeout=300)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
 
 
 # ------------------------------------------------------------------ the model
