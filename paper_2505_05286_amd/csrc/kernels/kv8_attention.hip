@@ -164,8 +164,7 @@ __device__ __forceinline__ void kv8_pair(Kv8State<DH>& S, const Kv8Pair<DH>& R, 
 // Split-K decode: one wavefront per part of a (sequence, kv-head) stream, its 16 columns the heads of the group.  Bound by
 // HBM: 64 contexts of 1-8k tokens (451 MB) in 78 us, 5.8 of the 6.0 TB/s that a plain read reaches.
 template <int DH, bool PLANNED>
-__global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
-  const int lane = threadIdx.x;
+__device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
   // this wavefront's sequence: parts come sequence by sequence, then head by head
   int item = blockIdx.x, b = -1, n_parts = 0;
   if (PLANNED) {
@@ -304,7 +303,18 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
   if (rq == 0) reinterpret_cast<float2*>(a.ws + a.ws_ml)[slot] = make_float2(S.m, S.l);
 }
 
-// Joins the parts of a sequence's heads, H (4 or 1) heads a workgroup; zeros for an empty context.  A thread owns
+template <int DH, bool PLANNED>
+__global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
+  const int lane = threadIdx.x, b = blockIdx.x;
+  const int n = b < a.S ? a.ctx[b] : 1;   // (looked at when the work is done)
+  decode_part<DH, PLANNED>(a, lane);
+  if (n > 0) return;
+  // sequence b is empty: zeros
+  uint16_t* out = a.out + b * a.out_stride;
+  for (int i = lane * 8; i < a.Hq * DH; i += 64 * 8) *reinterpret_cast<uint4*>(out + i) = make_uint4(0, 0, 0, 0);
+}
+
+// Joins the parts of a sequence's heads, H (4 or 1) heads a workgroup.  A thread owns
 // four dimensions and every R-th part, four of them in flight, with a running maximum.  With four heads and up to
 // kMergeAlone parts each wavefront joins a head of its own; otherwise the workgroup takes its heads in turn and its
 // streams meet in LDS.  H is 1 where four heads a workgroup would leave CUs without one and the
@@ -357,10 +367,7 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a) {
   const int c = threadIdx.x % C;
   uint16_t* out = a.out + b * a.out_stride + c * 4;
   const int n_pages = pages_of(ctx_of(a, b));
-  if (n_pages == 0) {
-    if (w < H && lane < C && h0 + w < a.Hq) *reinterpret_cast<uint2*>(out + (h0 + w) * DH) = make_uint2(0, 0);
-    return;
-  }
+  if (n_pages == 0) return;
   int n, before = 0;
   if (PLANNED) {
     before = a.starts[b];
@@ -455,146 +462,217 @@ struct Kv8PrefillArgs {
   int unit_cap, slots, qpi;
 };
 
-// The units of a batch from row0 and pos0 in device memory, longest first; one workgroup, of four wavefronts because
-// most of its time is barriers (@PLAN@ us for 16 chunks; with 16 wavefronts 4.8).
+// What the planning kernels share.  kPlanThreads threads, a thread for each block of a batch that is cut.
 constexpr int kPlanThreads = 256;
 static_assert(kPlanThreads >= kCus, "a thread for each block of a batch that is cut");
-__global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8PrefillArgs p) {
-  constexpr int kBins = 1024, kWaves = kPlanThreads / kWave, kPer = kBins / kPlanThreads;
-  __shared__ int32_t pre[kPlanThreads], wave_sums[kWaves], bins[kBins];
-  const Kv8AttnArgs& a = p.a;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+
+struct PlanLds {
+  int32_t sums[kPlanThreads / kWave], pre[kPlanThreads];
+};
+
+// Exclusive sum over the workgroup
+__device__ __forceinline__ int plan_scan(PlanLds& lds, int v, int& total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int x = wave_scan(v);
+  __syncthreads();
+  if (lane == 63) lds.sums[w] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanThreads / kWave; ++i) {
+    if (i < w) before += lds.sums[i];
+    all += lds.sums[i];
+  }
+  total = all;
+  return before + x - v;
+}
+// The last of the entries begin[0 .. n), ascending from begin[0] <= i, that is at or before i
+__device__ __forceinline__ int last_at(const int32_t* begin, int n, int i) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (begin[mid] <= i) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+__device__ __forceinline__ int plan_rows(const Kv8AttnArgs& a, int s, int& r0) {
+  r0 = min(max(a.row0[s], 0), a.T);
+  return max(min(a.row0[s + 1], a.T) - r0, 0);
+}
+// Block j of a sequence whose rows are r0 .. r0 + n - 1, whole
+__device__ __forceinline__ PrefillUnit plan_block(const Kv8AttnArgs& a, int queries, int s, int r0, int n, int j) {
   const int kcap = a.bt_stride * kPage;
-  auto scan = [&](int v, int& total) {   // exclusive, over the workgroup
-    const int x = wave_scan(v);
+  PrefillUnit u;
+  u.seq = s;
+  u.row = r0 + j * queries;
+  u.nq = min(queries, n - j * queries);
+  u.pos = min(max(a.pos0[s], -(1 << 30)), kcap) + j * queries;
+  u.t0 = 0;
+  u.t1 = (max(min(u.pos + u.nq, kcap), 0) + 63) / 64 * 2;
+  u.slot = -1;
+  u.pad = 0;
+  return u;
+}
+// The cut of a batch of few blocks, whose block threadIdx.x has these tiles (0 for a thread without one)
+struct PlanCut {
+  int parts, first, slot0, job;        // of this thread's block: its parts, its first unit, slot and job
+  int n_units, n_jobs;
+};
+__device__ __forceinline__ PlanCut plan_cut(PlanLds& lds, const Kv8AttnArgs& a, int n_blocks, int tiles) {
+  int halves, all;   // (half the tiles: under 256 blocks of up to 2^25 tiles stay in 32 bits)
+  plan_scan(lds, tiles >> 1, halves);
+  const int share = kv8_prefill_share(((int64_t)(uint32_t)halves + n_blocks) * 2, a.Hkv);   // no less than their sum
+  PlanCut c;
+  c.parts = (int)threadIdx.x < n_blocks ? kv8_prefill_parts(tiles, share) : 0;
+  // units, slots and jobs number under 2^10 each: one scan
+  const int cut = c.parts > 1;
+  const int at = plan_scan(lds, c.parts | (cut ? c.parts : 0) << 10 | cut << 20, all);
+  c.first = at & 1023;
+  c.slot0 = at >> 10 & 1023;
+  c.job = at >> 20;
+  c.n_units = all & 1023;
+  c.n_jobs = all >> 20;
+  return c;
+}
+// Part k of a cut block
+__device__ __forceinline__ void plan_part(PrefillUnit& u, int parts, int slot0, int k) {
+  const int len = kv8_prefill_part_tiles(u.t1, parts);
+  u.t0 = k * len;
+  u.t1 = min(u.t1, u.t0 + len);
+  u.slot = parts > 1 ? slot0 + k : -1;
+}
+
+// A batch of up to kPlanThreads sequences and blocks is planned by every workgroup of the kernels that follow for
+// itself, in the time that a list made by a launch of its own would take to read: this makes unit `want` (in
+// `unit`) or all jobs (in `jobs`), and returns their number.  Units come longest first; and among the first resident
+// workgroups the second half in reverse, so that a CU gets a long one and a short one.
+template <bool JOBS>
+struct SmallPlan {
+  PlanLds scan;
+  int32_t tiles[JOBS ? 1 : kPlanThreads];
+  PrefillUnit unit;
+  PrefillJob jobs[JOBS ? kCus : 1];
+};
+template <bool JOBS>
+__device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8AttnArgs& a, int queries, int want) {
+  const int tid = threadIdx.x;
+  int r0 = 0, total;
+  const int rows = tid < a.S ? plan_rows(a, tid, r0) : 0;
+  const int before = plan_scan(lds.scan, (rows + queries - 1) / queries, total);
+  lds.scan.pre[tid] = before;
+  __syncthreads();
+  const int n = min(total, kPlanThreads);   // (more only where row0 does not ascend)
+  PrefillUnit u;
+  u.t1 = 0;
+  if (tid < n) {
+    const int s = last_at(lds.scan.pre, a.S, tid);
+    const int m = plan_rows(a, s, r0);
+    u = plan_block(a, queries, s, r0, m, tid - lds.scan.pre[s]);
+  }
+  if (!kv8_prefill_cuts(n, a.Hkv)) {
+    if constexpr (JOBS) return 0;
+    const int half = kPrefillResident / 2 / a.Hkv, window = min(n, kPrefillResident / a.Hkv);
+    if (want >= half && want < window) want = half + window - 1 - want;
+    lds.tiles[tid] = u.t1;
     __syncthreads();
-    if (lane == 63) wave_sums[w] = x;
-    __syncthreads();
-    int before = 0, all = 0;
-    for (int i = 0; i < kWaves; ++i) {
-      if (i < w) before += wave_sums[i];
-      all += wave_sums[i];
+    int rank = 0;   // blocks that come before this one
+    for (int i = 0; i < n; ++i) {
+      const int t = lds.tiles[i];
+      rank += t > u.t1 || (t == u.t1 && i < tid);
     }
-    total = all;
-    return before + x - v;
-  };
-  auto rows_of = [&](int s, int& r0) {
-    r0 = min(max(a.row0[s], 0), a.T);
-    return max(min(a.row0[s + 1], a.T) - r0, 0);
-  };
-  // f(s, row0 of s, its rows, block j of s, number of the block) for every block; the number of blocks
-  int total = 0;
-  bool scanned = false;   // pre and total are those of the only kPlanThreads sequences
+    if (tid < n && rank == want) lds.unit = u;
+    __syncthreads();
+    return n;
+  }
+  const PlanCut c = plan_cut(lds.scan, a, n, u.t1);
+  if (JOBS) {
+    if (c.parts > 1) lds.jobs[JOBS ? c.job : 0] = PrefillJob{u.row, u.nq, c.slot0, c.parts};
+  } else if (want >= c.first && want < c.first + c.parts) {
+    plan_part(u, c.parts, c.slot0, want - c.first);
+    lds.unit = u;
+  }
+  __syncthreads();
+  return JOBS ? c.n_jobs : c.n_units;
+}
+
+// The units of a larger batch, in the order above, and the jobs; one workgroup, of four wavefronts because most of its
+// time is barriers (with 16 wavefronts 4.9 us for one cut chunk against 4.0).
+__global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8PrefillArgs p) {
+  constexpr int kBins = 1024, kPer = kBins / kPlanThreads;
+  __shared__ PlanLds lds;
+  __shared__ int32_t bins[kBins];
+  const Kv8AttnArgs& a = p.a;
+  const int tid = threadIdx.x;
+  // f(whole block, its number) for every block; the number of blocks
   auto blocks = [&](auto&& f) {
     int base = 0;
     for (int s0 = 0; s0 < a.S; s0 += kPlanThreads) {
-      if (!scanned) {
-        int r0;
-        const int n = s0 + tid < a.S ? rows_of(s0 + tid, r0) : 0;
-        const int before = scan((n + p.qpi - 1) / p.qpi, total);
-        pre[tid] = before;
-        scanned = a.S <= kPlanThreads;
-        __syncthreads();
-      }
+      int r0, total;
+      const int n = s0 + tid < a.S ? plan_rows(a, s0 + tid, r0) : 0;
+      const int before = plan_scan(lds, (n + p.qpi - 1) / p.qpi, total);
+      lds.pre[tid] = before;
+      __syncthreads();
       for (int i = tid; i < total; i += kPlanThreads) {
-        int lo = 0, hi = min(kPlanThreads, a.S - s0);   // the last sequence whose blocks begin at or before i (empty ones before it)
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (pre[mid] <= i) lo = mid;
-          else hi = mid;
-        }
-        int r;
-        const int m = rows_of(s0 + lo, r);
-        f(s0 + lo, r, m, i - pre[lo], base + i);
+        const int s = last_at(lds.pre, min(kPlanThreads, a.S - s0), i);
+        const int m = plan_rows(a, s0 + s, r0);
+        f(plan_block(a, p.qpi, s0 + s, r0, m, i - lds.pre[s]), base + i);
       }
       base += total;
     }
     return base;
   };
-  auto unit_of = [&](int s, int r0, int n, int j) {
-    PrefillUnit u;
-    u.seq = s;
-    u.row = r0 + j * p.qpi;
-    u.nq = min(p.qpi, n - j * p.qpi);
-    u.pos = min(max(a.pos0[s], -(1 << 30)), kcap) + j * p.qpi;
-    u.t0 = 0;
-    u.t1 = (max(min(u.pos + u.nq, kcap), 0) + 63) / 64 * 2;
-    u.slot = -1;
-    u.pad = 0;
-    return u;
-  };
   for (int i = tid; i < kBins; i += kPlanThreads) bins[i] = 0;
   __syncthreads();
   // bin of a tile count, so that longer units come first (with under kBins tiles: in exact order)
-  const int shift = max(0, 32 - __clz((kcap + 31) / 32) - 10);
+  const int shift = max(0, 32 - __clz((a.bt_stride * kPage + 31) / 32) - 10);
   auto bin_of = [&](int tiles) { return kBins - 1 - min(tiles >> shift, kBins - 1); };
-  uint32_t mine = 0;   // half the tiles: under 256 blocks of up to 2^25 tiles stay in 32 bits
-  const int n_blocks = blocks([&](int s, int r0, int n, int j, int) {
-    const int t = unit_of(s, r0, n, j).t1;
-    mine += t >> 1;
-    atomicAdd(&bins[bin_of(t)], 1);
-  });
+  const int n_blocks = blocks([&](const PrefillUnit& u, int) { atomicAdd(&bins[bin_of(u.t1)], 1); });
   __syncthreads();
   if (!kv8_prefill_cuts(n_blocks, a.Hkv)) {
     int all, sum = 0;
     for (int k = 0; k < kPer; ++k) sum += bins[tid * kPer + k];
-    int at = scan(sum, all);
+    int at = plan_scan(lds, sum, all);
     for (int k = 0; k < kPer; ++k) {
       const int n = bins[tid * kPer + k];
       bins[tid * kPer + k] = at;
       at += n;
     }
     __syncthreads();
-    blocks([&](int s, int r0, int n, int j, int) {
-      const PrefillUnit u = unit_of(s, r0, n, j);
-      const int i = atomicAdd(&bins[bin_of(u.t1)], 1);
+    const int n_units = min(n_blocks, p.unit_cap);
+    const int half = kPrefillResident / 2 / a.Hkv, window = min(n_units, kPrefillResident / a.Hkv);
+    blocks([&](const PrefillUnit& u, int) {
+      int i = atomicAdd(&bins[bin_of(u.t1)], 1);
+      if (i >= half && i < window) i = half + window - 1 - i;
       if (i < p.unit_cap) p.units[i] = u;
     });
     if (tid == 0) {
-      p.head->n_units = min(n_blocks, p.unit_cap);
+      p.head->n_units = n_units;
       p.head->n_jobs = 0;
     }
     return;
   }
-  // few blocks, under kCus: cut the long ones
-  int halves;
-  scan((int)mine, halves);
-  const int64_t tiles = ((int64_t)(uint32_t)halves + n_blocks) * 2;   // no less than their sum
-  const int share = kv8_prefill_share(tiles, a.Hkv);
   __shared__ PrefillUnit whole[kCus];
-  __shared__ int32_t first[kCus];   // a block's first unit
-  blocks([&](int s, int r0, int n, int j, int i) { whole[i] = unit_of(s, r0, n, j); });
+  __shared__ int32_t first[kCus], parts[kCus];
+  blocks([&](const PrefillUnit& u, int i) { whole[i] = u; });
   __syncthreads();
-  int n_part = 0;   // of block tid
-  if (tid < n_blocks) n_part = kv8_prefill_parts(whole[tid].t1, share);
-  int n_units, n_slots, n_jobs;
-  const int at = scan(n_part, n_units), slot0 = scan(n_part > 1 ? n_part : 0, n_slots);
-  const int job = scan(n_part > 1 ? 1 : 0, n_jobs);
+  const PlanCut c = plan_cut(lds, a, n_blocks, tid < n_blocks ? whole[tid].t1 : 0);
   if (tid < n_blocks) {
-    first[tid] = at;
-    whole[tid].t0 = n_part;
-    whole[tid].slot = slot0;
-    if (n_part > 1) p.jobs[job] = PrefillJob{whole[tid].row, whole[tid].nq, slot0, n_part};
+    first[tid] = c.first;
+    parts[tid] = c.parts;
+    whole[tid].slot = c.slot0;
+    if (c.parts > 1) p.jobs[c.job] = PrefillJob{whole[tid].row, whole[tid].nq, c.slot0, c.parts};
   }
   __syncthreads();
-  n_units = min(n_units, p.unit_cap);
-  for (int i = tid; i < n_units; i += kPlanThreads) {
-    int lo = 0, hi = n_blocks;   // the last block whose units begin at or before i
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (first[mid] <= i) lo = mid;
-      else hi = mid;
-    }
-    PrefillUnit u = whole[lo];
-    const int parts = u.t0, k = i - first[lo], len = kv8_prefill_part_tiles(u.t1, parts);
-    u.t0 = k * len;
-    u.t1 = min(u.t1, u.t0 + len);
-    u.slot = parts > 1 ? u.slot + k : -1;
+  for (int i = tid; i < c.n_units; i += kPlanThreads) {
+    const int b = last_at(first, n_blocks, i);
+    PrefillUnit u = whole[b];
+    plan_part(u, parts[b], u.slot, i - first[b]);
     p.units[i] = u;
   }
   if (tid == 0) {
-    p.head->n_units = n_units;
-    p.head->n_jobs = n_jobs;
+    p.head->n_units = c.n_units;
+    p.head->n_jobs = c.n_jobs;
   }
 }
 
@@ -607,7 +685,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
 // and writes them as exact bf16 (the page's power of two is applied by the conversion) in the order of the matrix
 // operands.  A step multiplies K of tile t + 1 and V of tile t, so that the scores of the next tile and the
 // exponentials of this one run side by side; the conversions run beside the product with V.
-template <int DH>
+template <int DH, bool SMALL>
 __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   constexpr int KS = DH / 16;      // 16-dim steps of QK^T
   constexpr int DT = DH / 32;      // 32-dim tiles of O^T
@@ -615,17 +693,21 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   __shared__ __attribute__((aligned(1024))) bf16_t K0[KT], K1[KT], V0[KT], V1[KT];
   const Kv8AttnArgs& a = p.a;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // Workgroup -> (unit, head): heads innermost, so that with 8 of them an XCD works on one head's keys; and among the
-  // first resident workgroups the second half of the units in reverse, so that a CU gets a long one and a short one
-  const int n_units = p.head->n_units;
-  int ui = blockIdx.x / a.Hkv;
-  const int kvh = blockIdx.x - ui * a.Hkv;
-  if (ui >= n_units) return;
-  {
-    const int half = kPrefillResident / 2 / a.Hkv, window = min(n_units, kPrefillResident / a.Hkv);
-    if (ui >= half && ui < window) ui = half + window - 1 - ui;
+  // Workgroup -> (unit, head): heads innermost, so that with 8 of them an XCD works on one head's keys
+  const int ui = blockIdx.x / a.Hkv, kvh = blockIdx.x - ui * a.Hkv;
+  PrefillUnit it;
+  if constexpr (SMALL) {
+    __shared__ SmallPlan<false> plan;
+    if (ui >= plan_small(plan, a, p.qpi, ui)) return;
+    // (what came through LDS is wavefront-uniform)
+    const int32_t* u = reinterpret_cast<const int32_t*>(&plan.unit);
+    int32_t* v = reinterpret_cast<int32_t*>(&it);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(PrefillUnit) / 4); ++i) v[i] = __builtin_amdgcn_readfirstlane(u[i]);
+  } else {
+    it = p.units[ui];   // (asked for together with the number of units; the array holds one for each workgroup)
+    if (ui >= p.head->n_units) return;
   }
-  const PrefillUnit it = p.units[ui];
   const int G = a.Hq / a.Hkv;
   const int npairs = it.nq * G;
   const int kend = min(it.pos + it.nq, a.bt_stride * kPage);   // keys [0, kend) are visible to some pair
@@ -955,7 +1037,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
 // Joins the parts of cut blocks: DH/4 threads a (query, head) pair and one of R streams of parts, P pairs a
 // workgroup; the workgroups walk the pairs of all jobs, so that a launch with nothing to join (the host does not know)
 // is short.
-template <int DH>
+template <int DH, bool SMALL>
 __global__ __launch_bounds__(256) void kv8_prefill_merge_kernel(Kv8PrefillArgs p) {
   constexpr int C = DH / 4, R = 4, P = 256 / C / R;
   const Kv8AttnArgs& a = p.a;
@@ -963,11 +1045,14 @@ __global__ __launch_bounds__(256) void kv8_prefill_merge_kernel(Kv8PrefillArgs p
   const int c = threadIdx.x % C, r = threadIdx.x / C % R, pl = threadIdx.x / C / R;
   __shared__ float2 s_ml[P][R];
   __shared__ float4 s_acc[P][R][C];
-  const int items = p.head->n_jobs * a.Hkv * (kPrefillPairs / P);
+  __shared__ SmallPlan<true> plan;
+  constexpr int GROUPS = kPrefillPairs / P;
+  const int n_jobs = SMALL ? plan_small(plan, a, p.qpi, 0) : p.head->n_jobs;
+  const int items = n_jobs * a.Hkv * GROUPS;
   for (int i = blockIdx.x; i < items; i += gridDim.x) {
-    const int job = i / (kPrefillPairs / P), jb = job / a.Hkv, kvh = job - jb * a.Hkv;
-    const PrefillJob mg = p.jobs[jb];
-    const int pair0 = i % (kPrefillPairs / P) * P;
+    const int job = i / GROUPS, jb = job / a.Hkv, kvh = job - jb * a.Hkv;
+    const PrefillJob mg = SMALL ? plan.jobs[jb] : p.jobs[jb];
+    const int pair0 = i % GROUPS * P;
     if (pair0 >= mg.nq * G) continue;   // (uniform over the workgroup)
     const int pair = pair0 + pl;        // a pair past the block's: its slot exists, its row is not written
     const size_t slot = ((size_t)kvh * p.slots + mg.slot0) * kPrefillPairs + pair;
@@ -1005,6 +1090,7 @@ static hipError_t decode_launch(const Kv8AttnArgs& a, hipStream_t st) {
   }
   hipLaunchKernelGGL((kv8_decode_kernel<DH, PLANNED>), dim3((unsigned)kv8_decode_items(a.S, a.Hkv)), dim3(64), 0, st, a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (a.bt_stride <= kKv8MinPages) return hipSuccess;   // no context is longer than a part
   const int64_t quads = (int64_t)a.S * ((a.Hq + 3) / 4);
   if (quads < kCus && a.bt_stride > kMergeAlone * kKv8MinPages)
     hipLaunchKernelGGL((kv8_merge_kernel<DH, 1, PLANNED>), dim3((unsigned)(a.S * a.Hq)), dim3(256), 0, st, a);
@@ -1021,6 +1107,20 @@ hipError_t kv8_decode_launch(const Kv8AttnArgs& args, hipStream_t st) {
   return a.dh == 128 ? decode_launch<128, false>(a, st) : decode_launch<64, false>(a, st);
 }
 
+// whole: blocks at most; cuts: whether blocks may be cut
+template <int DH, bool SMALL>
+static hipError_t prefill_launch(const Kv8PrefillArgs& p, int64_t whole, bool cuts, hipStream_t st) {
+  const int hkv = p.a.Hkv;
+  const int64_t units = cuts ? p.unit_cap : std::min<int64_t>(whole, p.unit_cap);
+  hipLaunchKernelGGL((kv8_prefill_kernel<DH, SMALL>), dim3((unsigned)(units * hkv)), dim3(256), 0, st, p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || !cuts) return e;
+  // cut blocks number under kCus / hkv, and no more than there are blocks; 256 / (dh / 4) / 4 pairs a workgroup
+  const int64_t jobs = std::min<int64_t>(whole, (kCus + hkv - 1) / hkv) * hkv;
+  const int64_t groups = std::min<int64_t>(jobs * kPrefillPairs / (256 / DH), 2 * kCus);
+  hipLaunchKernelGGL((kv8_prefill_merge_kernel<DH, SMALL>), dim3((unsigned)groups), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
 hipError_t kv8_prefill_launch(const Kv8AttnArgs& a, hipStream_t st) {
   const PrefillWs w = prefill_ws(a.S, a.T, a.Hq, a.Hkv, a.dh);
   Kv8PrefillArgs p{};
@@ -1033,19 +1133,15 @@ hipError_t kv8_prefill_launch(const Kv8AttnArgs& a, hipStream_t st) {
   p.unit_cap = w.unit_cap;
   p.slots = w.slots;
   p.qpi = prefill_queries_per_item(a.Hq / a.Hkv);
-  auto go = [&](auto kernel, int64_t grid, int threads) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, st, p);
-    return hipGetLastError();
-  };
-  hipError_t e = go(kv8_prefill_plan_kernel, 1, kPlanThreads);
-  if (e != hipSuccess) return e;
-  const int64_t grid = (int64_t)w.unit_cap * a.Hkv;
-  e = a.dh == 128 ? go(kv8_prefill_kernel<128>, grid, 256) : go(kv8_prefill_kernel<64>, grid, 256);
-  if (e != hipSuccess) return e;
-  // cut blocks number under kCus / Hkv, and no more than there are blocks; 256 / (dh / 4) / 4 pairs a workgroup
-  const int64_t jobs = std::min<int64_t>((int64_t)a.T / p.qpi + a.S, (kCus + a.Hkv - 1) / a.Hkv) * a.Hkv;
-  const int64_t groups = std::min<int64_t>(jobs * kPrefillPairs / (256 / a.dh), 2 * kCus);
-  return a.dh == 128 ? go(kv8_prefill_merge_kernel<128>, groups, 256) : go(kv8_prefill_merge_kernel<64>, groups, 256);
+  // A block is cut only into parts of more than kPrefillMinTiles / 2 tiles, so short tables need no room for parts
+  const int64_t whole = std::min<int64_t>((int64_t)a.T / p.qpi + a.S, INT32_MAX);
+  const int most = (a.bt_stride * kPage + 63) / 64 * 2;   // tiles of the longest block there can be
+  const bool cuts = most > kPrefillMinTiles;
+  if (a.S <= kPlanThreads && whole <= kPlanThreads)
+    return a.dh == 128 ? prefill_launch<128, true>(p, whole, cuts, st) : prefill_launch<64, true>(p, whole, cuts, st);
+  hipLaunchKernelGGL(kv8_prefill_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  return a.dh == 128 ? prefill_launch<128, false>(p, whole, cuts, st) : prefill_launch<64, false>(p, whole, cuts, st);
 }
 
 }  // namespace hxf
