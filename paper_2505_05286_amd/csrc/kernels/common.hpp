@@ -53,6 +53,23 @@ __device__ __forceinline__ uint2 e4m3x4_to_bf16(uint32_t c, float scale) {
   return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
 }
 
+// The same as fp16 (a subnormal or zero where the product is one), and two floats as fp16, nearest even
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint2 e4m3x4_to_f16(uint32_t c, float scale) {
+  const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, scale, false);
+  const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, scale, true);
+  return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+}
+__device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
+  const f16x2_t v = {(_Float16)lo, (_Float16)hi};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ f16x8 as_f16x8(uint4 v) { return __builtin_bit_cast(f16x8, v); }
+__device__ __forceinline__ f32x4 mfma16x16x32(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // 32x32x16 bf16 MFMA: A lane l holds row l%32, k (l/32)*8..+8; B lane l holds
@@ -60,6 +77,10 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // column l%32.
 __device__ __forceinline__ f32x16 mfma32x32x16(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ f32x16 mfma32x32x16(f16x8 a, f16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
 template <typename T>

@@ -99,16 +99,34 @@ __device__ __forceinline__ void kv8_load_page(Kv8Pair<DH>& R, int h, const Kv8At
 // Mask keeping the first n (0..4) of four bytes
 __device__ __forceinline__ uint32_t keep_bytes(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1; }
 
+// The product with V runs in fp16, whose weights are rounded to 2^-11 where bf16's are to 2^-8: V's codes are exact in it,
+// and a page's power of two goes into the exponent of its weights,
+//   w = 2^(x + e - m),  o += w c,  l += w 2^-e,
+// so that neither side leaves fp16's range whatever the scales are.  The reference m is set kRefBelow under the largest
+// x + e so far and moves only when one exceeds it by kRefRange: the weights stay under 2^15, the largest is 2^7 or more, and
+// one is rounded to 2^-11 of itself or to 2^-32 of the largest (fp16's subnormals), whichever is more.  A page scale under 2^kMinVExp counts as 2^kMinVExp
+// with smaller codes (fp16 subnormals down to 2^-84): pages of zeros, whose nominal scale is 2^-100, would otherwise
+// stand so far below their neighbours that their weights left the fp32 range of l.
+// v_exponent packs e and the codes' shift (e * 256 + shift) for a lane's table of pages; 0 for an entry that is no page.
+constexpr float kRefBelow = 7.f, kRefRange = 15.f;
+constexpr int kMinVExp = -60;
+__device__ __forceinline__ int v_exponent(float scale, bool there) {
+  const int b = (int)(__float_as_uint(scale) >> 23 & 255) - 127, e = max(b, kMinVExp);
+  return there ? e * 256 + (e - b) : 0;
+}
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((127 + e) << 23); }
+
 template <int DH>
 struct Kv8State {
   f32x4 acc[DH / 16];   // tile (u, n): row r of the lane's column is dimension u*64 + r*4 + n
-  float m, l;           // reference maximum of the column (log2 units); the lane's part of the denominator
+  float m, l;           // reference of the column's x + e (log2 units); the lane's part of the denominator
 };
 
-// Scores, online softmax and PV product of one pair.  ks, vs: the pages' scales; cnt: their tokens that count.
+// Scores, online softmax and PV product of one pair.  ks: the pages' K scales; ve: their v_exponent; cnt: their tokens
+// that count.
 template <int DH>
 __device__ __forceinline__ void kv8_pair(Kv8State<DH>& S, const Kv8Pair<DH>& R, const bf16x8 (&qf)[DH / 32],
-                                         const float (&ks)[2], const float (&vs)[2], const int (&cnt)[2],
+                                         const float (&ks)[2], const int (&ve)[2], const int (&cnt)[2],
                                          float scale_log2, int lane) {
   const int t0 = (lane >> 4) * 4;
   const bool full = cnt[0] + cnt[1] == 2 * kPage;   // wavefront-uniform
@@ -125,28 +143,31 @@ __device__ __forceinline__ void kv8_pair(Kv8State<DH>& S, const Kv8Pair<DH>& R, 
       s = mfma16x16x32(as_bf16x8(make_uint4(w2.x, w2.y, w3.x, w3.y)), qf[2 * u + 1], s);
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[4 * h + e] = full || t0 + e < cnt[h] ? s[e] * scale_log2 : kNegInf;
+    for (int e = 0; e < 4; ++e)
+      x[4 * h + e] = full || t0 + e < cnt[h] ? fmaf(s[e], scale_log2, (float)(ve[h] >> 8)) : kNegInf;
   }
   float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
   mx = half_swap_max(row_swap_max(mx));
-  // the reference moves only where a score exceeds it by more than 2^8: the weights stay below 256
-  if (__any(mx > S.m + 8.f)) {
-    const float m_new = fmaxf(S.m, mx);
+  if (__any(mx > S.m + kRefRange)) {
+    const float m_new = fmaxf(S.m, mx - kRefBelow);
     const float alpha = __builtin_amdgcn_exp2f(S.m - m_new);
     S.m = m_new;
     S.l *= alpha;
 #pragma unroll
     for (int n = 0; n < DH / 16; ++n) S.acc[n] *= alpha;
   }
-  float p[8];
+  float p[8], sum[2];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    p[e] = __builtin_amdgcn_exp2f(x[e] - S.m);
-    S.l += p[e];
+  for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(x[e] - S.m);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    sum[h] = (p[4 * h] + p[4 * h + 1]) + (p[4 * h + 2] + p[4 * h + 3]);
+    S.l = fmaf(sum[h], power_of_two(-(ve[h] >> 8)), S.l);
   }
-  // the weights of the product with V are rounded to bf16, the type of the matrix operand; the denominator is not
-  const bf16x8 pf =
-      as_bf16x8(make_uint4(pack_bf2(p[0], p[1]), pack_bf2(p[2], p[3]), pack_bf2(p[4], p[5]), pack_bf2(p[6], p[7])));
+  // the weights of the product with V are rounded to fp16, the denominator's are not
+  const f16x8 pf =
+      as_f16x8(make_uint4(pack_h2(p[0], p[1]), pack_h2(p[2], p[3]), pack_h2(p[4], p[5]), pack_h2(p[6], p[7])));
+  const float shift[2] = {power_of_two(-(ve[0] & 255)), power_of_two(-(ve[1] & 255))};
   // places that do not count may hold NaN codes, and zero times NaN is NaN
   const uint32_t keep[2] = {full ? ~0u : keep_bytes(cnt[0] - t0), full ? ~0u : keep_bytes(cnt[1] - t0)};
 #pragma unroll
@@ -155,8 +176,8 @@ __device__ __forceinline__ void kv8_pair(Kv8State<DH>& S, const Kv8Pair<DH>& R, 
     const uint32_t cb[4] = {R.v[1][u].x, R.v[1][u].y, R.v[1][u].z, R.v[1][u].w};
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      const uint2 va = e4m3x4_to_bf16(ca[n] & keep[0], vs[0]), vb = e4m3x4_to_bf16(cb[n] & keep[1], vs[1]);
-      S.acc[4 * u + n] = mfma16x16x32(as_bf16x8(make_uint4(va.x, va.y, vb.x, vb.y)), pf, S.acc[4 * u + n]);
+      const uint2 va = e4m3x4_to_f16(ca[n] & keep[0], shift[0]), vb = e4m3x4_to_f16(cb[n] & keep[1], shift[1]);
+      S.acc[4 * u + n] = mfma16x16x32(as_f16x8(make_uint4(va.x, va.y, vb.x, vb.y)), pf, S.acc[4 * u + n]);
     }
   }
 }
@@ -211,15 +232,17 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
   // scales of the pages being loaded and of those being multiplied.  A scale of 0 marks an entry that is no page.
   auto entries = [&](int r0) { return r0 + lane < np ? bt[r0 + lane] : 0; };
   int blk = entries(0), blk_next = entries(kWave);
-  float ks_next, vs_next;
+  float ks_next;
+  int ve_next;
   auto scales = [&]() {
     const bool there = (uint32_t)blk < (uint64_t)a.pool.n_blocks;
     if (!there) blk = 0;
     ks_next = there ? ksp[blk] : 0.f;
-    vs_next = there ? vsp[blk] : 0.f;
+    ve_next = v_exponent(vsp[blk], there);
   };
   scales();
-  float ks_now = ks_next, vs_now = vs_next;
+  float ks_now = ks_next;
+  int ve_now = ve_next;
   Kv8State<DH> S;
 #pragma unroll
   for (int i = 0; i < DH / 16; ++i) S.acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -244,19 +267,19 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
   auto multiply = [&](const Kv8Pair<DH>& P, int r) __attribute__((always_inline)) {
     if (r && r % kWave == 0) {
       ks_now = ks_next;
-      vs_now = vs_next;
+      ve_now = ve_next;
     }
-    float ks[2], vs[2];
-    int cnt[2];
+    float ks[2];
+    int ve[2], cnt[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int s = __builtin_amdgcn_readlane(__float_as_int(ks_now), r % kWave + h);
       const bool there = s != 0 && r + h < np;
       ks[h] = there ? __int_as_float(s) : 1.f;
-      vs[h] = there ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs_now), r % kWave + h)) : 1.f;
+      ve[h] = there ? __builtin_amdgcn_readlane(ve_now, r % kWave + h) : 0;
       cnt[h] = there ? min(kPage, n - (p0 + r + h) * kPage) : 0;
     }
-    kv8_pair<DH>(S, P, qf, ks, vs, cnt, a.scale_log2, lane);
+    kv8_pair<DH>(S, P, qf, ks, ve, cnt, a.scale_log2, lane);
   };
   static_for<NB - 1>([&](auto ic) {
     constexpr int J = decltype(ic)::value;
@@ -679,11 +702,11 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
 // Causal attention of a unit and kv-head, as the bf16 cache's prefill kernel computes it: the (query, head) pairs
 // of the block are the columns of
 //   S^T[32 keys x 32 pairs] = K[32 x dh] . Q^T[dh x 32]       (v_mfma_f32_32x32x16_bf16)
-//   O^T[32 dims x 32 pairs] += V^T[32 x 32 keys] . P^T[32 x 32]
-// with 32 pairs per wavefront.  Every wavefront multiplies every key, so a tile of 32 keys is turned into bf16 once
+//   O^T[32 dims x 32 pairs] += V^T[32 x 32 keys] . P^T[32 x 32]   (in fp16, see v_exponent)
+// with 32 pairs per wavefront.  Every wavefront multiplies every key, so a tile of 32 keys is converted once
 // for the workgroup, on its way into LDS: a thread loads DH/8 bytes of K and of V, two tiles ahead, into registers,
-// and writes them as exact bf16 (the page's power of two is applied by the conversion) in the order of the matrix
-// operands.  A step multiplies K of tile t + 1 and V of tile t, so that the scores of the next tile and the
+// and writes them, K as exact bf16 (the page's power of two is applied by the conversion), V's codes as exact fp16, in
+// the order of the matrix operands.  A step multiplies K of tile t + 1 and V of tile t, so that the scores of the next tile and the
 // exponentials of this one run side by side; the conversions run beside the product with V.
 template <int DH, bool SMALL>
 __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
@@ -739,13 +762,14 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   // tile's entries would leave no LDS read's wait without theirs.)
   auto entries = [&](int r0) { return bt[min(tbase * 2 + r0 + lane, last_page)]; };
   int blk = 0, blk_next = 0;
-  float ks_next = 0.f, vs_next = 0.f, ks_now = 0.f, vs_now = 0.f;
+  float ks_next = 0.f, ks_now = 0.f;
+  int ve_next = 0, ve_now = 0;
   auto scales = [&]() {
     const bool there = (uint32_t)blk < (uint32_t)a.pool.n_blocks;
     blk = there ? blk : 0;
     const float ks = ksp[blk], vs = vsp[blk];
     ks_next = there ? ks : 0.f;
-    vs_next = there ? vs : 0.f;
+    ve_next = v_exponent(vs, there);
   };
   // before K of tile t, a multiple of 32, is loaded; before K of any tile t is stored
   auto turn_loads = [&](int t) __attribute__((always_inline)) {
@@ -756,13 +780,13 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   auto turn_stores = [&](int t) __attribute__((always_inline)) {
     if ((t & 31) == 0) {
       ks_now = ks_next;
-      vs_now = vs_next;
+      ve_now = ve_next;
     }
   };
   // V of a tile is loaded and stored a step after its K, with the page and the scale that K looked up
   typedef uint32_t words_t[DH / 32];
   int e_last = 0, keep_lo = 0, keep_hi = 0;
-  float vs_last = 1.f;
+  float shift_last = 1.f;
   // (one buffer descriptor for each page: scalar work only, and the pools may exceed 4 GiB)
   auto page_rsrc = [&](const uint8_t* pool) __attribute__((always_inline)) {
     return make_rsrc(pool + kv_tile(kvh, a.pool.n_blocks, __builtin_amdgcn_readfirstlane(e_last), DH), kPage * DH);
@@ -800,13 +824,14 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
 #pragma unroll
     for (int c = 0; c < DH / 64; ++c) {
       const int row = v_row(lane * (DH / 64) + c);
-      const uint2 lo = e4m3x4_to_bf16(R[c] & keep_lo, vs_last), hi = e4m3x4_to_bf16(R[DH / 64 + c] & keep_hi, vs_last);
+      const uint2 lo = e4m3x4_to_f16(R[c] & keep_lo, shift_last), hi = e4m3x4_to_f16(R[DH / 64 + c] & keep_hi, shift_last);
       *reinterpret_cast<uint4*>(base + (pg * DH + row) * 16 + v_half(row, hw) * 8) = make_uint4(lo.x, lo.y, hi.x, hi.y);
     }
   };
   // scales and masks of tile t, before its K is stored (in a step: ahead of the matrix work, which waits for nothing
   // scalar then)
-  float ks_here = 1.f, vs_here = 1.f;
+  float ks_here = 1.f, shift_here = 1.f;
+  int e_now = 0, e_next = 0, e_after = 0;   // V exponents of the tile multiplied and of the two after it: of its pages, 16 bits each
   int lo_here = 0, hi_here = 0;
   auto look_up = [&](int t) __attribute__((always_inline)) {
     const int r = (t & 31) * 2;
@@ -817,15 +842,18 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     gone = (gone & ~(3u << sh)) | (3u - there0 - there1 * 2) << sh;
     const int sk = pg ? s1 : s0, none = (int)(pg ? there1 : there0) - 1;   // none: all ones where the page is none
     ks_here = __int_as_float(sk | (none & 0x3F800000));
-    const int sv = __builtin_amdgcn_readlane(__float_as_int(vs_now), r + pg);
-    vs_here = __int_as_float(sv | (none & 0x3F800000));
+    const int v0 = __builtin_amdgcn_readlane(ve_now, r), v1 = __builtin_amdgcn_readlane(ve_now, r + 1);
+    shift_here = power_of_two(-((pg ? v1 : v0) & 255));
+    e_now = e_next;
+    e_next = e_after;
+    e_after = (int)((uint32_t)(v0 >> 8) & 0xFFFFu | (uint32_t)(v1 >> 8) << 16);
     // places of V that do not count may hold NaN codes, and zero times NaN is NaN
     const int left = (kend - ((tbase + t) * 32 + pg * kPage + hw * 4)) & ~none;
     lo_here = keep_bytes(left);
     hi_here = keep_bytes(left - 8);
   };
   auto store_k = [&](const words_t& R, bf16_t* base) __attribute__((always_inline)) {
-    vs_last = vs_here;
+    shift_last = shift_here;
     keep_lo = lo_here;
     keep_hi = hi_here;
 #pragma unroll
@@ -856,13 +884,18 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     for (int ks = 0; ks < KS; ++ks) x = mfma32x32x16(kf[ks], qf[ks], x);
     return x;
   };
-  auto score_max = [&](const f32x16& x) __attribute__((always_inline)) {
-    float v = x[0];
+  // largest x + e of the pair; e: the exponents of the tile's pages (rows r < 8 and r >= 8 of the accumulator)
+  auto exp_of = [](int e, int page) __attribute__((always_inline)) { return page ? e >> 16 : (int)(int16_t)e; };
+  auto score_max = [&](const f32x16& x, int e) __attribute__((always_inline)) {
+    float v = x[0], u = x[8];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) v = fmaxf(v, x[r]);
-    return half_swap_max(v) * a.scale_log2;
+    for (int r = 1; r < 8; ++r) {
+      v = fmaxf(v, x[r]);
+      u = fmaxf(u, x[8 + r]);
+    }
+    return half_swap_max(fmaxf(fmaf(v, a.scale_log2, (float)exp_of(e, 0)), fmaf(u, a.scale_log2, (float)exp_of(e, 1))));
   };
-  // the mask of a tile that needs one, then the reference maximum, which moves only where a score exceeds it by 2^8
+  // the mask of a tile that needs one, then the reference
   auto settle = [&](f32x16& x, float& mx, int t) __attribute__((always_inline)) {
     const int k0 = (tbase + t) * 32;
     const uint32_t miss = gone >> ((t & 15) * 2) & 3;
@@ -872,10 +905,10 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
         const int key = k0 + (r >> 2) * 8 + h * 4 + (r & 3);
         if (key > qpos || key >= kend || (miss >> (r >> 3) & 1)) x[r] = kNegInf;
       }
-      mx = score_max(x);
+      mx = score_max(x, e_now);
     }
-    if (__any(mx > m + 8.f)) {
-      const float m_new = fmaxf(m, mx);
+    if (__any(mx > m + kRefRange)) {
+      const float m_new = fmaxf(m, mx - kRefBelow);
       const float alpha = __builtin_amdgcn_exp2f(m - m_new);
       m = m_new;
       l *= alpha;
@@ -892,22 +925,24 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) vv[st][dt] = *reinterpret_cast<const uint4*>(base + v_off + (st * DH + dt * 32) * 16);
   };
-  bf16x8 pf[2];
+  f16x8 pf[2];
   auto probs = [&](const f32x16& x) __attribute__((always_inline)) {
-    float ps = 0.f;
+    const float c[2] = {(float)exp_of(e_now, 0) - m, (float)exp_of(e_now, 1) - m};
+    float ps[2] = {0.f, 0.f};
     float pv[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      pv[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale_log2, -m));
-      ps += pv[r];
+      pv[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale_log2, c[r >> 3]));
+      ps[r >> 3] += pv[r];
     }
-    l += ps;
-    // rounded to bf16, the type of the matrix operand; the denominator is not
+    l = fmaf(ps[0], power_of_two(-exp_of(e_now, 0)), l);
+    l = fmaf(ps[1], power_of_two(-exp_of(e_now, 1)), l);
+    // the weights of the product with V are rounded to fp16, the denominator's are not
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-      bf16x8 v;
+      f16x8 v;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = (__bf16)pv[st * 8 + j];
+      for (int j = 0; j < 8; ++j) v[j] = (_Float16)pv[st * 8 + j];
       pf[st] = v;
     }
   };
@@ -915,7 +950,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
 #pragma unroll
     for (int st = 0; st < 2; ++st)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32x32x16(as_bf16x8(vv[st][dt]), pf[st], o[dt]);
+      for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32x32x16(as_f16x8(vv[st][dt]), pf[st], o[dt]);
   };
 
   // order of a step's matrix work: the K reads, then QK^T of the next tile one MFMA at a time with a V read and the
@@ -967,7 +1002,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     __syncthreads();
     read_k(K0);
     f32x16 s = scores();
-    float mx = score_max(s);
+    float mx = score_max(s, e_next);   // (look_up has gone as far as tile 1)
     __syncthreads();
     // a step: V of tile t + 1 and K of t + 2 into LDS, V of t + 3 and K of t + 4 on their way, scores of t + 1, output of t.
     // Past the last tile it moves and scores the last page again, which nothing uses: no step has a branch around
@@ -986,7 +1021,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
       accumulate();
       store_v(rv, v_next);
       store_k(rk, k_now);
-      mx = score_max(next);
+      mx = score_max(next, e_next);
       s = next;
       interleave();
       __builtin_amdgcn_sched_barrier(0);

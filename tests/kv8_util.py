@@ -163,7 +163,7 @@ def slot_map(start, n_new, free, bt, T):
 def attend(q, cache, blocks, n, hq, first=None):
     """softmax(q k / sqrt(dh)) v over the first n places of `blocks`: q float64 [m, Hq, dh]; query i sees the
     positions up to first + i (None: all).  Places of an entry that is no page have no weight.  Returns the
-    outputs and sum p |v|, the size that errors of the weights are measured by."""
+    outputs, and the error that assert_attention allows apart from the output's own rounding."""
     m, G = len(q), hq // cache.hkv
     out, size = np.zeros_like(q), np.zeros_like(q)
     if n == 0:
@@ -185,17 +185,25 @@ def attend(q, cache, blocks, n, hq, first=None):
         w /= w.sum(-1, keepdims=True)
         v = np.where(there[:, None], v, 0)
         out[:, h * G:(h + 1) * G] = w @ v
-        size[:, h * G:(h + 1) * G] = w @ np.abs(v)
+        # weights in fp16: 2^-11 of each, or, where it is less than 2^-14, 2^-25 of a unit of which the largest weight
+        # is 2^7 or more.  A weight is p 2^e with e its page's exponent (no less than -60), its partner v 2^-e:
+        # the second kind sums to at most 2^-32 (p_j 2^e_j) sum |v| 2^-e, j the key of the largest p 2^e.
+        e = np.maximum(np.log2(np.repeat(cache.scale["v"][h, at], PAGE)[:n].astype(np.float64)), -60)
+        e = np.where(there, e, 0)
+        j = np.argmax(np.where(seen[:, None], x * np.log2(np.e) + e, -np.inf), -1)
+        top = np.take_along_axis(w, j[..., None], -1) * np.exp2(e)[j][..., None]
+        floor = 2.0 ** -32 * top * ((seen[:, None] * np.exp2(-e)) @ np.abs(v))
+        size[:, h * G:(h + 1) * G] = (2.0 ** -11 + 2.0 ** -11) * (w @ np.abs(v)) + floor
     return out, size
 
 
 def assert_attention(got, ref, size, what):
-    """The kernels take q, K and V exactly, sum in float32, and round twice to bf16 (2^-8 of the value each): the
-    weights of the product with V, and the output.  The float32 scores (sums of dh products, times a constant,
-    exponentials) are off by under 2^-12 for the scores of these tests (|x| < 64: 64 * 2^-24 * a few roundings,
-    and 128 * 2^-24 of the products' sum), and the float32 sums by less."""
+    """The kernels take q, K and V exactly, sum in float32, and round twice: the weights of the product with V to fp16
+    (see attend) and the output to bf16 (2^-8).  The float32 scores (sums of dh products, times a constant,
+    exponentials) are off by under 2^-12 for the scores of these tests (|x| < 64: 64 * 2^-24 * a few
+    roundings, and 128 * 2^-24 of the products' sum), and the float32 sums by less: 2^-11 of the weights in all."""
     assert np.all(np.isfinite(got)), what
-    over = np.abs(got - ref) - (2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -11) * size + 1e-30)
+    over = np.abs(got - ref) - (2.0 ** -8 * np.abs(ref) + size + 1e-30)
     assert over.max(initial=-1) <= 0, f"{what}: over by {over.max():.3e} at {np.unravel_index(over.argmax(), over.shape)}"
 
 

@@ -361,11 +361,28 @@ def test_decode_extreme_scores():
         cache, bt = _attention_case(rng, [700, 3], 8, 2, 128)
         cache.scale["k"][:] = np.minimum(cache.scale["k"], 2.0 ** -4)
         _decode(cache, bt, np.array([700, 3]), 8, rng, what=f"q {q_scale}", q_scale=q_scale)
-    for s in (2.0 ** -90, 2.0 ** 60):
+    for s in (2.0 ** -50, 2.0 ** -66, 2.0 ** 60, 2.0 ** 110):
         cache, bt = _attention_case(rng, [90], 4, 1, 64)
         cache.scale["v"][:] *= s
         cache.scale["k"][:] *= 2.0 ** -40
         _decode(cache, bt, np.array([90]), 4, rng, what=f"v {s}")
+        _prefill(cache, bt, np.array([70]), np.array([20]), 4, rng, what=f"v {s}")
+
+
+def test_attention_over_pages_of_very_different_sizes():
+    """Scales of V far apart in one context, pages of zeros (whose scale is the least there is) among them: zeros
+    weigh in the denominator as any other value does."""
+    rng = np.random.default_rng(41)
+    for dh in (64, 128):
+        cache, bt = _attention_case(rng, [400, 33], 4, 2, dh)
+        for b in range(25):
+            cache.scale["v"][:, bt[0, b]] = 2.0 ** [-6, -100, 3, -30, 10][b % 5]
+            if b % 5 == 1:
+                cache.codes["v"][:, bt[0, b]] = 0
+        cache.scale["v"][:, bt[1, 0]] = 2.0 ** -100
+        cache.codes["v"][:, bt[1, 0]] = 0
+        _decode(cache, bt, np.array([400, 33]), 4, rng, what="sizes")
+        _prefill(cache, bt, np.array([300, 0]), np.array([100, 33]), 4, rng, what="sizes")
 
 
 def test_decode_offsets_beyond_32_bits():
