@@ -99,34 +99,27 @@ __device__ __forceinline__ void kv8_load_page(Kv8Pair<DH>& R, int h, const Kv8At
 // Mask keeping the first n (0..4) of four bytes
 __device__ __forceinline__ uint32_t keep_bytes(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1; }
 
-// The product with V runs in fp16, whose weights are rounded to 2^-11 where bf16's are to 2^-8: V's codes are exact in it,
-// and a page's power of two goes into the exponent of its weights,
-//   w = 2^(x + e - m),  o += w c,  l += w 2^-e,
-// so that neither side leaves fp16's range whatever the scales are.  The reference m is set kRefBelow under the largest
-// x + e so far and moves only when one exceeds it by kRefRange: the weights stay under 2^15, the largest is 2^7 or more, and
-// one is rounded to 2^-11 of itself or to 2^-32 of the largest (fp16's subnormals), whichever is more.  A page scale under 2^kMinVExp counts as 2^kMinVExp
-// with smaller codes (fp16 subnormals down to 2^-84): pages of zeros, whose nominal scale is 2^-100, would otherwise
-// stand so far below their neighbours that their weights left the fp32 range of l.
-// v_exponent packs e and the codes' shift (e * 256 + shift) for a lane's table of pages; 0 for an entry that is no page.
+// The product with V runs in fp16, whose weights are rounded to 2^-11 where bf16's are to 2^-8, and V's codes are exact in
+// it: with E the largest exponent of the pages' scales so far, V enters as code * 2^(its exponent - E) and the outputs are
+// in units of 2^E, which moves (upwards) with the tables of 64 pages.  Codes of a page under 2^-15 of the largest scale
+// become fp16 subnormals, off by up to 2^-25 of 2^E.  The weights are 2^(x - m): the reference m is set kRefBelow under
+// the largest score so far and moves only when one exceeds it by kRefRange, so that they stay under 2^15, the largest is
+// 2^7 or more, and one is rounded to 2^-11 of itself or to 2^-32 of the largest, whichever is more.
 constexpr float kRefBelow = 7.f, kRefRange = 15.f;
-constexpr int kMinVExp = -60;
-__device__ __forceinline__ int v_exponent(float scale, bool there) {
-  const int b = (int)(__float_as_uint(scale) >> 23 & 255) - 127, e = max(b, kMinVExp);
-  return there ? e * 256 + (e - b) : 0;
-}
-__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((127 + e) << 23); }
-
+constexpr int kNoExp = -127;   // exponent of an entry that is no page
+__device__ __forceinline__ int exponent_of(float scale) { return (int)(__float_as_uint(scale) >> 23 & 255) - 127; }
+__device__ __forceinline__ float power_of_two(int e) { return e < -126 ? 0.f : __int_as_float((127 + e) << 23); }
 template <int DH>
 struct Kv8State {
   f32x4 acc[DH / 16];   // tile (u, n): row r of the lane's column is dimension u*64 + r*4 + n
-  float m, l;           // reference of the column's x + e (log2 units); the lane's part of the denominator
+  float m, l;           // reference of the column's scores (log2 units); the lane's part of the denominator
 };
 
-// Scores, online softmax and PV product of one pair.  ks: the pages' K scales; ve: their v_exponent; cnt: their tokens
-// that count.
+// Scores, online softmax and PV product of one pair.  ks: the pages' K scales; vs: what their V codes are
+// multiplied by; cnt: their tokens that count.
 template <int DH>
 __device__ __forceinline__ void kv8_pair(Kv8State<DH>& S, const Kv8Pair<DH>& R, const bf16x8 (&qf)[DH / 32],
-                                         const float (&ks)[2], const int (&ve)[2], const int (&cnt)[2],
+                                         const float (&ks)[2], const float (&vs)[2], const int (&cnt)[2],
                                          float scale_log2, int lane) {
   const int t0 = (lane >> 4) * 4;
   const bool full = cnt[0] + cnt[1] == 2 * kPage;   // wavefront-uniform
@@ -143,8 +136,7 @@ __device__ __forceinline__ void kv8_pair(Kv8State<DH>& S, const Kv8Pair<DH>& R, 
       s = mfma16x16x32(as_bf16x8(make_uint4(w2.x, w2.y, w3.x, w3.y)), qf[2 * u + 1], s);
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      x[4 * h + e] = full || t0 + e < cnt[h] ? fmaf(s[e], scale_log2, (float)(ve[h] >> 8)) : kNegInf;
+    for (int e = 0; e < 4; ++e) x[4 * h + e] = full || t0 + e < cnt[h] ? s[e] * scale_log2 : kNegInf;
   }
   float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
   mx = half_swap_max(row_swap_max(mx));
@@ -156,18 +148,15 @@ __device__ __forceinline__ void kv8_pair(Kv8State<DH>& S, const Kv8Pair<DH>& R, 
 #pragma unroll
     for (int n = 0; n < DH / 16; ++n) S.acc[n] *= alpha;
   }
-  float p[8], sum[2];
+  float p[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(x[e] - S.m);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    sum[h] = (p[4 * h] + p[4 * h + 1]) + (p[4 * h + 2] + p[4 * h + 3]);
-    S.l = fmaf(sum[h], power_of_two(-(ve[h] >> 8)), S.l);
+  for (int e = 0; e < 8; ++e) {
+    p[e] = __builtin_amdgcn_exp2f(x[e] - S.m);
+    S.l += p[e];
   }
   // the weights of the product with V are rounded to fp16, the denominator's are not
   const f16x8 pf =
       as_f16x8(make_uint4(pack_h2(p[0], p[1]), pack_h2(p[2], p[3]), pack_h2(p[4], p[5]), pack_h2(p[6], p[7])));
-  const float shift[2] = {power_of_two(-(ve[0] & 255)), power_of_two(-(ve[1] & 255))};
   // places that do not count may hold NaN codes, and zero times NaN is NaN
   const uint32_t keep[2] = {full ? ~0u : keep_bytes(cnt[0] - t0), full ? ~0u : keep_bytes(cnt[1] - t0)};
 #pragma unroll
@@ -176,7 +165,7 @@ __device__ __forceinline__ void kv8_pair(Kv8State<DH>& S, const Kv8Pair<DH>& R, 
     const uint32_t cb[4] = {R.v[1][u].x, R.v[1][u].y, R.v[1][u].z, R.v[1][u].w};
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      const uint2 va = e4m3x4_to_f16(ca[n] & keep[0], shift[0]), vb = e4m3x4_to_f16(cb[n] & keep[1], shift[1]);
+      const uint2 va = e4m3x4_to_f16(ca[n] & keep[0], vs[0]), vb = e4m3x4_to_f16(cb[n] & keep[1], vs[1]);
       S.acc[4 * u + n] = mfma16x16x32(as_f16x8(make_uint4(va.x, va.y, vb.x, vb.y)), pf, S.acc[4 * u + n]);
     }
   }
@@ -230,19 +219,21 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
   const float* vsp = a.pool.vs + kvh * a.pool.n_blocks;
   // Tables of 64 pages, one page a lane: the numbers of the pages being loaded and of the 64 after them, and the
   // scales of the pages being loaded and of those being multiplied.  A scale of 0 marks an entry that is no page.
-  auto entries = [&](int r0) { return r0 + lane < np ? bt[r0 + lane] : 0; };
+  auto entries = [&](int r0) { return r0 + lane < np ? bt[r0 + lane] : -1; };
   int blk = entries(0), blk_next = entries(kWave);
-  float ks_next;
-  int ve_next;
+  float ks_next, vs_next;
+  int e_next = kNoExp;   // E of the tables being loaded; of those multiplied: e_now
   auto scales = [&]() {
     const bool there = (uint32_t)blk < (uint64_t)a.pool.n_blocks;
     if (!there) blk = 0;
     ks_next = there ? ksp[blk] : 0.f;
-    ve_next = v_exponent(vsp[blk], there);
+    const int e = there ? exponent_of(vsp[blk]) : kNoExp;
+    e_next = max(e_next, wave_max(e));
+    vs_next = power_of_two(e - e_next);
   };
   scales();
-  float ks_now = ks_next;
-  int ve_now = ve_next;
+  float ks_now = ks_next, vs_now = vs_next;
+  int e_now = e_next;
   Kv8State<DH> S;
 #pragma unroll
   for (int i = 0; i < DH / 16; ++i) S.acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -267,19 +258,25 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
   auto multiply = [&](const Kv8Pair<DH>& P, int r) __attribute__((always_inline)) {
     if (r && r % kWave == 0) {
       ks_now = ks_next;
-      ve_now = ve_next;
+      vs_now = vs_next;
+      if (e_now != e_next) {
+        const float f = power_of_two(e_now - e_next);
+#pragma unroll
+        for (int i = 0; i < DH / 16; ++i) S.acc[i] *= f;
+        e_now = e_next;
+      }
     }
-    float ks[2];
-    int ve[2], cnt[2];
+    float ks[2], vs[2];
+    int cnt[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int s = __builtin_amdgcn_readlane(__float_as_int(ks_now), r % kWave + h);
       const bool there = s != 0 && r + h < np;
       ks[h] = there ? __int_as_float(s) : 1.f;
-      ve[h] = there ? __builtin_amdgcn_readlane(ve_now, r % kWave + h) : 0;
+      vs[h] = there ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs_now), r % kWave + h)) : 1.f;
       cnt[h] = there ? min(kPage, n - (p0 + r + h) * kPage) : 0;
     }
-    kv8_pair<DH>(S, P, qf, ks, ve, cnt, a.scale_log2, lane);
+    kv8_pair<DH>(S, P, qf, ks, vs, cnt, a.scale_log2, lane);
   };
   static_for<NB - 1>([&](auto ic) {
     constexpr int J = decltype(ic)::value;
@@ -299,8 +296,9 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
   S.l += __shfl_xor(S.l, 32, kWave);
   if (!ok) return;
   // the lane's dimensions are u*64 + 16*rq + 4e + n: 16 successive ones for each u
+  const float unit = power_of_two(max(e_now, -126));
   if (n_parts == 1) {
-    const float inv = S.l == 0.f ? 0.f : 1.f / S.l;
+    const float inv = S.l == 0.f ? 0.f : unit / S.l;
     uint16_t* o = a.out + b * a.out_stride + (kvh * G + col) * DH + rq * 16;
 #pragma unroll
     for (int u = 0; u < DH / 64; ++u) {
@@ -322,7 +320,8 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       *reinterpret_cast<float4*>(o + u * 64 + 4 * e) =
-          make_float4(S.acc[4 * u][e], S.acc[4 * u + 1][e], S.acc[4 * u + 2][e], S.acc[4 * u + 3][e]);
+          make_float4(S.acc[4 * u][e] * unit, S.acc[4 * u + 1][e] * unit, S.acc[4 * u + 2][e] * unit,
+                      S.acc[4 * u + 3][e] * unit);
   if (rq == 0) reinterpret_cast<float2*>(a.ws + a.ws_ml)[slot] = make_float2(S.m, S.l);
 }
 
@@ -702,7 +701,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
 // Causal attention of a unit and kv-head, as the bf16 cache's prefill kernel computes it: the (query, head) pairs
 // of the block are the columns of
 //   S^T[32 keys x 32 pairs] = K[32 x dh] . Q^T[dh x 32]       (v_mfma_f32_32x32x16_bf16)
-//   O^T[32 dims x 32 pairs] += V^T[32 x 32 keys] . P^T[32 x 32]   (in fp16, see v_exponent)
+//   O^T[32 dims x 32 pairs] += V^T[32 x 32 keys] . P^T[32 x 32]   (in fp16)
 // with 32 pairs per wavefront.  Every wavefront multiplies every key, so a tile of 32 keys is converted once
 // for the workgroup, on its way into LDS: a thread loads DH/8 bytes of K and of V, two tiles ahead, into registers,
 // and writes them, K as exact bf16 (the page's power of two is applied by the conversion), V's codes as exact fp16, in
@@ -762,14 +761,16 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   // tile's entries would leave no LDS read's wait without theirs.)
   auto entries = [&](int r0) { return bt[min(tbase * 2 + r0 + lane, last_page)]; };
   int blk = 0, blk_next = 0;
-  float ks_next = 0.f, ks_now = 0.f;
-  int ve_next = 0, ve_now = 0;
+  float ks_next = 0.f, vs_next = 0.f, ks_now = 0.f, vs_now = 0.f;
+  int e_next = kNoExp, e_now = kNoExp;   // E of the tables being loaded, and of the tiles being multiplied
   auto scales = [&]() {
     const bool there = (uint32_t)blk < (uint32_t)a.pool.n_blocks;
     blk = there ? blk : 0;
     const float ks = ksp[blk], vs = vsp[blk];
     ks_next = there ? ks : 0.f;
-    ve_next = v_exponent(vs, there);
+    const int e = there ? exponent_of(vs) : kNoExp;
+    e_next = max(e_next, wave_max(e));
+    vs_next = power_of_two(e - e_next);
   };
   // before K of tile t, a multiple of 32, is loaded; before K of any tile t is stored
   auto turn_loads = [&](int t) __attribute__((always_inline)) {
@@ -780,13 +781,13 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   auto turn_stores = [&](int t) __attribute__((always_inline)) {
     if ((t & 31) == 0) {
       ks_now = ks_next;
-      ve_now = ve_next;
+      vs_now = vs_next;
     }
   };
   // V of a tile is loaded and stored a step after its K, with the page and the scale that K looked up
   typedef uint32_t words_t[DH / 32];
   int e_last = 0, keep_lo = 0, keep_hi = 0;
-  float shift_last = 1.f;
+  float vs_last = 1.f;
   // (one buffer descriptor for each page: scalar work only, and the pools may exceed 4 GiB)
   auto page_rsrc = [&](const uint8_t* pool) __attribute__((always_inline)) {
     return make_rsrc(pool + kv_tile(kvh, a.pool.n_blocks, __builtin_amdgcn_readfirstlane(e_last), DH), kPage * DH);
@@ -824,14 +825,13 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
 #pragma unroll
     for (int c = 0; c < DH / 64; ++c) {
       const int row = v_row(lane * (DH / 64) + c);
-      const uint2 lo = e4m3x4_to_f16(R[c] & keep_lo, shift_last), hi = e4m3x4_to_f16(R[DH / 64 + c] & keep_hi, shift_last);
+      const uint2 lo = e4m3x4_to_f16(R[c] & keep_lo, vs_last), hi = e4m3x4_to_f16(R[DH / 64 + c] & keep_hi, vs_last);
       *reinterpret_cast<uint4*>(base + (pg * DH + row) * 16 + v_half(row, hw) * 8) = make_uint4(lo.x, lo.y, hi.x, hi.y);
     }
   };
   // scales and masks of tile t, before its K is stored (in a step: ahead of the matrix work, which waits for nothing
   // scalar then)
-  float ks_here = 1.f, shift_here = 1.f;
-  int e_now = 0, e_next = 0, e_after = 0;   // V exponents of the tile multiplied and of the two after it: of its pages, 16 bits each
+  float ks_here = 1.f, vs_here = 1.f;
   int lo_here = 0, hi_here = 0;
   auto look_up = [&](int t) __attribute__((always_inline)) {
     const int r = (t & 31) * 2;
@@ -842,18 +842,14 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     gone = (gone & ~(3u << sh)) | (3u - there0 - there1 * 2) << sh;
     const int sk = pg ? s1 : s0, none = (int)(pg ? there1 : there0) - 1;   // none: all ones where the page is none
     ks_here = __int_as_float(sk | (none & 0x3F800000));
-    const int v0 = __builtin_amdgcn_readlane(ve_now, r), v1 = __builtin_amdgcn_readlane(ve_now, r + 1);
-    shift_here = power_of_two(-((pg ? v1 : v0) & 255));
-    e_now = e_next;
-    e_next = e_after;
-    e_after = (int)((uint32_t)(v0 >> 8) & 0xFFFFu | (uint32_t)(v1 >> 8) << 16);
+    vs_here = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs_now), r + pg));   // (its codes are masked where there is no page)
     // places of V that do not count may hold NaN codes, and zero times NaN is NaN
     const int left = (kend - ((tbase + t) * 32 + pg * kPage + hw * 4)) & ~none;
     lo_here = keep_bytes(left);
     hi_here = keep_bytes(left - 8);
   };
   auto store_k = [&](const words_t& R, bf16_t* base) __attribute__((always_inline)) {
-    shift_last = shift_here;
+    vs_last = vs_here;
     keep_lo = lo_here;
     keep_hi = hi_here;
 #pragma unroll
@@ -884,16 +880,12 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     for (int ks = 0; ks < KS; ++ks) x = mfma32x32x16(kf[ks], qf[ks], x);
     return x;
   };
-  // largest x + e of the pair; e: the exponents of the tile's pages (rows r < 8 and r >= 8 of the accumulator)
-  auto exp_of = [](int e, int page) __attribute__((always_inline)) { return page ? e >> 16 : (int)(int16_t)e; };
-  auto score_max = [&](const f32x16& x, int e) __attribute__((always_inline)) {
-    float v = x[0], u = x[8];
+  // largest scaled score of the pair (the scale is positive)
+  auto score_max = [&](const f32x16& x) __attribute__((always_inline)) {
+    float v = x[0];
 #pragma unroll
-    for (int r = 1; r < 8; ++r) {
-      v = fmaxf(v, x[r]);
-      u = fmaxf(u, x[8 + r]);
-    }
-    return half_swap_max(fmaxf(fmaf(v, a.scale_log2, (float)exp_of(e, 0)), fmaf(u, a.scale_log2, (float)exp_of(e, 1))));
+    for (int r = 1; r < 16; ++r) v = fmaxf(v, x[r]);
+    return half_swap_max(v) * a.scale_log2;
   };
   // the mask of a tile that needs one, then the reference
   auto settle = [&](f32x16& x, float& mx, int t) __attribute__((always_inline)) {
@@ -905,7 +897,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
         const int key = k0 + (r >> 2) * 8 + h * 4 + (r & 3);
         if (key > qpos || key >= kend || (miss >> (r >> 3) & 1)) x[r] = kNegInf;
       }
-      mx = score_max(x, e_now);
+      mx = score_max(x);
     }
     if (__any(mx > m + kRefRange)) {
       const float m_new = fmaxf(m, mx - kRefBelow);
@@ -927,16 +919,14 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   };
   f16x8 pf[2];
   auto probs = [&](const f32x16& x) __attribute__((always_inline)) {
-    const float c[2] = {(float)exp_of(e_now, 0) - m, (float)exp_of(e_now, 1) - m};
-    float ps[2] = {0.f, 0.f};
+    float ps = 0.f;
     float pv[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      pv[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale_log2, c[r >> 3]));
-      ps[r >> 3] += pv[r];
+      pv[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale_log2, -m));
+      ps += pv[r];
     }
-    l = fmaf(ps[0], power_of_two(-exp_of(e_now, 0)), l);
-    l = fmaf(ps[1], power_of_two(-exp_of(e_now, 1)), l);
+    l += ps;
     // the weights of the product with V are rounded to fp16, the denominator's are not
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
@@ -1002,7 +992,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     __syncthreads();
     read_k(K0);
     f32x16 s = scores();
-    float mx = score_max(s, e_next);   // (look_up has gone as far as tile 1)
+    float mx = score_max(s);
     __syncthreads();
     // a step: V of tile t + 1 and K of t + 2 into LDS, V of t + 3 and K of t + 4 on their way, scores of t + 1, output of t.
     // Past the last tile it moves and scores the last page again, which nothing uses: no step has a branch around
@@ -1011,6 +1001,14 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
         __attribute__((always_inline)) {
       turn_stores(t + 2);
       look_up(t + 2);
+      if ((t & 31) == 0 && e_now != e_next) {   // (t + 4 is no multiple of 32: e_next is that of tile t's table)
+        const float f = power_of_two(e_now - e_next);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[dt][e] *= f;
+        e_now = e_next;
+      }
       settle(s, mx, t);
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(1);   // over the other workgroup's wavefront while that moves tiles
@@ -1021,7 +1019,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
       accumulate();
       store_v(rv, v_next);
       store_k(rk, k_now);
-      mx = score_max(next, e_next);
+      mx = score_max(next);
       s = next;
       interleave();
       __builtin_amdgcn_sched_barrier(0);
@@ -1046,6 +1044,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
 
   const float lt = l + __shfl_xor(l, 32, kWave);
   if (!pair_ok) return;
+  const float unit = power_of_two(max(e_now, -126));
   if (it.slot >= 0) {
     const size_t slot = ((size_t)kvh * p.slots + it.slot) * kPrefillPairs + pair;
     float* po = p.part_o + slot * DH;
@@ -1054,11 +1053,11 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
 #pragma unroll
       for (int g4 = 0; g4 < 4; ++g4)
         *reinterpret_cast<float4*>(po + dt * 32 + g4 * 8 + h * 4) =
-            make_float4(o[dt][g4 * 4], o[dt][g4 * 4 + 1], o[dt][g4 * 4 + 2], o[dt][g4 * 4 + 3]);
+            make_float4(o[dt][g4 * 4] * unit, o[dt][g4 * 4 + 1] * unit, o[dt][g4 * 4 + 2] * unit, o[dt][g4 * 4 + 3] * unit);
     if (h == 0) *reinterpret_cast<float2*>(p.part_ml + slot * 2) = make_float2(m, lt);
     return;
   }
-  const float inv = lt == 0.f ? 0.f : 1.f / lt;
+  const float inv = lt == 0.f ? 0.f : unit / lt;
   uint16_t* out = a.out + row * a.out_stride + col0;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)

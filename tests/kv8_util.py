@@ -185,14 +185,14 @@ def attend(q, cache, blocks, n, hq, first=None):
         w /= w.sum(-1, keepdims=True)
         v = np.where(there[:, None], v, 0)
         out[:, h * G:(h + 1) * G] = w @ v
-        # weights in fp16: 2^-11 of each, or, where it is less than 2^-14, 2^-25 of a unit of which the largest weight
-        # is 2^7 or more.  A weight is p 2^e with e its page's exponent (no less than -60), its partner v 2^-e:
-        # the second kind sums to at most 2^-32 (p_j 2^e_j) sum |v| 2^-e, j the key of the largest p 2^e.
-        e = np.maximum(np.log2(np.repeat(cache.scale["v"][h, at], PAGE)[:n].astype(np.float64)), -60)
-        e = np.where(there, e, 0)
-        j = np.argmax(np.where(seen[:, None], x * np.log2(np.e) + e, -np.inf), -1)
-        top = np.take_along_axis(w, j[..., None], -1) * np.exp2(e)[j][..., None]
-        floor = 2.0 ** -32 * top * ((seen[:, None] * np.exp2(-e)) @ np.abs(v))
+        # Weights in fp16: off by 2^-11 of each, or, under 2^-14, by 2^-25, where the largest weight is 2^7 or more; so
+        # the second kind by 2^-32 p_j of the normalised ones, p_j the largest: 2^-32 p_j sum |v| in all.
+        # V in fp16, in units of the largest page scale 2^E: exact for scales from 2^-15 of it on (codes are
+        # multiples of 2^-9, fp16's subnormals of 2^-24), otherwise off by 2^-25 2^E, which the weights average.
+        floor = 2.0 ** -32 * w.max(-1, keepdims=True) * (seen[:, None].astype(np.float64) @ np.abs(v))
+        scales = cache.scale["v"][h, at].astype(np.float64)
+        if scales.min() < 2.0 ** -15 * scales.max():
+            floor += 2.0 ** -25 * scales.max()
         size[:, h * G:(h + 1) * G] = (2.0 ** -11 + 2.0 ** -11) * (w @ np.abs(v)) + floor
     return out, size
 
