@@ -215,8 +215,9 @@ int hxf_op_rope_kv8_write(const void* qkv, int64_t qkv_stride, const int32_t* po
  * head_dim), attends to positions [0, ctx[b]) (ctx on the device, taken as in [0, 16 bt_stride]) through
  * bt [B, bt_stride]; out bf16 rows of out_stride elements.  ctx 0 (an empty place of a padded batch):
  * zeros.  Tokens of a block-table entry that is no page of the pool are not read and have no weight.  Entries past
- * the context are not read.  workspace: hxf_op_decode_attention_kv8_workspace_bytes bytes, 16-byte aligned, whose
- * contents need not be kept between calls; calls that may overlap need one each. */
+ * the context are not read.  q, out, the pool and the workspace must not overlap.  workspace:
+ * hxf_op_decode_attention_kv8_workspace_bytes bytes, 16-byte aligned, whose contents need not be kept between
+ * calls; calls that may overlap need one each. */
 int64_t hxf_op_decode_attention_kv8_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t head_dim);
 int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_pool* pool, const int32_t* bt,
                                 int32_t bt_stride, const int32_t* ctx, void* out, int64_t out_stride, int32_t B,
@@ -227,7 +228,8 @@ int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_p
  * (row0 [S+1] ascending, on the device, as hxf_op_slot_map makes it; taken as in [0, T]) at positions
  * pos0[s], pos0[s]+1, ... (pos0 on the device); each attends to the positions up to its own through bt[s],
  * whose keys are in the cache already.  Rows of no sequence are left as they are in out.  Positions from
- * 16 bt_stride on are not in the cache: no key there is seen.  Bad entries, strides and workspace as for
+ * 16 bt_stride on are not in the cache: no key there is seen.  NaN in the cache (a value that
+ * was not finite) reaches the queries that see it and no other.  Bad entries, strides and workspace as for
  * hxf_op_decode_attention_kv8. */
 int64_t hxf_op_prefill_attention_kv8_workspace_bytes(int32_t S, int32_t T, int32_t Hq, int32_t Hkv, int32_t head_dim);
 int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_pool* pool, const int32_t* bt,

@@ -7,6 +7,7 @@ namespace hxf {
 namespace {
 
 constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kLowest = -3.0e38f;   // a reference before any score: finite, so that a column without keys keeps zero weights
 
 constexpr int kKv8DecodeScan = 128;
 
@@ -109,6 +110,7 @@ constexpr float kRefBelow = 7.f, kRefRange = 15.f;
 constexpr int kNoExp = -127;   // exponent of an entry that is no page
 __device__ __forceinline__ int exponent_of(float scale) { return (int)(__float_as_uint(scale) >> 23 & 255) - 127; }
 __device__ __forceinline__ float power_of_two(int e) { return e < -126 ? 0.f : __int_as_float((127 + e) << 23); }
+
 template <int DH>
 struct Kv8State {
   f32x4 acc[DH / 16];   // tile (u, n): row r of the lane's column is dimension u*64 + r*4 + n
@@ -237,7 +239,7 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
   Kv8State<DH> S;
 #pragma unroll
   for (int i = 0; i < DH / 16; ++i) S.acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  S.m = -1e30f;   // finite, so that a column without keys keeps zero weights
+  S.m = kLowest;
   S.l = 0.f;
   // Pairs of pages in registers: one multiplied, one on its way.  A third takes the registers of a third wavefront
   // on the SIMD, whose loads hide more: 128 contexts of 1.5-3k tokens, 32 + 8 heads, 109 us against 118, 97 of
@@ -336,17 +338,16 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
   for (int i = lane * 8; i < a.Hq * DH; i += 64 * 8) *reinterpret_cast<uint4*>(out + i) = make_uint4(0, 0, 0, 0);
 }
 
-// Joins the parts of a sequence's heads, H (4 or 1) heads a workgroup.  A thread owns
-// four dimensions and every R-th part, four of them in flight, with a running maximum.  With four heads and up to
-// kMergeAlone parts each wavefront joins a head of its own; otherwise the workgroup takes its heads in turn and its
-// streams meet in LDS.  H is 1 where four heads a workgroup would leave CUs without one and the
-// tables are long enough for more parts than that.  64 sequences of up to 11
-// parts: 4.7 us (H = 1: 7.7); a lone context of 64 parts: 4.7 us with H = 1, 9.5 with 4, 17.2 with a wavefront for
-// each head.
+// Joins the parts of a sequence's heads, H (4 or 1) heads a workgroup.  A thread owns four dimensions and every R-th
+// part, four of them in flight, with a running maximum.  With four heads and up to kMergeAlone parts each wavefront joins
+// a head of its own; otherwise the workgroup takes its heads in turn and its streams meet in LDS.  H is 1 where four
+// heads a workgroup would leave CUs without one and the tables are long enough for more parts than that.  64 sequences
+// of up to 11 parts: 4.7 us (H = 1: 7.7); a lone context of 64 parts: 4.7 us with H = 1, 9.5 with 4, 17.2 with a
+// wavefront for each head.
 constexpr int kMergeAlone = 16;
 template <int DH>
 struct MergeState {
-  float M = -1e30f, L = 0.f;
+  float M = kLowest, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   __device__ __forceinline__ void fold(float2 v, float4 x) {
     const float m = fmaxf(M, v.x);
@@ -441,9 +442,8 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a) {
 
 // ------------------------------------------------------------------ prefill
 // One block of queries of a sequence (up to 128 / G of them), or one part of its keys: rows [row, row + nq) at positions
-// pos .. over the key tiles [t0, t1) of 32 positions, an even
-// number of them.  slot < 0: the whole block, whose output it writes; otherwise the
-// partial slot.  Every kv-head runs the same units.
+// pos .. over the key tiles [t0, t1) of 32 positions, an even number of them.  slot < 0: the whole block, whose output it
+// writes; otherwise the partial slot.  Every kv-head runs the same units.
 struct PrefillUnit {
   int32_t seq, row, nq, pos;
   int32_t t0, t1, slot, pad;
@@ -702,11 +702,15 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
 // of the block are the columns of
 //   S^T[32 keys x 32 pairs] = K[32 x dh] . Q^T[dh x 32]       (v_mfma_f32_32x32x16_bf16)
 //   O^T[32 dims x 32 pairs] += V^T[32 x 32 keys] . P^T[32 x 32]   (in fp16)
-// with 32 pairs per wavefront.  Every wavefront multiplies every key, so a tile of 32 keys is converted once
-// for the workgroup, on its way into LDS: a thread loads DH/8 bytes of K and of V, two tiles ahead, into registers,
-// and writes them, K as exact bf16 (the page's power of two is applied by the conversion), V's codes as exact fp16, in
-// the order of the matrix operands.  A step multiplies K of tile t + 1 and V of tile t, so that the scores of the next tile and the
+// with 32 pairs per wavefront.  Every wavefront multiplies every key, so a tile of 32 keys is converted once for the
+// workgroup, on its way into LDS: a thread loads DH/8 bytes of K and of V, two tiles ahead, into registers, and writes
+// them, K as exact bf16 (the page's power of two is applied by the conversion), V's codes as fp16, in the order of the
+// matrix operands.  A step multiplies K of tile t + 1 and V of tile t, so that the scores of the next tile and the
 // exponentials of this one run side by side; the conversions run beside the product with V.
+//
+// What bounds it: at 6144 + 2048 the power limit and the wavefronts' waits (MFMA busy 41% of the cycles, LDS ports 31%);
+// 2048 queries there 251 us, 0.96 PFLOP/s, as the bf16 cache's kernel.  17 queries over 30k keys: 27 us,
+// 2.3 TB/s, of which four are the plan and the first loads.
 template <int DH, bool SMALL>
 __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   constexpr int KS = DH / 16;      // 16-dim steps of QK^T
@@ -754,7 +758,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   // What this thread moves of a tile: page pg of its two, half hw of the page's K chunks, and of V the groups of four
   // tokens hw and hw + 2 (the order in which the keys of the P^T operand lie) of DH/64 dimensions.
   const int pg = w >> 1, hw = w & 1;
-  const int k_src = hw * (DH * 8) + lane * (DH / 8);
+  const int k_src = hw * (DH * 8) + (DH == 128 ? lane * 16 : (lane >> 5) * 256 + (lane & 15) * 16 + (lane >> 4 & 1) * 8);
   const int v_src = (hw * DH + lane * (DH / 64)) * 4;
   // Tables of 64 pages (32 tiles), one page a lane: the pages being loaded and the 64 after them, and the scales of the
   // pages being loaded and of those being stored.  A scale of 0 marks an entry that is no page.  (Scalar loads of each
@@ -815,12 +819,12 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   };
   uint32_t gone = 0;   // two bits for each of the last 16 tiles stored: its pages that are no page of the pool
   // K: DH/64 chunks of 8 dimensions of one token; V: 8 positions of DH/64 dimensions.  Among 32 dimensions of V the even
-  // ones come first, and the halves of rows change places by bits 3 and 4 of the row, so that the 16 lanes of a read
-  // (successive dimensions) and of a write (every second one at dh 128) hit distinct banks.
+  // ones come first, and the halves of rows change places by bits 2 and 4 of the row, so that the 16 lanes of a read
+  // (successive dimensions, 64 banks) and the 8 of a write (every second one at dh 128, 32 banks) hit distinct banks.
   auto v_row = [](int d) { return (d & ~31) | (d >> 1 & 15) | (d & 1) << 4; };
-  auto v_half = [](int row, int half) { return half ^ (row >> 3 & 1) ^ (row >> 4 & 1); };
+  auto v_half = [](int row, int half) { return half ^ (row >> 2 & 1) ^ (row >> 4 & 1); };
   const int k_dst = pg * (KT / 2) + (DH == 128 ? ((hw * 8 + (lane >> 4) * 2) * 16 + (lane & 15)) * 8
-                                               : ((hw * 4 + (lane >> 5) * 2 + (lane & 1)) * 16 + ((lane & 31) >> 1)) * 8);
+                                               : ((hw * 4 + (lane >> 4)) * 16 + (lane & 15)) * 8);
   auto store_v = [&](const words_t& R, bf16_t* base) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < DH / 64; ++c) {
@@ -864,7 +868,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
-  float m = -1e30f, l = 0.f;   // finite, so that a fully masked pair keeps zero weights
+  float m = kLowest, l = 0.f;
   const int k_off = ((lane & 31) >> 4) * (KT / 2) + (lane & 15) * 8 + h * 128;
   const int v_off = v_row(lane & 31) * 16 + v_half(v_row(lane & 31), h) * 8;
   bf16x8 kf[KS];
@@ -887,8 +891,45 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     for (int r = 1; r < 16; ++r) v = fmaxf(v, x[r]);
     return half_swap_max(v) * a.scale_log2;
   };
+  // V of a tile that some pairs see in part, NaN in it: a weight of zero would spread it to pairs that do not see its
+  // key.  So the tile's NaN become zeros in LDS, and infinities are added where a pair sees one, as
+  //   (2 where V is NaN)^T . (2^127 where the key is seen),
+  // which the end turns into NaN: nothing else in the outputs is infinite.
+  // Every wavefront looks at the whole tile, so all of them take the branch with the barriers, or none.  (V's codes are
+  // at most 448 in fp16, whose two highest exponent bits are set together in NaN alone.)  The look costs 1% of the time
+  // at 6144 + 2048, 2% for chunks of 5 to 256 queries over 4000 keys; one at the codes on their way into LDS, a step
+  // ahead, cost 3% and 6%.
+  auto nan_bits = [](uint32_t x) { return x & x << 1 & 0x40004000u; };   // (as bf16: 2)
+  auto spread_nan = [&](bf16_t* base, int k0, uint32_t miss) __attribute__((always_inline)) {
+    uint32_t any = 0;
+    const uint4* words = reinterpret_cast<const uint4*>(base) + lane;
+#pragma unroll 2
+    for (int i = 0; i < KT / 8; i += kWave)
+      any |= nan_bits(words[i].x) | nan_bits(words[i].y) | nan_bits(words[i].z) | nan_bits(words[i].w);
+    if (!__any(any != 0)) return;
+    bf16x8 seen[2];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = k0 + (r >> 2) * 8 + h * 4 + (r & 3);
+      seen[r >> 3][r & 7] = key > qpos || key >= kend || (miss >> (r >> 3) & 1) ? (__bf16)0.f : (__bf16)0x1p127f;
+    }
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const uint4 v = *reinterpret_cast<const uint4*>(base + v_off + (st * DH + dt * 32) * 16);
+        const uint4 n = make_uint4(nan_bits(v.x), nan_bits(v.y), nan_bits(v.z), nan_bits(v.w));
+        o[dt] = mfma32x32x16(as_bf16x8(n), seen[st], o[dt]);
+      }
+    __syncthreads();
+    for (int i = threadIdx.x; i < KT / 2; i += 256) {
+      const uint32_t x = reinterpret_cast<uint32_t*>(base)[i];
+      reinterpret_cast<uint32_t*>(base)[i] = x & ~((nan_bits(x) >> 14) * 0xFFFFu);
+    }
+    __syncthreads();
+  };
   // the mask of a tile that needs one, then the reference
-  auto settle = [&](f32x16& x, float& mx, int t) __attribute__((always_inline)) {
+  auto settle = [&](f32x16& x, float& mx, bf16_t* v_now, int t) __attribute__((always_inline)) {
     const int k0 = (tbase + t) * 32;
     const uint32_t miss = gone >> ((t & 15) * 2) & 3;
     if (k0 + 32 > kend || k0 + 31 > it.pos || miss) {
@@ -898,6 +939,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
         if (key > qpos || key >= kend || (miss >> (r >> 3) & 1)) x[r] = kNegInf;
       }
       mx = score_max(x);
+      spread_nan(v_now, k0, miss);
     }
     if (__any(mx > m + kRefRange)) {
       const float m_new = fmaxf(m, mx - kRefBelow);
@@ -963,10 +1005,6 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   };
 
   if (ntiles > 0) {
-    // Past the last tile a step moves and scores the last one again, which nothing uses: no step has a branch, so
-    // the loads in flight stay counted.
-    // Past the last tile a step moves and scores the last page again, which nothing uses: no step has a branch around
-    // its loads, so that those in flight stay counted.
     words_t RK0, RK1, RV0, RV1;   // tiles on their way: K of two, V of two
     blk_next = entries(0);
     turn_loads(0);
@@ -1009,7 +1047,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
           for (int e = 0; e < 16; ++e) o[dt][e] *= f;
         e_now = e_next;
       }
-      settle(s, mx, t);
+      settle(s, mx, v_now, t);
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(1);   // over the other workgroup's wavefront while that moves tiles
       read_k(k_next);
@@ -1028,7 +1066,6 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
       load_k(rk, t + 4);
       __syncthreads();
     };
-    // (the tables turn outside of the loop over steps, whose loads stay counted)
     // (the tables turn outside of the loop over steps, whose loads stay counted; ntiles is even)
     for (int t = 0;;) {
       const int stop = min(ntiles, ((t + 4) | 31) - 3);   // the next t with t + 4 a multiple of 32
@@ -1042,6 +1079,10 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     }
   }
 
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = fmaf(o[dt][e], 0.f, o[dt][e]);   // infinity to NaN (see spread_nan)
   const float lt = l + __shfl_xor(l, 32, kWave);
   if (!pair_ok) return;
   const float unit = power_of_two(max(e_now, -126));

@@ -1,5 +1,7 @@
 """The operators of the 8-bit KV cache against a plain model in float64 (tests/kv8_util.py): tables and
 codes to the last bit, attention within the roundings it makes."""
+import copy
+
 import numpy as np
 import pytest
 
@@ -521,6 +523,66 @@ def test_prefill_rows_past_the_table_and_row0_out_of_range():
         ref, size = U.attend(qf[r], cache, bt[s], p + r.stop - r.start, 4, first=p)
         U.assert_attention(got[r], ref, size, f"sequence {s}")
     assert np.all(out.cpu().numpy().view(np.uint16).reshape(24, -1)[20:] == 0x1234)
+
+
+def _outputs(cache, bt, pos0, n, hq, rng, decode):
+    """q float64 and outputs of prefill, or of decode (n 1 everywhere), nothing checked."""
+    t = torch()
+    S, T, hkv, dh = len(n), int(np.sum(n)), cache.hkv, cache.dh
+    dev = DevCache(cache)
+    bits, _ = rand_bf16(rng, (T, hq * dh))
+    q, out, d_bt = dev_bits(bits), dev_bits(np.zeros((T, hq * dh), np.uint16)), i32(bt)
+    row0, d_pos0, ctx = i32(np.concatenate([[0], np.cumsum(n)])), i32(pos0), i32(np.add(pos0, n))
+    m = (hxf.op_decode_attention_kv8_workspace_bytes(S, hq, hkv, dh) if decode else
+         hxf.op_prefill_attention_kv8_workspace_bytes(S, T, hq, hkv, dh))
+    ws = t.full((m,), 0xFF, dtype=t.uint8, device="cuda:0")
+    log(f"values that are not finite: {'decode' if decode else 'prefill'} S={S} T={T} {hq}/{hkv}x{dh}")
+    if decode:
+        hxf.op_decode_attention_kv8(q.data_ptr(), hq * dh, dev.pool, d_bt.data_ptr(), bt.shape[1], ctx.data_ptr(),
+                                    out.data_ptr(), hq * dh, S, hq, hkv, dh, ws.data_ptr(), m)
+    else:
+        hxf.op_prefill_attention_kv8(q.data_ptr(), hq * dh, dev.pool, d_bt.data_ptr(), bt.shape[1], row0.data_ptr(),
+                                     d_pos0.data_ptr(), out.data_ptr(), hq * dh, S, T, hq, hkv, dh, ws.data_ptr(), m)
+    t.cuda.synchronize()
+    return U.f32_of(bits).astype(np.float64).reshape(T, hq, dh), host_f64(out).reshape(T, hq, dh)
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(8, 2, 128), (4, 2, 64), (2, 2, 128)])
+@pytest.mark.parametrize("decode", [False, True])
+def test_nan_in_the_cache_reaches_the_queries_that_see_it(hq, hkv, dh, decode):
+    """NaN of V in some dimensions of some places, and one NaN of K: exactly the outputs whose sums hold them are NaN,
+    those of earlier queries of the same block are not."""
+    rng = np.random.default_rng(hq + dh)
+    pos0, n = np.array([100, 0, 2000, 40, 7, 0]), np.array([70, 45, 40, 1, 3, 5])
+    if decode:
+        pos0, n = pos0 + n - 1, np.ones(6, np.int64)
+    cache, bt = _attention_case(rng, pos0 + n, hq, hkv, dh)
+    clean = copy.deepcopy(cache)
+    v_nan, k_nan = [], []       # (sequence, position, head, dimension or None)
+    for s, p, d in ((0, 104, 3), (0, 120, dh - 1), (0, 169, 17), (1, 0, 0), (1, 31, 33), (1, 44, 2), (2, 5, 40), (2, 2001, 41),
+                    (2, 2017, 42), (2, 2039, 43), (4, 9, 1)):
+        h = (p + d) % hkv
+        cache.codes["v"][h, bt[s, p // 16], p % 16, d] = 0x7F if p % 2 else 0xFF
+        v_nan.append((s, p, h, d))
+    for s, p, h in ((0, 150, 0), (1, 20, 1)):
+        cache.codes["k"][h, bt[s, p // 16], p % 16, 5] = 0x7F
+        k_nan.append((s, p, h))
+    q, got = _outputs(cache, bt, pos0, n, hq, rng, decode)
+    G, r0 = hq // hkv, 0
+    for s in range(len(n)):
+        r = slice(r0, r0 + n[s])
+        ref, size = U.attend(q[r], clean, bt[s], int(pos0[s] + n[s]), hq, first=int(pos0[s]))
+        nan = np.zeros(ref.shape, bool)
+        for j, p, h, d in v_nan:
+            if j == s:
+                nan[max(p - pos0[s], 0):, h * G:(h + 1) * G, d] = True
+        for j, p, h in k_nan:
+            if j == s:
+                nan[max(p - pos0[s], 0):, h * G:(h + 1) * G] = True
+        what = f"sequence {s}"
+        assert np.array_equal(np.isnan(got[r]), nan), what
+        U.assert_attention(np.where(nan, 0, got[r]), np.where(nan, 0, ref), size, what)
+        r0 += n[s]
 
 
 def test_prefill_long_blocks_that_are_not_cut():
