@@ -189,8 +189,8 @@ typedef struct hxf_kv8_pool {
  *   status [2]  pages taken, rows
  * All or nothing: when the pages or the T rows do not suffice, a sequence needs more than bt_stride pages,
  * or a length is negative, status is {-1, 0}, bt is left as it is, row0 is 0, ctx is start (0 for a negative one)
- * and every row is {pos 0, slot -1}.  S <= HXF_SLOT_MAP_MAX_SEQS.  All arrays are on the device; the outputs must not
- * overlap the inputs or each other. */
+ * and every row is {pos 0, slot -1}.  S <= HXF_SLOT_MAP_MAX_SEQS, T and
+ * free_cap < 2^30.  All arrays are on the device; the outputs must not overlap the inputs or each other. */
 #define HXF_SLOT_MAP_MAX_SEQS 4096
 int hxf_op_slot_map(const int32_t* start, const int32_t* n_new, int32_t S, const int32_t* free_pages,
                     const int32_t* n_free, int32_t free_cap, int32_t* bt, int32_t bt_stride, int32_t* row0,
@@ -206,7 +206,7 @@ int hxf_op_slot_map(const int32_t* start, const int32_t* n_new, int32_t S, const
  * before them stay: the scale is the larger of the page's and the new rows', and where it grows the old codes
  * are requantised.  Tokens behind the new rows are left as they are.  A row whose slot is not in [0, 16 n_blocks), or
  * (with a table) whose pos is not in [0, max_pos), is skipped, its q_out row included.
- * qkv and q_out 16-byte aligned, strides multiples of 8; no buffer may overlap another. */
+ * qkv and q_out 16-byte aligned, strides multiples of 8, T < 2^30; no buffer may overlap another. */
 int hxf_op_rope_kv8_write(const void* qkv, int64_t qkv_stride, const int32_t* pos, const int32_t* slot,
                           const void* rope_table, int32_t max_pos, void* q_out, int64_t q_stride,
                           const hxf_kv8_pool* pool, int32_t T, int32_t Hq, int32_t Hkv, int32_t head_dim, void* stream);

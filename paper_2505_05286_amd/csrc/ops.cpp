@@ -446,7 +446,8 @@ bool rows_ok(const void* p, int64_t stride, int64_t width) {
   return p && aligned16(p) && stride >= width && stride % 8 == 0;
 }
 
-// (wavefront and grid indices are 32 bits wide)
+// (row, page, wavefront and grid indices are 32 bits wide)
+bool count_ok(int32_t n) { return n >= 0 && n < (1 << 30); }
 bool batch_ok(int64_t n, int Hq) { return n * Hq < (int64_t(1) << 29); }
 
 bool table_ok(const int32_t* bt, int32_t bt_stride) { return bt && bt_stride > 0 && bt_stride < (1 << 26); }
@@ -456,7 +457,7 @@ bool table_ok(const int32_t* bt, int32_t bt_stride) { return bt && bt_stride > 0
 int hxf_op_slot_map(const int32_t* start, const int32_t* n_new, int32_t S, const int32_t* free_pages,
                     const int32_t* n_free, int32_t free_cap, int32_t* bt, int32_t bt_stride, int32_t* row0,
                     int32_t* pos, int32_t* slot, int32_t T, int32_t* ctx, int32_t* status, void* stream) {
-  if (S < 0 || S > HXF_SLOT_MAP_MAX_SEQS || T < 0 || free_cap < 0 || !row0 || !status || !n_free ||
+  if (S < 0 || S > HXF_SLOT_MAP_MAX_SEQS || !count_ok(T) || !count_ok(free_cap) || !row0 || !status || !n_free ||
       (free_cap > 0 && !free_pages) || (T > 0 && (!pos || !slot)))
     return HXF_EINVAL;
   if (S > 0 && (!start || !n_new || !ctx || !table_ok(bt, bt_stride))) return HXF_EINVAL;
@@ -482,7 +483,7 @@ int hxf_op_slot_map(const int32_t* start, const int32_t* n_new, int32_t S, const
 int hxf_op_rope_kv8_write(const void* qkv, int64_t qkv_stride, const int32_t* pos, const int32_t* slot,
                           const void* rope_table, int32_t max_pos, void* q_out, int64_t q_stride,
                           const hxf_kv8_pool* pool, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh, void* stream) {
-  if (T < 0 || !shapes_ok(Hq, Hkv, dh) || !pool_ok(pool) || !slot) return HXF_EINVAL;
+  if (!count_ok(T) || !shapes_ok(Hq, Hkv, dh) || !pool_ok(pool) || !slot) return HXF_EINVAL;
   if (!rows_ok(qkv, qkv_stride, (int64_t)(Hq + 2 * Hkv) * dh) || (q_out && !rows_ok(q_out, q_stride, (int64_t)Hq * dh)))
     return HXF_EINVAL;
   if (rope_table && (!pos || max_pos <= 0 || !aligned16(rope_table))) return HXF_EINVAL;

@@ -67,6 +67,13 @@ def test_write_refuses(bad):
     _refused(hxf.EINVAL, _write, **bad)
 
 
+@pytest.mark.parametrize("f,bad", [(_slot_map, dict(T=1 << 30)), (_slot_map, dict(T=2 ** 31 - 1)),
+                                   (_slot_map, dict(free_cap=1 << 30)), (_slot_map, dict(free_cap=2 ** 31 - 1)),
+                                   (_write, dict(T=1 << 30)), (_write, dict(T=2 ** 31 - 1))])
+def test_counts_whose_indices_would_pass_32_bits_are_refused(f, bad):
+    _refused(hxf.EINVAL, f, **bad)
+
+
 def _decode(**k):
     d = dict(q=A, q_stride=512, pool=_pool(), bt=A, bt_stride=4, ctx=A, out=A, out_stride=512, B=3, Hq=4, Hkv=2,
              dh=128, ws=A, ws_bytes=1 << 40)
