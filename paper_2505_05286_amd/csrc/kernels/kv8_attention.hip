@@ -557,12 +557,12 @@ __device__ __forceinline__ PlanCut plan_cut(PlanLds& lds, const Kv8AttnArgs& a, 
   c.n_jobs = all >> 20;
   return c;
 }
-// Part k of a cut block
-__device__ __forceinline__ void plan_part(PrefillUnit& u, int parts, int slot0, int k) {
+// Part k of a cut block.  (Slots number under `slots` where row0 ascends.)
+__device__ __forceinline__ void plan_part(PrefillUnit& u, int parts, int slot0, int k, int slots) {
   const int len = kv8_prefill_part_tiles(u.t1, parts);
   u.t0 = k * len;
   u.t1 = min(u.t1, u.t0 + len);
-  u.slot = parts > 1 ? slot0 + k : -1;
+  u.slot = parts > 1 ? min(slot0 + k, slots - 1) : -1;
 }
 
 // A batch of up to kPlanThreads sequences and blocks is planned by every workgroup of the kernels that follow for
@@ -577,7 +577,7 @@ struct SmallPlan {
   PrefillJob jobs[JOBS ? kCus : 1];
 };
 template <bool JOBS>
-__device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8AttnArgs& a, int queries, int want) {
+__device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8AttnArgs& a, int queries, int slots, int want) {
   const int tid = threadIdx.x;
   int r0 = 0, total;
   const int rows = tid < a.S ? plan_rows(a, tid, r0) : 0;
@@ -611,7 +611,7 @@ __device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8AttnArg
   if (JOBS) {
     if (c.parts > 1) lds.jobs[JOBS ? c.job : 0] = PrefillJob{u.row, u.nq, c.slot0, c.parts};
   } else if (want >= c.first && want < c.first + c.parts) {
-    plan_part(u, c.parts, c.slot0, want - c.first);
+    plan_part(u, c.parts, c.slot0, want - c.first, slots);
     lds.unit = u;
   }
   __syncthreads();
@@ -689,7 +689,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
   for (int i = tid; i < c.n_units; i += kPlanThreads) {
     const int b = last_at(first, n_blocks, i);
     PrefillUnit u = whole[b];
-    plan_part(u, parts[b], u.slot, i - first[b]);
+    plan_part(u, parts[b], u.slot, i - first[b], p.slots);
     p.units[i] = u;
   }
   if (tid == 0) {
@@ -724,7 +724,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   PrefillUnit it;
   if constexpr (SMALL) {
     __shared__ SmallPlan<false> plan;
-    if (ui >= plan_small(plan, a, p.qpi, ui)) return;
+    if (ui >= plan_small(plan, a, p.qpi, p.slots, ui)) return;
     // (what came through LDS is wavefront-uniform)
     const int32_t* u = reinterpret_cast<const int32_t*>(&plan.unit);
     int32_t* v = reinterpret_cast<int32_t*>(&it);
@@ -1122,13 +1122,13 @@ __global__ __launch_bounds__(256) void kv8_prefill_merge_kernel(Kv8PrefillArgs p
   __shared__ float4 s_acc[P][R][C];
   __shared__ SmallPlan<true> plan;
   constexpr int GROUPS = kPrefillPairs / P;
-  const int n_jobs = SMALL ? plan_small(plan, a, p.qpi, 0) : p.head->n_jobs;
+  const int n_jobs = SMALL ? plan_small(plan, a, p.qpi, p.slots, 0) : p.head->n_jobs;
   const int items = n_jobs * a.Hkv * GROUPS;
   for (int i = blockIdx.x; i < items; i += gridDim.x) {
     const int job = i / GROUPS, jb = job / a.Hkv, kvh = job - jb * a.Hkv;
     const PrefillJob mg = SMALL ? plan.jobs[jb] : p.jobs[jb];
     const int pair0 = i % GROUPS * P;
-    if (pair0 >= mg.nq * G) continue;   // (uniform over the workgroup)
+    if (pair0 >= mg.nq * G || mg.slot0 + mg.n_part > p.slots) continue;   // (uniform over the workgroup)
     const int pair = pair0 + pl;        // a pair past the block's: its slot exists, its row is not written
     const size_t slot = ((size_t)kvh * p.slots + mg.slot0) * kPrefillPairs + pair;
     MergeState<DH> S;

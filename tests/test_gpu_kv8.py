@@ -525,6 +525,28 @@ def test_prefill_rows_past_the_table_and_row0_out_of_range():
     assert np.all(out.cpu().numpy().view(np.uint16).reshape(24, -1)[20:] == 0x1234)
 
 
+@pytest.mark.parametrize("S,T", [(10, 256), (401, 256), (3, 64)])
+def test_prefill_row0_that_does_not_ascend_stays_in_its_buffers(S, T):
+    """More rows than T in all, over contexts long enough to be cut: nothing is written past the workspace or out."""
+    t = torch()
+    rng = np.random.default_rng(S)
+    cache, bt = _attention_case(rng, [2500] * 2, 16, 1, 64)
+    bt = bt[np.arange(S) % 2]
+    dev = DevCache(cache)
+    row0 = np.zeros(S + 1, np.int64)
+    row0[1:10:2] = T
+    q, d_bt, d_row0, pos0 = dev_bits(rand_bf16(rng, (T, 1024))[0]), i32(bt), i32(row0), i32(np.full(S, 2200))
+    out = dev_bits(np.full((T + 8, 1024), 0x1234, np.uint16))
+    m = hxf.op_prefill_attention_kv8_workspace_bytes(S, T, 16, 1, 64)
+    ws = t.full((m + (16 << 20),), 0x5A, dtype=t.uint8, device="cuda:0")
+    log(f"prefill kv8 row0 that does not ascend: S={S} T={T}")
+    hxf.op_prefill_attention_kv8(q.data_ptr(), 1024, dev.pool, d_bt.data_ptr(), bt.shape[1], d_row0.data_ptr(),
+                                 pos0.data_ptr(), out.data_ptr(), 1024, S, T, 16, 1, 64, ws.data_ptr(), m)
+    t.cuda.synchronize()
+    assert bool((ws[m:] == 0x5A).all())
+    assert np.all(out.cpu().numpy().view(np.uint16)[T:] == 0x1234)
+
+
 def _outputs(cache, bt, pos0, n, hq, rng, decode):
     """q float64 and outputs of prefill, or of decode (n 1 everywhere), nothing checked."""
     t = torch()
