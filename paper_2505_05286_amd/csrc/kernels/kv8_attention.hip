@@ -761,17 +761,20 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   const int k_src = hw * (DH * 8) + (DH == 128 ? lane * 16 : (lane >> 5) * 256 + (lane & 15) * 16 + (lane >> 4 & 1) * 8);
   const int v_src = (hw * DH + lane * (DH / 64)) * 4;
   // Tables of 64 pages (32 tiles), one page a lane: the pages being loaded and the 64 after them, and the scales of the
-  // pages being loaded and of those being stored.  A scale of 0 marks an entry that is no page.  (Scalar loads of each
-  // tile's entries would leave no LDS read's wait without theirs.)
+  // pages being loaded and of those being stored.  (Scalar loads of each tile's entries would leave no LDS read's wait
+  // without theirs.)  An entry that is no page reads page 0, whose keys `settle` masks.
   auto entries = [&](int r0) { return bt[min(tbase * 2 + r0 + lane, last_page)]; };
   int blk = 0, blk_next = 0;
   float ks_next = 0.f, vs_next = 0.f, ks_now = 0.f, vs_now = 0.f;
-  int e_next = kNoExp, e_now = kNoExp;   // E of the tables being loaded, and of the tiles being multiplied
+  // E, and the entries that are no page, of the tables being loaded, and of the tiles being multiplied
+  int e_next = kNoExp, e_now = kNoExp;
+  uint64_t gone_next = 0, gone_now = 0;
   auto scales = [&]() {
     const bool there = (uint32_t)blk < (uint32_t)a.pool.n_blocks;
+    gone_next = __ballot(!there);
     blk = there ? blk : 0;
-    const float ks = ksp[blk], vs = vsp[blk];
-    ks_next = there ? ks : 0.f;
+    const float vs = vsp[blk];
+    ks_next = ksp[blk];
     const int e = there ? exponent_of(vs) : kNoExp;
     e_next = max(e_next, wave_max(e));
     vs_next = power_of_two(e - e_next);
@@ -790,7 +793,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   };
   // V of a tile is loaded and stored a step after its K, with the page and the scale that K looked up
   typedef uint32_t words_t[DH / 32];
-  int e_last = 0, keep_lo = 0, keep_hi = 0;
+  int e_last = 0;
   float vs_last = 1.f;
   // (one buffer descriptor for each page: scalar work only, and the pools may exceed 4 GiB)
   auto page_rsrc = [&](const uint8_t* pool) __attribute__((always_inline)) {
@@ -817,7 +820,6 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
       R[1] = buf_load4(rs, v_src, 8 * DH);
     }
   };
-  uint32_t gone = 0;   // two bits for each of the last 16 tiles stored: its pages that are no page of the pool
   // K: DH/64 chunks of 8 dimensions of one token; V: 8 positions of DH/64 dimensions.  Among 32 dimensions of V the even
   // ones come first, and the halves of rows change places by bits 2 and 4 of the row, so that the 16 lanes of a read
   // (successive dimensions, 64 banks) and the 8 of a write (every second one at dh 128, 32 banks) hit distinct banks.
@@ -829,33 +831,19 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
 #pragma unroll
     for (int c = 0; c < DH / 64; ++c) {
       const int row = v_row(lane * (DH / 64) + c);
-      const uint2 lo = e4m3x4_to_f16(R[c] & keep_lo, vs_last), hi = e4m3x4_to_f16(R[DH / 64 + c] & keep_hi, vs_last);
+      const uint2 lo = e4m3x4_to_f16(R[c], vs_last), hi = e4m3x4_to_f16(R[DH / 64 + c], vs_last);
       *reinterpret_cast<uint4*>(base + (pg * DH + row) * 16 + v_half(row, hw) * 8) = make_uint4(lo.x, lo.y, hi.x, hi.y);
     }
   };
-  // scales and masks of tile t, before its K is stored (in a step: ahead of the matrix work, which waits for nothing
-  // scalar then)
+  // scales of tile t, before its K is stored (in a step: ahead of the matrix work, which waits for nothing scalar then)
   float ks_here = 1.f, vs_here = 1.f;
-  int lo_here = 0, hi_here = 0;
   auto look_up = [&](int t) __attribute__((always_inline)) {
-    const int r = (t & 31) * 2;
-    const int s0 = __builtin_amdgcn_readlane(__float_as_int(ks_now), r), s1 = __builtin_amdgcn_readlane(__float_as_int(ks_now), r + 1);
-    // (selects by arithmetic: branches here would cut the step into pieces that are scheduled apart)
-    const uint32_t there0 = min((uint32_t)s0, 1u), there1 = min((uint32_t)s1, 1u);
-    const int sh = (t & 15) * 2;
-    gone = (gone & ~(3u << sh)) | (3u - there0 - there1 * 2) << sh;
-    const int sk = pg ? s1 : s0, none = (int)(pg ? there1 : there0) - 1;   // none: all ones where the page is none
-    ks_here = __int_as_float(sk | (none & 0x3F800000));
-    vs_here = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs_now), r + pg));   // (its codes are masked where there is no page)
-    // places of V that do not count may hold NaN codes, and zero times NaN is NaN
-    const int left = (kend - ((tbase + t) * 32 + pg * kPage + hw * 4)) & ~none;
-    lo_here = keep_bytes(left);
-    hi_here = keep_bytes(left - 8);
+    const int r = (t & 31) * 2 + pg;
+    ks_here = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ks_now), r));
+    vs_here = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs_now), r));
   };
   auto store_k = [&](const words_t& R, bf16_t* base) __attribute__((always_inline)) {
     vs_last = vs_here;
-    keep_lo = lo_here;
-    keep_hi = hi_here;
 #pragma unroll
     for (int c = 0; c < DH / 64; ++c) {
       const uint2 lo = e4m3x4_to_bf16(R[2 * c], ks_here), hi = e4m3x4_to_bf16(R[2 * c + 1], ks_here);
@@ -891,8 +879,8 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     for (int r = 1; r < 16; ++r) v = fmaxf(v, x[r]);
     return half_swap_max(v) * a.scale_log2;
   };
-  // V of a tile that some pairs see in part, NaN in it: a weight of zero would spread it to pairs that do not see its
-  // key.  So the tile's NaN become zeros in LDS, and infinities are added where a pair sees one, as
+  // NaN in V of a tile with masked keys (one that some pairs see and others do not, or a place past the context, which
+  // may hold anything): a weight of zero would spread it to pairs that do not see its key.  So the tile's NaN become zeros in LDS, and infinities are added where a pair sees one, as
   //   (2 where V is NaN)^T . (2^127 where the key is seen),
   // which the end turns into NaN: nothing else in the outputs is infinite.
   // Every wavefront looks at the whole tile, so all of them take the branch with the barriers, or none.  (V's codes are
@@ -931,7 +919,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   // the mask of a tile that needs one, then the reference
   auto settle = [&](f32x16& x, float& mx, bf16_t* v_now, int t) __attribute__((always_inline)) {
     const int k0 = (tbase + t) * 32;
-    const uint32_t miss = gone >> ((t & 15) * 2) & 3;
+    const uint32_t miss = (uint32_t)(gone_now >> ((t & 31) * 2)) & 3;
     if (k0 + 32 > kend || k0 + 31 > it.pos || miss) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -1039,13 +1027,16 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
         __attribute__((always_inline)) {
       turn_stores(t + 2);
       look_up(t + 2);
-      if ((t & 31) == 0 && e_now != e_next) {   // (t + 4 is no multiple of 32: e_next is that of tile t's table)
-        const float f = power_of_two(e_now - e_next);
+      if ((t & 31) == 0) {   // (t + 4 is no multiple of 32: e_next is that of tile t's table)
+        gone_now = gone_next;
+        if (e_now != e_next) {
+          const float f = power_of_two(e_now - e_next);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+          for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[dt][e] *= f;
-        e_now = e_next;
+            for (int e = 0; e < 16; ++e) o[dt][e] *= f;
+          e_now = e_next;
+        }
       }
       settle(s, mx, v_now, t);
       __builtin_amdgcn_sched_barrier(0);
