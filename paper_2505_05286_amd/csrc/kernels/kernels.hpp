@@ -327,31 +327,56 @@ inline int64_t kv8_decode_items(int64_t n_seqs, int hkv) {
 }
 // Prefill work split, made by a kernel from the rows and positions in device memory.  A block of up to 128 / G queries
 // of a sequence is one unit of work for every kv-head, over its key tiles of 32 positions (taken in pairs).  Where
-// whole blocks would be fewer than the CUs, blocks longer than an even share of all tiles over the resident workgroups
-// are cut into parts of equal length, at least kPrefillMinTiles tiles.
+// whole blocks would be fewer than kPrefillCutUnits, all of a head's pairs, block after block, are dealt out in equal
+// shares to the workgroups resident at once: a block is cut where a share ends, unless it exceeds one by
+// kPrefillMinTiles pairs at most, or the piece would be shorter than kPrefillMinTiles / 4.  32 + 8 heads, us, against
+// equal parts of each block, of no more than a share and so more of them than are resident: 512 queries at 8192 104 / 137,
+// 640 at 9000 140 / 163, 800 at 20000 310 / 402.  With 304 blocks 153 cut, 163 whole; 264 104 / 116; 256 blocks of up to
+// 1500 keys 46 / 44; 352 of 4000 keys 178 / 157, 384 of 8700 265 / 258.
 constexpr int kCus = 256;
-__host__ __device__ inline bool kv8_prefill_cuts(int64_t blocks, int hkv) { return blocks * hkv < kCus; }
-// tiles: no less than the sum of all blocks' tiles
-__host__ __device__ inline int kv8_prefill_share(int64_t tiles, int hkv) {
-  const int64_t t = (tiles * hkv + kPrefillResident - 1) / kPrefillResident;
-  return (int)(t > kPrefillMinTiles ? t : kPrefillMinTiles);
+constexpr int kPrefillCutUnits = 320;
+__host__ __device__ inline bool kv8_prefill_cuts(int64_t blocks, int hkv) {
+  return blocks * hkv < kPrefillCutUnits && blocks <= kCus;   // (a thread plans a block)
 }
-// Parts of a block of `tiles` (even) tiles, at least one; part k is the tiles [k * len, min(tiles, (k + 1) * len))
-__host__ __device__ inline int kv8_prefill_part_tiles(int tiles, int parts) { return (tiles / 2 + parts - 1) / parts * 2; }
-__host__ __device__ inline int kv8_prefill_parts(int tiles, int share) {
-  const int most = (tiles + share - 1) / share;
-  if (most <= 1) return 1;
-  const int len = kv8_prefill_part_tiles(tiles, most);
-  return (tiles + len - 1) / len;
+// Sizes are counted in 2^shift pairs, so that those of all blocks that are cut stay in 32 bits
+__host__ __device__ inline int kv8_prefill_shift(int bt_stride) { return bt_stride >> 24; }
+__host__ __device__ inline uint32_t kv8_prefill_size(int tiles, int shift) {
+  return ((uint32_t)(tiles >> 1) + (1u << shift) - 1) >> shift;
+}
+__host__ __device__ inline int kv8_prefill_streams(int hkv) { return kPrefillResident > hkv ? kPrefillResident / hkv : 1; }
+__host__ __device__ inline uint32_t kv8_prefill_share(uint32_t total, int hkv) {
+  const uint32_t n = (uint32_t)kv8_prefill_streams(hkv), t = total / n + (total % n != 0);
+  return t > kPrefillMinTiles / 2 ? t : kPrefillMinTiles / 2;
+}
+// The block of sizes [at, at + size): its parts (at least one), which begin at 0 and, from part 1 on, where shares
+// cut, cut + 1, ... end
+struct Kv8Cut {
+  uint32_t cut;
+  int parts;
+};
+__host__ __device__ inline Kv8Cut kv8_prefill_cut(uint32_t at, uint32_t size, uint32_t share) {
+  Kv8Cut c{0, 1};
+  if (size <= share + kPrefillMinTiles) return c;
+  uint32_t lo = at / share + 1, hi = (at + size - 1) / share;
+  if (lo * share - at < kPrefillMinTiles / 4) ++lo;
+  if (at + size - hi * share < kPrefillMinTiles / 4) --hi;
+  if (lo > hi) return c;
+  c.cut = lo;
+  c.parts = (int)(hi - lo) + 2;
+  return c;
+}
+// First tile of part k of a block of `tiles` tiles, and of the one after it for k + 1
+__host__ __device__ inline int kv8_prefill_part_tile(Kv8Cut c, uint32_t at, uint32_t share, int shift, int tiles, int k) {
+  return k == 0 ? 0 : k >= c.parts ? tiles : (int)((c.cut + k - 1) * share - at) << (shift + 1);
 }
 // Units that hold any batch of S sequences and T rows, and partial slots of a kv-head: blocks number at most
-// T / q + S; cut ones, over all heads, under kCus blocks and kPrefillResident more parts than blocks.
+// T / q + S; cut ones, over all heads, under kPrefillCutUnits, with a cut for each share but one.
 inline int64_t kv8_prefill_unit_cap(int64_t S, int64_t T, int queries, int hkv) {
-  const int64_t cut = (kCus + kPrefillResident) / hkv, whole = T / queries + S;
+  const int64_t cut = (kPrefillCutUnits + kPrefillResident) / hkv, whole = T / queries + S;
   return (cut > whole ? cut : whole) + 1;
 }
 inline int64_t kv8_prefill_slots(int64_t S, int64_t T, int queries, int hkv) {
-  const int64_t cut = (kCus + kPrefillResident) / hkv, whole = T / queries + S + kPrefillResident / hkv;
+  const int64_t cut = (kPrefillCutUnits + kPrefillResident) / hkv, whole = T / queries + S + kv8_prefill_streams(hkv);
   return (cut < whole ? cut : whole) + 1;
 }
 int64_t kv8_decode_ws_bytes(int B, int Hq, int Hkv, int dh);

@@ -486,7 +486,7 @@ struct Kv8PrefillArgs {
 
 // What the planning kernels share.  kPlanThreads threads, a thread for each block of a batch that is cut.
 constexpr int kPlanThreads = 256;
-static_assert(kPlanThreads >= kCus, "a thread for each block of a batch that is cut");
+static_assert(kPlanThreads == kCus, "a thread for each block of a batch that is cut");
 
 struct PlanLds {
   int32_t sums[kPlanThreads / kWave], pre[kPlanThreads];
@@ -536,33 +536,78 @@ __device__ __forceinline__ PrefillUnit plan_block(const Kv8AttnArgs& a, int quer
   u.pad = 0;
   return u;
 }
-// The cut of a batch of few blocks, whose block threadIdx.x has these tiles (0 for a thread without one)
+// The cut of a batch of few blocks, thread b's being u (past the blocks: with t1 0)
 struct PlanCut {
-  int parts, first, slot0, job;        // of this thread's block: its parts, its first unit, slot and job
+  uint32_t at, share;             // this thread's block: the sizes before it
+  int parts, first, job;          // its parts, their first unit (and partial slot), its job
   int n_units, n_jobs;
 };
-__device__ __forceinline__ PlanCut plan_cut(PlanLds& lds, const Kv8AttnArgs& a, int n_blocks, int tiles) {
-  int halves, all;   // (half the tiles: under 256 blocks of up to 2^25 tiles stay in 32 bits)
-  plan_scan(lds, tiles >> 1, halves);
-  const int share = kv8_prefill_share(((int64_t)(uint32_t)halves + n_blocks) * 2, a.Hkv);   // no less than their sum
+__device__ __forceinline__ PlanCut plan_cut(PlanLds& lds, const Kv8AttnArgs& a, int n_blocks, const PrefillUnit& u) {
+  const uint32_t size = kv8_prefill_size(u.t1, kv8_prefill_shift(a.bt_stride));
+  int total, all;
   PlanCut c;
-  c.parts = (int)threadIdx.x < n_blocks ? kv8_prefill_parts(tiles, share) : 0;
-  // units, slots and jobs number under 2^10 each: one scan
-  const int cut = c.parts > 1;
-  const int at = plan_scan(lds, c.parts | (cut ? c.parts : 0) << 10 | cut << 20, all);
-  c.first = at & 1023;
-  c.slot0 = at >> 10 & 1023;
-  c.job = at >> 20;
-  c.n_units = all & 1023;
-  c.n_jobs = all >> 20;
+  c.at = (uint32_t)plan_scan(lds, (int)size, total);
+  c.share = kv8_prefill_share((uint32_t)total, a.Hkv);
+  c.parts = (int)threadIdx.x < n_blocks ? kv8_prefill_cut(c.at, size, c.share).parts : 0;
+  // units and jobs number under 2^12 each: one scan
+  const int n = plan_scan(lds, c.parts | (c.parts > 1) << 16, all);
+  c.first = n & 0xFFFF;
+  c.job = n >> 16;
+  c.n_units = all & 0xFFFF;
+  c.n_jobs = all >> 16;
   return c;
 }
-// Part k of a cut block.  (Slots number under `slots` where row0 ascends.)
-__device__ __forceinline__ void plan_part(PrefillUnit& u, int parts, int slot0, int k, int slots) {
-  const int len = kv8_prefill_part_tiles(u.t1, parts);
-  u.t0 = k * len;
-  u.t1 = min(u.t1, u.t0 + len);
-  u.slot = parts > 1 ? min(slot0 + k, slots - 1) : -1;
+// The blocks of a batch that is cut, and the tiles of its units
+struct CutLds {
+  PrefillUnit whole[kCus];
+  uint32_t at[kCus];
+  int32_t first[kCus];
+  int32_t tiles[kCus + kPrefillResident + 4] __attribute__((aligned(16)));
+};
+// f(unit, its place) for every unit of that batch, in the order in which they are to run: the longest first where not all
+// are resident at once.  (Partial slots number under `slots` where row0 ascends.)
+template <typename F>
+__device__ __forceinline__ void plan_units(CutLds& lds, const Kv8AttnArgs& a, int n_blocks, const PrefillUnit& u,
+                                           const PlanCut& c, int slots, F&& f) {
+  const int tid = threadIdx.x, shift = kv8_prefill_shift(a.bt_stride);
+  lds.whole[tid] = u;
+  lds.at[tid] = c.at;
+  lds.first[tid] = c.first;
+  __syncthreads();
+  auto unit = [&](int i) {
+    const int b = last_at(lds.first, n_blocks, i), k = i - lds.first[b];
+    PrefillUnit x = lds.whole[b];
+    const uint32_t at = lds.at[b];
+    const Kv8Cut cut = kv8_prefill_cut(at, kv8_prefill_size(x.t1, shift), c.share);
+    x.t0 = kv8_prefill_part_tile(cut, at, c.share, shift, x.t1, k);
+    x.t1 = kv8_prefill_part_tile(cut, at, c.share, shift, x.t1, k + 1);
+    x.slot = cut.parts > 1 ? min(i, slots - 1) : -1;
+    return x;
+  };
+  if (c.n_units <= kv8_prefill_streams(a.Hkv)) {
+    for (int i = tid; i < c.n_units; i += kPlanThreads) f(unit(i), i);
+    return;
+  }
+  for (int i = tid; i < c.n_units + 4; i += kPlanThreads) {
+    int n = -1;
+    if (i < c.n_units) {
+      const PrefillUnit x = unit(i);
+      n = x.t1 - x.t0;
+    }
+    lds.tiles[i] = n;
+  }
+  __syncthreads();
+  for (int i = tid; i < c.n_units; i += kPlanThreads) {
+    const int mine = lds.tiles[i];
+    int rank = 0;   // units that come before this one
+#pragma unroll 4
+    for (int j = 0; j < c.n_units; j += 4) {
+      const int4 t = *reinterpret_cast<const int4*>(lds.tiles + j);
+      rank += (t.x > mine || (t.x == mine && j < i)) + (t.y > mine || (t.y == mine && j + 1 < i)) +
+              (t.z > mine || (t.z == mine && j + 2 < i)) + (t.w > mine || (t.w == mine && j + 3 < i));
+    }
+    f(unit(i), rank);
+  }
 }
 
 // A batch of up to kPlanThreads sequences and blocks is planned by every workgroup of the kernels that follow for
@@ -572,9 +617,16 @@ __device__ __forceinline__ void plan_part(PrefillUnit& u, int parts, int slot0, 
 template <bool JOBS>
 struct SmallPlan {
   PlanLds scan;
-  int32_t tiles[JOBS ? 1 : kPlanThreads];
   PrefillUnit unit;
-  PrefillJob jobs[JOBS ? kCus : 1];
+  union {
+    int32_t tiles[kPlanThreads];
+    CutLds cut;
+  };
+};
+template <>
+struct SmallPlan<true> {
+  PlanLds scan;
+  PrefillJob jobs[kCus];
 };
 template <bool JOBS>
 __device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8AttnArgs& a, int queries, int slots, int want) {
@@ -593,26 +645,30 @@ __device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8AttnArg
     u = plan_block(a, queries, s, r0, m, tid - lds.scan.pre[s]);
   }
   if (!kv8_prefill_cuts(n, a.Hkv)) {
-    if constexpr (JOBS) return 0;
-    const int half = kPrefillResident / 2 / a.Hkv, window = min(n, kPrefillResident / a.Hkv);
-    if (want >= half && want < window) want = half + window - 1 - want;
-    lds.tiles[tid] = u.t1;
-    __syncthreads();
-    int rank = 0;   // blocks that come before this one
-    for (int i = 0; i < n; ++i) {
-      const int t = lds.tiles[i];
-      rank += t > u.t1 || (t == u.t1 && i < tid);
+    if constexpr (JOBS) {
+      return 0;
+    } else {
+      const int half = kPrefillResident / 2 / a.Hkv, window = min(n, kPrefillResident / a.Hkv);
+      if (want >= half && want < window) want = half + window - 1 - want;
+      lds.tiles[tid] = u.t1;
+      __syncthreads();
+      int rank = 0;   // blocks that come before this one
+      for (int i = 0; i < n; ++i) {
+        const int t = lds.tiles[i];
+        rank += t > u.t1 || (t == u.t1 && i < tid);
+      }
+      if (tid < n && rank == want) lds.unit = u;
+      __syncthreads();
+      return n;
     }
-    if (tid < n && rank == want) lds.unit = u;
-    __syncthreads();
-    return n;
   }
-  const PlanCut c = plan_cut(lds.scan, a, n, u.t1);
-  if (JOBS) {
-    if (c.parts > 1) lds.jobs[JOBS ? c.job : 0] = PrefillJob{u.row, u.nq, c.slot0, c.parts};
-  } else if (want >= c.first && want < c.first + c.parts) {
-    plan_part(u, c.parts, c.slot0, want - c.first, slots);
-    lds.unit = u;
+  const PlanCut c = plan_cut(lds.scan, a, n, u);
+  if constexpr (JOBS) {
+    if (c.parts > 1) lds.jobs[c.job] = PrefillJob{u.row, u.nq, c.first, c.parts};
+  } else {
+    plan_units(lds.cut, a, n, u, c, slots, [&](const PrefillUnit& x, int place) {
+      if (place == want) lds.unit = x;
+    });
   }
   __syncthreads();
   return JOBS ? c.n_jobs : c.n_units;
@@ -674,24 +730,15 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
     }
     return;
   }
-  __shared__ PrefillUnit whole[kCus];
-  __shared__ int32_t first[kCus], parts[kCus];
-  blocks([&](const PrefillUnit& u, int i) { whole[i] = u; });
+  __shared__ CutLds cut;
+  blocks([&](const PrefillUnit& u, int i) { cut.whole[i] = u; });
   __syncthreads();
-  const PlanCut c = plan_cut(lds, a, n_blocks, tid < n_blocks ? whole[tid].t1 : 0);
-  if (tid < n_blocks) {
-    first[tid] = c.first;
-    parts[tid] = c.parts;
-    whole[tid].slot = c.slot0;
-    if (c.parts > 1) p.jobs[c.job] = PrefillJob{whole[tid].row, whole[tid].nq, c.slot0, c.parts};
-  }
-  __syncthreads();
-  for (int i = tid; i < c.n_units; i += kPlanThreads) {
-    const int b = last_at(first, n_blocks, i);
-    PrefillUnit u = whole[b];
-    plan_part(u, parts[b], u.slot, i - first[b], p.slots);
-    p.units[i] = u;
-  }
+  PrefillUnit u;
+  u.t1 = 0;
+  if (tid < n_blocks) u = cut.whole[tid];
+  const PlanCut c = plan_cut(lds, a, n_blocks, u);
+  if (c.parts > 1) p.jobs[c.job] = PrefillJob{u.row, u.nq, c.first, c.parts};
+  plan_units(cut, a, n_blocks, u, c, p.slots, [&](const PrefillUnit& x, int place) { p.units[place] = x; });
   if (tid == 0) {
     p.head->n_units = c.n_units;
     p.head->n_jobs = c.n_jobs;
@@ -793,15 +840,17 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   };
   // V of a tile is loaded and stored a step after its K, with the page and the scale that K looked up
   typedef uint32_t words_t[DH / 32];
-  int e_last = 0;
+  uint64_t at_last = 0;
   float vs_last = 1.f;
   // (one buffer descriptor for each page: scalar work only, and the pools may exceed 4 GiB)
-  auto page_rsrc = [&](const uint8_t* pool) __attribute__((always_inline)) {
-    return make_rsrc(pool + kv_tile(kvh, a.pool.n_blocks, __builtin_amdgcn_readfirstlane(e_last), DH), kPage * DH);
-  };
+  const uint8_t* k_head = a.pool.k + kv_tile(kvh, a.pool.n_blocks, 0, DH);
+  const uint8_t* v_head = a.pool.v + kv_tile(kvh, a.pool.n_blocks, 0, DH);
+  float scale_log2 = a.scale_log2;
+  // (what the steps use, apart from the arguments' registers: those are spilled and fetched back sixteen at a time)
+  asm volatile("" : "+s"(k_head), "+s"(v_head), "+s"(scale_log2));
   auto load_k = [&](words_t& R, int t) __attribute__((always_inline)) {
-    e_last = __builtin_amdgcn_readlane(blk, (t & 31) * 2 + pg);
-    const rsrc_t rs = page_rsrc(a.pool.k);
+    at_last = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(blk, (t & 31) * 2 + pg) * (kPage * DH);
+    const rsrc_t rs = make_rsrc(k_head + at_last, kPage * DH);
     if constexpr (DH == 128) {
       const uint4 x = buf_load16(rs, k_src, 0);
       R[0] = x.x; R[1] = x.y; R[2] = x.z; R[3] = x.w;
@@ -811,7 +860,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     }
   };
   auto load_v = [&](words_t& R) __attribute__((always_inline)) {
-    const rsrc_t rs = page_rsrc(a.pool.v);
+    const rsrc_t rs = make_rsrc(v_head + at_last, kPage * DH);
     if constexpr (DH == 128) {
       const uint2 y = buf_load8(rs, v_src, 0), z = buf_load8(rs, v_src, 8 * DH);
       R[0] = y.x; R[1] = y.y; R[2] = z.x; R[3] = z.y;
@@ -877,7 +926,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     float v = x[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) v = fmaxf(v, x[r]);
-    return half_swap_max(v) * a.scale_log2;
+    return half_swap_max(v) * scale_log2;
   };
   // NaN in V of a tile with masked keys (one that some pairs see and others do not, or a place past the context, which
   // may hold anything): a weight of zero would spread it to pairs that do not see its key.  So the tile's NaN become zeros in LDS, and infinities are added where a pair sees one, as
@@ -953,7 +1002,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     float pv[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      pv[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale_log2, -m));
+      pv[r] = __builtin_amdgcn_exp2f(fmaf(x[r], scale_log2, -m));
       ps += pv[r];
     }
     l += ps;
@@ -1100,40 +1149,53 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
                      pack_bf2(o[dt][g4 * 4 + 2] * inv, o[dt][g4 * 4 + 3] * inv));
 }
 
-// Joins the parts of cut blocks: DH/4 threads a (query, head) pair and one of R streams of parts, P pairs a
-// workgroup; the workgroups walk the pairs of all jobs, so that a launch with nothing to join (the host does not know)
-// is short.
+// Joins the parts of cut blocks: DH/4 threads a (query, head) pair; the workgroups walk the pairs of all jobs, so that a
+// launch with nothing to join (the host does not know) is short.  With few jobs, of many parts then, R streams of parts
+// share a pair (17 queries over 30k keys 34 us; with one 41); with more than kMergeWalk rounds of that, a pair has one
+// (512 queries at 8192 107 us; with R 120).
+constexpr int kMergeWalk = 2;
 template <int DH, bool SMALL>
 __global__ __launch_bounds__(256) void kv8_prefill_merge_kernel(Kv8PrefillArgs p) {
-  constexpr int C = DH / 4, R = 4, P = 256 / C / R;
+  constexpr int C = DH / 4, N = 256 / C, R = 4;
   const Kv8AttnArgs& a = p.a;
   const int G = a.Hq / a.Hkv;
-  const int c = threadIdx.x % C, r = threadIdx.x / C % R, pl = threadIdx.x / C / R;
-  __shared__ float2 s_ml[P][R];
-  __shared__ float4 s_acc[P][R][C];
+  const int c = threadIdx.x % C, row = threadIdx.x / C;
+  __shared__ float2 s_ml[N];
+  __shared__ float4 s_acc[N][C];
   __shared__ SmallPlan<true> plan;
-  constexpr int GROUPS = kPrefillPairs / P;
   const int n_jobs = SMALL ? plan_small(plan, a, p.qpi, p.slots, 0) : p.head->n_jobs;
-  const int items = n_jobs * a.Hkv * GROUPS;
-  for (int i = blockIdx.x; i < items; i += gridDim.x) {
-    const int job = i / GROUPS, jb = job / a.Hkv, kvh = job - jb * a.Hkv;
-    const PrefillJob mg = SMALL ? plan.jobs[jb] : p.jobs[jb];
-    const int pair0 = i % GROUPS * P;
-    if (pair0 >= mg.nq * G || mg.slot0 + mg.n_part > p.slots) continue;   // (uniform over the workgroup)
-    const int pair = pair0 + pl;        // a pair past the block's: its slot exists, its row is not written
-    const size_t slot = ((size_t)kvh * p.slots + mg.slot0) * kPrefillPairs + pair;
-    MergeState<DH> S;
-    S.take(reinterpret_cast<const float2*>(p.part_ml) + slot, p.part_o + slot * DH + c * 4, kPrefillPairs, mg.n_part, r, R);
-    __syncthreads();
-    if (c == 0) s_ml[pl][r] = make_float2(S.M, S.L);
-    s_acc[pl][r][c] = S.acc;
-    __syncthreads();
-    if (r == 0 && pair < mg.nq * G) {
-      for (int j = 1; j < R; ++j) S.fold(s_ml[pl][j], s_acc[pl][j][c]);
-      const int qi = pair / G, hj = pair - qi * G;
-      S.write(a.out + (int64_t)(mg.row + qi) * a.out_stride + (kvh * G + hj) * DH + c * 4);
+  // f(job, head, pair of this thread) for every R-th row, or every row
+  auto walk = [&](int streams, auto&& f) {
+    const int groups = kPrefillPairs / N * streams;
+    for (int i = blockIdx.x; i < n_jobs * a.Hkv * groups; i += gridDim.x) {
+      const int job = i / groups, jb = job / a.Hkv, kvh = job - jb * a.Hkv;
+      const PrefillJob mg = SMALL ? plan.jobs[jb] : p.jobs[jb];
+      const int pair0 = (i - job * groups) * (N / streams);
+      if (pair0 >= mg.nq * G || mg.slot0 + mg.n_part > p.slots) continue;   // (uniform over the workgroup)
+      const int pair = pair0 + row / streams;   // a pair past the block's: its slot exists, its row is not written
+      const size_t slot = ((size_t)kvh * p.slots + mg.slot0) * kPrefillPairs + pair;
+      MergeState<DH> S;
+      S.take(reinterpret_cast<const float2*>(p.part_ml) + slot, p.part_o + slot * DH + c * 4, kPrefillPairs, mg.n_part,
+             row % streams, streams);
+      f(S);
+      if (row % streams == 0 && pair < mg.nq * G) {
+        const int qi = pair / G, hj = pair - qi * G;
+        S.write(a.out + (int64_t)(mg.row + qi) * a.out_stride + (kvh * G + hj) * DH + c * 4);
+      }
     }
+  };
+  if (n_jobs * a.Hkv * (kPrefillPairs * R / N) > kMergeWalk * (int)gridDim.x) {
+    walk(1, [](MergeState<DH>&) {});
+    return;
   }
+  walk(R, [&](MergeState<DH>& S) {
+    __syncthreads();
+    if (c == 0) s_ml[row] = make_float2(S.M, S.L);
+    s_acc[row][c] = S.acc;
+    __syncthreads();
+    if (row % R == 0)
+      for (int j = 1; j < R; ++j) S.fold(s_ml[row + j], s_acc[row + j][c]);
+  });
 }
 
 }  // namespace
@@ -1180,9 +1242,9 @@ static hipError_t prefill_launch(const Kv8PrefillArgs& p, int64_t whole, bool cu
   const int64_t units = cuts ? p.unit_cap : std::min<int64_t>(whole, p.unit_cap);
   hipLaunchKernelGGL((kv8_prefill_kernel<DH, SMALL>), dim3((unsigned)(units * hkv)), dim3(256), 0, st, p);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || !cuts) return e;
-  // cut blocks number under kCus / hkv, and no more than there are blocks; 256 / (dh / 4) / 4 pairs a workgroup
-  const int64_t jobs = std::min<int64_t>(whole, (kCus + hkv - 1) / hkv) * hkv;
-  const int64_t groups = std::min<int64_t>(jobs * kPrefillPairs / (256 / DH), 2 * kCus);
+  // cut blocks, over all heads, number under kPrefillCutUnits; 256 / (dh / 4) / 4 pairs a workgroup
+  const int64_t jobs = std::min<int64_t>(whole * hkv, kPrefillCutUnits);
+  const int64_t groups = std::min<int64_t>(jobs * kPrefillPairs / (256 / DH), 4 * kCus);
   hipLaunchKernelGGL((kv8_prefill_merge_kernel<DH, SMALL>), dim3((unsigned)groups), dim3(256), 0, st, p);
   return hipGetLastError();
 }
@@ -1199,10 +1261,10 @@ hipError_t kv8_prefill_launch(const Kv8AttnArgs& a, hipStream_t st) {
   p.unit_cap = w.unit_cap;
   p.slots = w.slots;
   p.qpi = prefill_queries_per_item(a.Hq / a.Hkv);
-  // A block is cut only into parts of more than kPrefillMinTiles / 2 tiles, so short tables need no room for parts
+  // A block of up to 3 kPrefillMinTiles tiles is never cut: with short tables there is nothing to join
   const int64_t whole = std::min<int64_t>((int64_t)a.T / p.qpi + a.S, INT32_MAX);
   const int most = (a.bt_stride * kPage + 63) / 64 * 2;   // tiles of the longest block there can be
-  const bool cuts = most > kPrefillMinTiles;
+  const bool cuts = most > 3 * kPrefillMinTiles;
   if (a.S <= kPlanThreads && whole <= kPlanThreads)
     return a.dh == 128 ? prefill_launch<128, true>(p, whole, cuts, st) : prefill_launch<64, true>(p, whole, cuts, st);
   hipLaunchKernelGGL(kv8_prefill_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);

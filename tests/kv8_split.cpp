@@ -40,14 +40,13 @@ static void decode(const std::vector<int>& pages, int hkv) {
 
 static void prefill(const std::vector<int>& rows, const std::vector<int64_t>& pos, int hkv, int group, int64_t pad) {
   const int q = kPrefillPairs / group;
-  int64_t T = pad, blocks = 0, tiles = 0;
+  int64_t T = pad, blocks = 0;
   std::vector<int> all;
   for (size_t s = 0; s < rows.size(); ++s) {
     T += rows[s];
     for (int r = 0; r < rows[s]; r += q) {
       const int64_t end = std::min<int64_t>(pos[s] + std::min(r + q, rows[s]), int64_t(1) << 30);
       all.push_back((int)((std::max<int64_t>(end, 0) + 63) / 64 * 2));
-      tiles += all.back();
       ++blocks;
     }
   }
@@ -57,17 +56,30 @@ static void prefill(const std::vector<int>& rows, const std::vector<int64_t>& po
     CHECK(blocks < cap);
     return;
   }
-  CHECK(blocks < kCus);
-  const int share = kv8_prefill_share(tiles + 2 * blocks, hkv);
-  int64_t units = 0, used = 0;
+  CHECK(blocks <= kCus && blocks * hkv < kPrefillCutUnits);
+  const int shift = kv8_prefill_shift(1 << 26 >> (pad % 3));   // of long tables, whatever the blocks are
+  uint64_t total = 0;
+  for (int t : all) total += kv8_prefill_size(t, shift);
+  CHECK(total < (uint64_t(1) << 31));
+  const uint32_t share = kv8_prefill_share((uint32_t)total, hkv);
+  int64_t units = 0;
+  uint32_t at = 0;
   for (int t : all) {
-    const int n = kv8_prefill_parts(t, share), len = kv8_prefill_part_tiles(t, n);
-    CHECK(n >= 1 && len % 2 == 0);
-    if (t) CHECK((int64_t)(n - 1) * len < t && (int64_t)n * len >= t);
-    units += n;
-    if (n > 1) used += n;
+    const uint32_t size = kv8_prefill_size(t, shift);
+    const Kv8Cut c = kv8_prefill_cut(at, size, share);
+    CHECK(c.parts >= 1);
+    int end = 0;
+    for (int k = 0; k < c.parts; ++k) {   // successive, even, none of several empty or far beyond a share
+      const int t0 = kv8_prefill_part_tile(c, at, share, shift, t, k), t1 = kv8_prefill_part_tile(c, at, share, shift, t, k + 1);
+      CHECK(t0 == end && t0 % 2 == 0 && t1 % 2 == 0 && (t1 > t0 || c.parts == 1));
+      CHECK(t1 - t0 <= ((int64_t)share + kPrefillMinTiles) << (shift + 1));
+      end = t1;
+    }
+    CHECK(end == t);
+    units += c.parts;
+    at += size;
   }
-  CHECK(units < cap && used < slots);
+  CHECK(units <= blocks + kv8_prefill_streams(hkv) && units < cap && units < slots && units <= kCus + kPrefillResident);
 }
 
 int main() {

@@ -525,6 +525,34 @@ def test_prefill_rows_past_the_table_and_row0_out_of_range():
     assert np.all(out.cpu().numpy().view(np.uint16).reshape(24, -1)[20:] == 0x1234)
 
 
+@pytest.mark.parametrize("heads,n,hi_pos,places", [
+    ((32, 8, 128), [300, 250, 200, 150, 40, 33, 17, 1], 2500, 0), ((32, 8, 128), [300, 250, 200, 150, 40, 33, 17, 1], 2500, 300),
+    ((16, 1, 64), [700, 450, 200, 9], 2000, 0), ((16, 1, 64), [700, 450, 200, 9], 2000, 280), ((8, 2, 64), [1, 1, 130, 1], 9000, 0),
+    ((40, 8, 128), [64, 200, 256, 7, 90], 1200, 0), ((6, 6, 64), [129, 300, 20], 4000, 0)])
+def test_prefill_blocks_dealt_out_in_shares(heads, n, hi_pos, places):
+    """Blocks of very different lengths, cut where the workgroups' shares end, more pieces than are resident at once;
+    places: empty ones among them, for the batches that a launch of its own plans."""
+    hq, hkv, dh = heads
+    rng = np.random.default_rng(hi_pos + places)
+    n, pos0 = np.array(n + [0] * places), rng.integers(0, hi_pos, len(n) + places)
+    pos0[:3] = hi_pos, 5, hi_pos // 2
+    order = rng.permutation(len(n))
+    n, pos0 = n[order], pos0[order]
+    pos0[n == 0] = 0
+    cache, bt = _attention_case(rng, pos0 + n, hq, hkv, dh)
+    _prefill(cache, bt, pos0, n, hq, rng, pad=3, what="shares")
+
+
+def test_prefill_of_a_very_wide_table():
+    """2^25 entries a sequence: the work split counts in coarser units."""
+    rng = np.random.default_rng(21)
+    pos0, n = np.array([4000]), np.array([45])
+    cache, bt = _attention_case(rng, pos0 + n, 8, 2, 128)
+    wide = np.full((1, 1 << 25), -1, np.int32)
+    wide[:, :bt.shape[1]] = bt
+    _prefill(cache, wide, pos0, n, 8, rng, what="wide table")
+
+
 @pytest.mark.parametrize("S,T", [(10, 256), (401, 256), (3, 64)])
 def test_prefill_row0_that_does_not_ascend_stays_in_its_buffers(S, T):
     """More rows than T in all, over contexts long enough to be cut: nothing is written past the workspace or out."""
