@@ -482,6 +482,7 @@ struct Kv8PrefillArgs {
   float* part_o;    // [Hkv][slots][128 pairs][dh]: unnormalized
   float* part_ml;   // [Hkv][slots][128 pairs][2]: (maximum in log2 units, sum)
   int unit_cap, slots, qpi;
+  bool cuts;        // whether blocks may be cut
 };
 
 // What the planning kernels share.  kPlanThreads threads, a thread for each block of a batch that is cut.
@@ -557,6 +558,15 @@ __device__ __forceinline__ PlanCut plan_cut(PlanLds& lds, const Kv8AttnArgs& a, 
   c.n_jobs = all >> 16;
   return c;
 }
+// Part k of a cut block, whose sizes begin at `at`, as unit i.  (Partial slots number under `slots` where row0 ascends.)
+__device__ __forceinline__ void plan_part(PrefillUnit& u, const Kv8AttnArgs& a, uint32_t at, uint32_t share, int k, int i,
+                                          int slots) {
+  const int shift = kv8_prefill_shift(a.bt_stride), tiles = u.t1;
+  const Kv8Cut cut = kv8_prefill_cut(at, kv8_prefill_size(tiles, shift), share);
+  u.t0 = kv8_prefill_part_tile(cut, at, share, shift, tiles, k);
+  u.t1 = kv8_prefill_part_tile(cut, at, share, shift, tiles, k + 1);
+  u.slot = cut.parts > 1 ? min(i, slots - 1) : -1;
+}
 // The blocks of a batch that is cut, and the tiles of its units
 struct CutLds {
   PrefillUnit whole[kCus];
@@ -565,23 +575,19 @@ struct CutLds {
   int32_t tiles[kCus + kPrefillResident + 4] __attribute__((aligned(16)));
 };
 // f(unit, its place) for every unit of that batch, in the order in which they are to run: the longest first where not all
-// are resident at once.  (Partial slots number under `slots` where row0 ascends.)
+// are resident at once.
 template <typename F>
 __device__ __forceinline__ void plan_units(CutLds& lds, const Kv8AttnArgs& a, int n_blocks, const PrefillUnit& u,
                                            const PlanCut& c, int slots, F&& f) {
-  const int tid = threadIdx.x, shift = kv8_prefill_shift(a.bt_stride);
+  const int tid = threadIdx.x;
   lds.whole[tid] = u;
   lds.at[tid] = c.at;
   lds.first[tid] = c.first;
   __syncthreads();
   auto unit = [&](int i) {
-    const int b = last_at(lds.first, n_blocks, i), k = i - lds.first[b];
+    const int b = last_at(lds.first, n_blocks, i);
     PrefillUnit x = lds.whole[b];
-    const uint32_t at = lds.at[b];
-    const Kv8Cut cut = kv8_prefill_cut(at, kv8_prefill_size(x.t1, shift), c.share);
-    x.t0 = kv8_prefill_part_tile(cut, at, c.share, shift, x.t1, k);
-    x.t1 = kv8_prefill_part_tile(cut, at, c.share, shift, x.t1, k + 1);
-    x.slot = cut.parts > 1 ? min(i, slots - 1) : -1;
+    plan_part(x, a, lds.at[b], c.share, i - lds.first[b], i, slots);
     return x;
   };
   if (c.n_units <= kv8_prefill_streams(a.Hkv)) {
@@ -629,8 +635,9 @@ struct SmallPlan<true> {
   PrefillJob jobs[kCus];
 };
 template <bool JOBS>
-__device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8AttnArgs& a, int queries, int slots, int want) {
-  const int tid = threadIdx.x;
+__device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8PrefillArgs& p, int want) {
+  const Kv8AttnArgs& a = p.a;
+  const int tid = threadIdx.x, queries = p.qpi;
   int r0 = 0, total;
   const int rows = tid < a.S ? plan_rows(a, tid, r0) : 0;
   const int before = plan_scan(lds.scan, (rows + queries - 1) / queries, total);
@@ -644,10 +651,15 @@ __device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8AttnArg
     const int m = plan_rows(a, s, r0);
     u = plan_block(a, queries, s, r0, m, tid - lds.scan.pre[s]);
   }
-  if (!kv8_prefill_cuts(n, a.Hkv)) {
+  if (!p.cuts || !kv8_prefill_cuts(n, a.Hkv)) {
     if constexpr (JOBS) {
       return 0;
     } else {
+      if (n * a.Hkv <= kCus) {   // a CU each, in any order
+        if (tid == want) lds.unit = u;
+        __syncthreads();
+        return n;
+      }
       const int half = kPrefillResident / 2 / a.Hkv, window = min(n, kPrefillResident / a.Hkv);
       if (want >= half && want < window) want = half + window - 1 - want;
       lds.tiles[tid] = u.t1;
@@ -665,8 +677,13 @@ __device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8AttnArg
   const PlanCut c = plan_cut(lds.scan, a, n, u);
   if constexpr (JOBS) {
     if (c.parts > 1) lds.jobs[c.job] = PrefillJob{u.row, u.nq, c.first, c.parts};
+  } else if (c.n_units <= kv8_prefill_streams(a.Hkv)) {
+    if (want >= c.first && want < c.first + c.parts) {
+      plan_part(u, a, c.at, c.share, want - c.first, want, p.slots);
+      lds.unit = u;
+    }
   } else {
-    plan_units(lds.cut, a, n, u, c, slots, [&](const PrefillUnit& x, int place) {
+    plan_units(lds.cut, a, n, u, c, p.slots, [&](const PrefillUnit& x, int place) {
       if (place == want) lds.unit = x;
     });
   }
@@ -707,7 +724,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
   auto bin_of = [&](int tiles) { return kBins - 1 - min(tiles >> shift, kBins - 1); };
   const int n_blocks = blocks([&](const PrefillUnit& u, int) { atomicAdd(&bins[bin_of(u.t1)], 1); });
   __syncthreads();
-  if (!kv8_prefill_cuts(n_blocks, a.Hkv)) {
+  if (!p.cuts || !kv8_prefill_cuts(n_blocks, a.Hkv)) {
     int all, sum = 0;
     for (int k = 0; k < kPer; ++k) sum += bins[tid * kPer + k];
     int at = plan_scan(lds, sum, all);
@@ -771,7 +788,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   PrefillUnit it;
   if constexpr (SMALL) {
     __shared__ SmallPlan<false> plan;
-    if (ui >= plan_small(plan, a, p.qpi, p.slots, ui)) return;
+    if (ui >= plan_small(plan, p, ui)) return;
     // (what came through LDS is wavefront-uniform)
     const int32_t* u = reinterpret_cast<const int32_t*>(&plan.unit);
     int32_t* v = reinterpret_cast<int32_t*>(&it);
@@ -1163,7 +1180,7 @@ __global__ __launch_bounds__(256) void kv8_prefill_merge_kernel(Kv8PrefillArgs p
   __shared__ float2 s_ml[N];
   __shared__ float4 s_acc[N][C];
   __shared__ SmallPlan<true> plan;
-  const int n_jobs = SMALL ? plan_small(plan, a, p.qpi, p.slots, 0) : p.head->n_jobs;
+  const int n_jobs = SMALL ? plan_small(plan, p, 0) : p.head->n_jobs;
   // f(job, head, pair of this thread) for every R-th row, or every row
   auto walk = [&](int streams, auto&& f) {
     const int groups = kPrefillPairs / N * streams;
@@ -1235,13 +1252,13 @@ hipError_t kv8_decode_launch(const Kv8AttnArgs& args, hipStream_t st) {
   return a.dh == 128 ? decode_launch<128, false>(a, st) : decode_launch<64, false>(a, st);
 }
 
-// whole: blocks at most; cuts: whether blocks may be cut
+// whole: blocks at most
 template <int DH, bool SMALL>
-static hipError_t prefill_launch(const Kv8PrefillArgs& p, int64_t whole, bool cuts, hipStream_t st) {
+static hipError_t prefill_launch(const Kv8PrefillArgs& p, int64_t whole, hipStream_t st) {
   const int hkv = p.a.Hkv;
-  const int64_t units = cuts ? p.unit_cap : std::min<int64_t>(whole, p.unit_cap);
+  const int64_t units = p.cuts ? p.unit_cap : std::min<int64_t>(whole, p.unit_cap);
   hipLaunchKernelGGL((kv8_prefill_kernel<DH, SMALL>), dim3((unsigned)(units * hkv)), dim3(256), 0, st, p);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || !cuts) return e;
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || !p.cuts) return e;
   // cut blocks, over all heads, number under kPrefillCutUnits; 256 / (dh / 4) / 4 pairs a workgroup
   const int64_t jobs = std::min<int64_t>(whole * hkv, kPrefillCutUnits);
   const int64_t groups = std::min<int64_t>(jobs * kPrefillPairs / (256 / DH), 4 * kCus);
@@ -1264,12 +1281,12 @@ hipError_t kv8_prefill_launch(const Kv8AttnArgs& a, hipStream_t st) {
   // A block of up to 3 kPrefillMinTiles tiles is never cut: with short tables there is nothing to join
   const int64_t whole = std::min<int64_t>((int64_t)a.T / p.qpi + a.S, INT32_MAX);
   const int most = (a.bt_stride * kPage + 63) / 64 * 2;   // tiles of the longest block there can be
-  const bool cuts = most > 3 * kPrefillMinTiles;
+  p.cuts = most > 3 * kPrefillMinTiles;
   if (a.S <= kPlanThreads && whole <= kPlanThreads)
-    return a.dh == 128 ? prefill_launch<128, true>(p, whole, cuts, st) : prefill_launch<64, true>(p, whole, cuts, st);
+    return a.dh == 128 ? prefill_launch<128, true>(p, whole, st) : prefill_launch<64, true>(p, whole, st);
   hipLaunchKernelGGL(kv8_prefill_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  return a.dh == 128 ? prefill_launch<128, false>(p, whole, cuts, st) : prefill_launch<64, false>(p, whole, cuts, st);
+  return a.dh == 128 ? prefill_launch<128, false>(p, whole, st) : prefill_launch<64, false>(p, whole, st);
 }
 
 }  // namespace hxf
