@@ -772,9 +772,10 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
 // matrix operands.  A step multiplies K of tile t + 1 and V of tile t, so that the scores of the next tile and the
 // exponentials of this one run side by side; the conversions run beside the product with V.
 //
-// What bounds it: at 6144 + 2048 the power limit and the wavefronts' waits (MFMA busy 41% of the cycles, LDS ports 31%);
-// 2048 queries there 251 us, 0.96 PFLOP/s, as the bf16 cache's kernel.  17 queries over 30k keys: 27 us,
-// 2.3 TB/s, of which four are the plan and the first loads.
+// What bounds it: at 6144 + 2048 the power limit (13% more cycles than the bf16 cache's kernel in less time) and the
+// wavefronts' waits (MFMA busy 46% of the cycles, LDS ports 35%); 2048 queries there 247 us, 0.97 PFLOP/s, where the
+// bf16 cache's kernel takes 257.  17 queries over 30k keys: 28 us, 2.2 TB/s, of which four are the plan and the first
+// loads, and the steps' latency the rest.
 template <int DH, bool SMALL>
 __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   constexpr int KS = DH / 16;      // 16-dim steps of QK^T
