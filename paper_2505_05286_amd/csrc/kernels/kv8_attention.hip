@@ -616,11 +616,10 @@ __device__ __forceinline__ void plan_units(CutLds& lds, const Kv8AttnArgs& a, in
   }
 }
 
-// A batch of up to kPlanThreads sequences and blocks is planned by every workgroup of the kernels that follow for
-// itself, in the time that a list made by a launch of its own would take to read: this makes unit `want` (in
-// `unit`) or all jobs (in `jobs`), and returns their number.  Units come longest first; and among the first resident
+// A batch of up to kPlanThreads sequences and blocks is planned by every workgroup for itself, in the time that a list
+// made by a launch of its own would take to read: this makes unit `want` and returns the units' number.  The first
+// workgroup leaves the jobs for the launch that joins them.  Units come longest first; and among the first resident
 // workgroups the second half in reverse, so that a CU gets a long one and a short one.
-template <bool JOBS>
 struct SmallPlan {
   PlanLds scan;
   PrefillUnit unit;
@@ -629,13 +628,7 @@ struct SmallPlan {
     CutLds cut;
   };
 };
-template <>
-struct SmallPlan<true> {
-  PlanLds scan;
-  PrefillJob jobs[kCus];
-};
-template <bool JOBS>
-__device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8PrefillArgs& p, int want) {
+__device__ __forceinline__ int plan_small(SmallPlan& lds, const Kv8PrefillArgs& p, int want) {
   const Kv8AttnArgs& a = p.a;
   const int tid = threadIdx.x, queries = p.qpi;
   int r0 = 0, total;
@@ -652,32 +645,31 @@ __device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8Prefill
     u = plan_block(a, queries, s, r0, m, tid - lds.scan.pre[s]);
   }
   if (!p.cuts || !kv8_prefill_cuts(n, a.Hkv)) {
-    if constexpr (JOBS) {
-      return 0;
-    } else {
-      if (n * a.Hkv <= kCus) {   // a CU each, in any order
-        if (tid == want) lds.unit = u;
-        __syncthreads();
-        return n;
-      }
-      const int half = kPrefillResident / 2 / a.Hkv, window = min(n, kPrefillResident / a.Hkv);
-      if (want >= half && want < window) want = half + window - 1 - want;
-      lds.tiles[tid] = u.t1;
-      __syncthreads();
-      int rank = 0;   // blocks that come before this one
-      for (int i = 0; i < n; ++i) {
-        const int t = lds.tiles[i];
-        rank += t > u.t1 || (t == u.t1 && i < tid);
-      }
-      if (tid < n && rank == want) lds.unit = u;
+    if (blockIdx.x == 0 && tid == 0) p.head->n_jobs = 0;
+    if (n * a.Hkv <= kCus) {   // a CU each, in any order
+      if (tid == want) lds.unit = u;
       __syncthreads();
       return n;
     }
+    const int half = kPrefillResident / 2 / a.Hkv, window = min(n, kPrefillResident / a.Hkv);
+    if (want >= half && want < window) want = half + window - 1 - want;
+    lds.tiles[tid] = u.t1;
+    __syncthreads();
+    int rank = 0;   // blocks that come before this one
+    for (int i = 0; i < n; ++i) {
+      const int t = lds.tiles[i];
+      rank += t > u.t1 || (t == u.t1 && i < tid);
+    }
+    if (tid < n && rank == want) lds.unit = u;
+    __syncthreads();
+    return n;
   }
   const PlanCut c = plan_cut(lds.scan, a, n, u);
-  if constexpr (JOBS) {
-    if (c.parts > 1) lds.jobs[c.job] = PrefillJob{u.row, u.nq, c.first, c.parts};
-  } else if (c.n_units <= kv8_prefill_streams(a.Hkv)) {
+  if (blockIdx.x == 0) {
+    if (c.parts > 1) p.jobs[c.job] = PrefillJob{u.row, u.nq, c.first, c.parts};
+    if (tid == 0) p.head->n_jobs = c.n_jobs;
+  }
+  if (c.n_units <= kv8_prefill_streams(a.Hkv)) {
     if (want >= c.first && want < c.first + c.parts) {
       plan_part(u, a, c.at, c.share, want - c.first, want, p.slots);
       lds.unit = u;
@@ -688,7 +680,7 @@ __device__ __forceinline__ int plan_small(SmallPlan<JOBS>& lds, const Kv8Prefill
     });
   }
   __syncthreads();
-  return JOBS ? c.n_jobs : c.n_units;
+  return c.n_units;
 }
 
 // The units of a larger batch, in the order above, and the jobs; one workgroup, of four wavefronts because most of its
@@ -788,7 +780,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   const int ui = blockIdx.x / a.Hkv, kvh = blockIdx.x - ui * a.Hkv;
   PrefillUnit it;
   if constexpr (SMALL) {
-    __shared__ SmallPlan<false> plan;
+    __shared__ SmallPlan plan;
     if (ui >= plan_small(plan, p, ui)) return;
     // (what came through LDS is wavefront-uniform)
     const int32_t* u = reinterpret_cast<const int32_t*>(&plan.unit);
@@ -1172,7 +1164,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
 // share a pair (17 queries over 30k keys 34 us; with one 41); with more than kMergeWalk rounds of that, a pair has one
 // (512 queries at 8192 107 us; with R 120).
 constexpr int kMergeWalk = 2;
-template <int DH, bool SMALL>
+template <int DH>
 __global__ __launch_bounds__(256) void kv8_prefill_merge_kernel(Kv8PrefillArgs p) {
   constexpr int C = DH / 4, N = 256 / C, R = 4;
   const Kv8AttnArgs& a = p.a;
@@ -1180,14 +1172,13 @@ __global__ __launch_bounds__(256) void kv8_prefill_merge_kernel(Kv8PrefillArgs p
   const int c = threadIdx.x % C, row = threadIdx.x / C;
   __shared__ float2 s_ml[N];
   __shared__ float4 s_acc[N][C];
-  __shared__ SmallPlan<true> plan;
-  const int n_jobs = SMALL ? plan_small(plan, p, 0) : p.head->n_jobs;
+  const int n_jobs = p.head->n_jobs;
   // f(job, head, pair of this thread) for every R-th row, or every row
   auto walk = [&](int streams, auto&& f) {
     const int groups = kPrefillPairs / N * streams;
     for (int i = blockIdx.x; i < n_jobs * a.Hkv * groups; i += gridDim.x) {
       const int job = i / groups, jb = job / a.Hkv, kvh = job - jb * a.Hkv;
-      const PrefillJob mg = SMALL ? plan.jobs[jb] : p.jobs[jb];
+      const PrefillJob mg = p.jobs[jb];
       const int pair0 = (i - job * groups) * (N / streams);
       if (pair0 >= mg.nq * G || mg.slot0 + mg.n_part > p.slots) continue;   // (uniform over the workgroup)
       const int pair = pair0 + row / streams;   // a pair past the block's: its slot exists, its row is not written
@@ -1263,7 +1254,7 @@ static hipError_t prefill_launch(const Kv8PrefillArgs& p, int64_t whole, hipStre
   // cut blocks, over all heads, number under kPrefillCutUnits; 256 / (dh / 4) / 4 pairs a workgroup
   const int64_t jobs = std::min<int64_t>(whole * hkv, kPrefillCutUnits);
   const int64_t groups = std::min<int64_t>(jobs * kPrefillPairs / (256 / DH), 4 * kCus);
-  hipLaunchKernelGGL((kv8_prefill_merge_kernel<DH, SMALL>), dim3((unsigned)groups), dim3(256), 0, st, p);
+  hipLaunchKernelGGL((kv8_prefill_merge_kernel<DH>), dim3((unsigned)groups), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 
