@@ -296,7 +296,7 @@ struct Kv8AttnArgs {
   float scale_log2;      // log2(e) / sqrt(dh)
   uint8_t* ws;
   int64_t ws_ml;         // decode: offset of the partials' (maximum, sum) pairs
-  int32_t* starts;       // decode: parts before each sequence, where a launch makes them
+  int32_t* starts;       // decode: [B + 1] parts of a kv-head before each sequence
 };
 // Decode work split, made by the kernels themselves from the contexts in device memory.  As for the bf16
 // cache, each (sequence, kv-head) stream of pages is cut into equal parts no longer than an even share of

@@ -30,7 +30,19 @@ __device__ __forceinline__ int decode_target(const Kv8AttnArgs& a, int lane) {
   return (int)min(kv8_target_pages(total, a.S, a.Hkv), (int64_t)1 << 27);
 }
 
-// starts[b]: parts of a kv-head's streams before sequence b, for b = 0 .. S
+// starts[b]: parts of a kv-head's streams before sequence b, for b = 0 .. S.  By one wavefront:
+__device__ __forceinline__ void decode_starts(const Kv8AttnArgs& a, int lane) {
+  const int target = decode_target(a, lane);
+  int before = 0;
+  for (int i0 = 0; i0 < a.S; i0 += kWave) {
+    const int n = i0 + lane < a.S ? kv8_parts(pages_of(ctx_of(a, i0 + lane)), target) : 0;
+    const int upto = wave_scan(n);
+    if (i0 + lane < a.S) a.starts[i0 + lane] = before + upto - n;
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  if (lane == 0) a.starts[a.S] = before;
+}
+// ... and by a workgroup:
 __global__ __launch_bounds__(1024) void kv8_decode_plan_kernel(Kv8AttnArgs a) {
   __shared__ int64_t sums[16];
   __shared__ int32_t waves[16];
@@ -331,6 +343,7 @@ template <int DH, bool PLANNED>
 __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
   const int lane = threadIdx.x, b = blockIdx.x;
   const int n = b < a.S ? a.ctx[b] : 1;   // (looked at when the work is done)
+  if (!PLANNED && blockIdx.x == gridDim.x - 1) decode_starts(a, lane);   // for the join: the last seldom has a part
   decode_part<DH, PLANNED>(a, lane);
   if (n > 0) return;
   // sequence b is empty: zeros
@@ -381,7 +394,7 @@ struct MergeState {
   }
 };
 
-template <int DH, int H, bool PLANNED>
+template <int DH, int H>
 __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a) {
   constexpr int C = DH / 4, R = 256 / C;   // threads across a row, streams of parts in a workgroup
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -389,21 +402,8 @@ __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a) {
   const int b = blockIdx.x / groups, h0 = (blockIdx.x - b * groups) * H;
   const int c = threadIdx.x % C;
   uint16_t* out = a.out + b * a.out_stride + c * 4;
-  const int n_pages = pages_of(ctx_of(a, b));
-  if (n_pages == 0) return;
-  int n, before = 0;
-  if (PLANNED) {
-    before = a.starts[b];
-    n = a.starts[b + 1] - before;
-    if (n == 1) return;
-  } else {
-    const int target = decode_target(a, lane);
-    n = kv8_parts(n_pages, target);
-    if (n == 1) return;
-    for (int i0 = 0; i0 < b; i0 += kWave)
-      before += __builtin_amdgcn_readlane(
-          wave_scan(i0 + lane < b ? kv8_parts(pages_of(ctx_of(a, i0 + lane)), target) : 0), 63);
-  }
+  const int before = a.starts[b], n = a.starts[b + 1] - before;
+  if (n <= 1) return;
   const int G = a.Hq / a.Hkv;
   const float2* ml = reinterpret_cast<const float2*>(a.ws + a.ws_ml);
   const float* o = reinterpret_cast<const float*>(a.ws) + c * 4;
@@ -1230,9 +1230,9 @@ static hipError_t decode_launch(const Kv8AttnArgs& a, hipStream_t st) {
   if (a.bt_stride <= kKv8MinPages) return hipSuccess;   // no context is longer than a part
   const int64_t quads = (int64_t)a.S * ((a.Hq + 3) / 4);
   if (quads < kCus && a.bt_stride > kMergeAlone * kKv8MinPages)
-    hipLaunchKernelGGL((kv8_merge_kernel<DH, 1, PLANNED>), dim3((unsigned)(a.S * a.Hq)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((kv8_merge_kernel<DH, 1>), dim3((unsigned)(a.S * a.Hq)), dim3(256), 0, st, a);
   else
-    hipLaunchKernelGGL((kv8_merge_kernel<DH, 4, PLANNED>), dim3((unsigned)quads), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((kv8_merge_kernel<DH, 4>), dim3((unsigned)quads), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
