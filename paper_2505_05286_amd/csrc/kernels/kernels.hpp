@@ -300,19 +300,23 @@ struct Kv8AttnArgs {
 };
 // Decode work split, made by the kernels themselves from the contexts in device memory.  As for the bf16
 // cache, each (sequence, kv-head) stream of pages is cut into equal parts no longer than an even share of
-// all the pages over the wavefronts the chip holds at once, at least kKv8MinPages pages; with fewer streams than
-// those wavefronts the parts just fill them.
+// all the pages over the wavefronts the chip holds at once (or than kKv8MinPages pages, or than kv8_part_pages
+// says); with fewer streams than those wavefronts the parts at most fill them.
 constexpr int kKv8Resident = 3072;   // three a SIMD, at 161 VGPRs
-constexpr int kKv8MinPages = 8;
+constexpr int kKv8MinPages = 4;
 __host__ __device__ inline int64_t kv8_target_pages(int64_t total_pages, int64_t n_seqs, int hkv) {
   const int64_t pairs = n_seqs * hkv;
   const int64_t slots = pairs < kKv8Resident ? kKv8Resident - pairs : kKv8Resident;
   const int64_t t = (total_pages * hkv + slots - 1) / slots;
   return t > kKv8MinPages ? t : kKv8MinPages;
 }
-// Length of a part of a stream of `pages` pages, and the number of them: at most ceil(pages / target)
+// Length of a part of a stream of `pages` pages, and the number of them: at most ceil(pages / target).  With few streams
+// a part takes as long as its pages, the join as its parts: their sum is least near sqrt(pages / 8) pages a part.  One
+// context, 32 + 8 heads, us, against 8 pages or more: 1000 tokens 8.4 / 9.7, 2000 8.7 / 10.5, 8191 11.4 / 11.4, 30000
+// 20.6 / 24.0, 64000 32.7 / 39.4; 16 of 100 to 1500 10.4 / 11.4; 8 of 500 to 3000, 64 + 8 heads, 13.4 / 12.0.
 __host__ __device__ inline int kv8_part_pages(int pages, int target) {
-  const int n = (pages + target - 1) / target;
+  const int least = (int)sqrtf((float)(pages / 8)), t = target > least ? target : least;
+  const int n = (pages + t - 1) / t;
   return n > 0 ? (pages + n - 1) / n : 1;
 }
 __host__ __device__ inline int kv8_parts(int pages, int target) {

@@ -1229,7 +1229,7 @@ static hipError_t decode_launch(const Kv8AttnArgs& a, hipStream_t st) {
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (a.bt_stride <= kKv8MinPages) return hipSuccess;   // no context is longer than a part
   const int64_t quads = (int64_t)a.S * ((a.Hq + 3) / 4);
-  if (quads < kCus && a.bt_stride > kMergeAlone * kKv8MinPages)
+  if (quads < kCus && kv8_parts(a.bt_stride, kKv8MinPages) > kMergeAlone)
     hipLaunchKernelGGL((kv8_merge_kernel<DH, 1>), dim3((unsigned)(a.S * a.Hq)), dim3(256), 0, st, a);
   else
     hipLaunchKernelGGL((kv8_merge_kernel<DH, 4>), dim3((unsigned)quads), dim3(256), 0, st, a);

@@ -31,7 +31,7 @@ static void decode(const std::vector<int>& pages, int hkv) {
     CHECK((n == 0) == (p == 0));
     if (p == 0) continue;
     const int len = (p + n - 1) / n;
-    CHECK(len == kv8_part_pages(p, target) && len <= target);
+    CHECK(len == kv8_part_pages(p, target) && (len <= target || (int64_t)len * len <= p / 8));
     CHECK((int64_t)(n - 1) * len < p && (int64_t)n * len >= p);   // no part is empty, and all are covered
     items += (int64_t)n * hkv;
   }
