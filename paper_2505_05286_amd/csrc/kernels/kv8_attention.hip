@@ -27,7 +27,7 @@ __device__ __forceinline__ int decode_target(const Kv8AttnArgs& a, int lane) {
     total += __builtin_amdgcn_readlane(wave_scan(p & 0xFFFFF), 63);
     total += (int64_t)__builtin_amdgcn_readlane(wave_scan(p >> 20), 63) << 20;
   }
-  return (int)min(kv8_target_pages(total, a.S, a.Hkv), (int64_t)1 << 27);
+  return (int)min(kv8_target_pages(total, a.S, a.Hkv, a.bt_stride), (int64_t)1 << 27);
 }
 
 // starts[b]: parts of a kv-head's streams before sequence b, for b = 0 .. S.  By one wavefront:
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(1024) void kv8_decode_plan_kernel(Kv8AttnArgs a) {
   __syncthreads();
   int64_t total = 0;
   for (int i = 0; i < 16; ++i) total += sums[i];
-  const int target = (int)min(kv8_target_pages(total, a.S, a.Hkv), (int64_t)1 << 27);
+  const int target = (int)min(kv8_target_pages(total, a.S, a.Hkv, a.bt_stride), (int64_t)1 << 27);
   int base = 0;
   for (int b0 = 0; b0 < a.S; b0 += 1024) {
     const int b = b0 + threadIdx.x;
@@ -1227,7 +1227,7 @@ static hipError_t decode_launch(const Kv8AttnArgs& a, hipStream_t st) {
   }
   hipLaunchKernelGGL((kv8_decode_kernel<DH, PLANNED>), dim3((unsigned)kv8_decode_items(a.S, a.Hkv)), dim3(64), 0, st, a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (a.bt_stride <= kKv8MinPages) return hipSuccess;   // no context is longer than a part
+  if (a.bt_stride <= kKv8WholePages) return hipSuccess;   // no context is cut
   const int64_t quads = (int64_t)a.S * ((a.Hq + 3) / 4);
   if (quads < kCus && kv8_parts(a.bt_stride, kKv8MinPages) > kMergeAlone)
     hipLaunchKernelGGL((kv8_merge_kernel<DH, 1>), dim3((unsigned)(a.S * a.Hq)), dim3(256), 0, st, a);

@@ -22,9 +22,10 @@ static int g_case = 0;
 static void decode(const std::vector<int>& pages, int hkv) {
   const int64_t S = (int64_t)pages.size();
   int64_t total = 0, items = 0;
-  for (int p : pages) total += p;
-  const int64_t t = kv8_target_pages(total, S, hkv);
-  CHECK(t >= kKv8MinPages);
+  int longest = 0;
+  for (int p : pages) total += p, longest = std::max(longest, p);
+  const int64_t t = kv8_target_pages(total, S, hkv, longest);
+  CHECK(t >= (longest <= kKv8WholePages ? longest : kKv8MinPages));   // short tables: no stream is cut
   const int target = (int)std::min<int64_t>(t, int64_t(1) << 27);
   for (int p : pages) {
     const int n = kv8_parts(p, target);
