@@ -351,13 +351,14 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
   for (int i = lane * 8; i < a.Hq * DH; i += 64 * 8) *reinterpret_cast<uint4*>(out + i) = make_uint4(0, 0, 0, 0);
 }
 
-// Joins the parts of a sequence's heads, H (4 or 1) heads a workgroup.  A thread owns four dimensions and every R-th
-// part, four of them in flight, with a running maximum.  With four heads and up to kMergeAlone parts each wavefront joins
-// a head of its own; otherwise the workgroup takes its heads in turn and its streams meet in LDS.  H is 1 where four
-// heads a workgroup would leave CUs without one and the tables are long enough for more parts than that.  64 sequences
-// of up to 11 parts: 4.7 us (H = 1: 7.7); a lone context of 64 parts: 4.7 us with H = 1, 9.5 with 4, 17.2 with a
-// wavefront for each head.
+// Joins the parts of a sequence's heads.  A thread owns four dimensions and every R-th part, four of them in flight, with a
+// running maximum; the streams of a wavefront meet by exchanges between lanes, those of wavefronts in LDS.  A wavefront
+// takes a head, unless that would leave CUs without a workgroup and the tables are long enough for more than kMergeAlone
+// parts: then a workgroup takes a head, or, with up to kMergeWide such workgroups, a quarter of its dimensions.
+// 64 sequences of up to 11 parts: 4.7 us (a workgroup a head: 7.7).  Both launches for a context of 30000 tokens (118
+// parts): 17.8 us with quarters, 19.9 with whole heads; 64000 29.5 / 32.7; 16 contexts of 100 to 1500 11.2 / 10.4.
 constexpr int kMergeAlone = 16;
+constexpr int kMergeWide = 1024;
 template <int DH>
 struct MergeState {
   float M = kLowest, L = 0.f;
@@ -392,52 +393,68 @@ struct MergeState {
     const float inv = L == 0.f ? 0.f : 1.f / L;
     *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf2(acc.x * inv, acc.y * inv), pack_bf2(acc.z * inv, acc.w * inv));
   }
+  // streams of lanes X, 2 X, ... apart, into each of them
+  template <int X>
+  __device__ __forceinline__ void fold_lanes() {
+#pragma unroll
+    for (int x = X; x < kWave; x *= 2) {
+      const float2 v = make_float2(__shfl_xor(M, x, kWave), __shfl_xor(L, x, kWave));
+      const float4 y = make_float4(__shfl_xor(acc.x, x, kWave), __shfl_xor(acc.y, x, kWave), __shfl_xor(acc.z, x, kWave),
+                                   __shfl_xor(acc.w, x, kWave));
+      fold(v, y);
+    }
+  }
 };
 
-template <int DH, int H>
+// The parts of `head` of sequence b: their number, and the first one's place
+__device__ __forceinline__ int merge_parts(const Kv8AttnArgs& a, int b, int head, size_t& first) {
+  const int before = a.starts[b], n = a.starts[b + 1] - before, G = a.Hq / a.Hkv;
+  first = ((size_t)before * a.Hkv + (size_t)(head / G) * n) * G + head % G;
+  return n;
+}
+
+// A head a wavefront
+template <int DH>
 __global__ __launch_bounds__(256) void kv8_merge_kernel(Kv8AttnArgs a) {
-  constexpr int C = DH / 4, R = 256 / C;   // threads across a row, streams of parts in a workgroup
+  constexpr int C = DH / 4;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int groups = (a.Hq + H - 1) / H;
-  const int b = blockIdx.x / groups, h0 = (blockIdx.x - b * groups) * H;
-  const int c = threadIdx.x % C;
-  uint16_t* out = a.out + b * a.out_stride + c * 4;
-  const int before = a.starts[b], n = a.starts[b + 1] - before;
+  const int groups = (a.Hq + 3) / 4, b = blockIdx.x / groups, head = (blockIdx.x - b * groups) * 4 + w;
+  if (head >= a.Hq) return;
+  size_t f;
+  const int n = merge_parts(a, b, head, f);
   if (n <= 1) return;
-  const int G = a.Hq / a.Hkv;
-  const float2* ml = reinterpret_cast<const float2*>(a.ws + a.ws_ml);
-  const float* o = reinterpret_cast<const float*>(a.ws) + c * 4;
-  auto first = [&](int head) { return ((size_t)before * a.Hkv + (size_t)(head / G) * n) * G + head % G; };
-  if (H == 4 && n <= kMergeAlone) {
-    if (h0 + w >= a.Hq) return;
-    const size_t f = first(h0 + w);
-    MergeState<DH> S;
-    S.take(ml + f, o + f * DH, G, n, lane / C, kWave / C);
-#pragma unroll
-    for (int x = C; x < kWave; x *= 2) {
-      const float2 v = make_float2(__shfl_xor(S.M, x, kWave), __shfl_xor(S.L, x, kWave));
-      const float4 y = make_float4(__shfl_xor(S.acc.x, x, kWave), __shfl_xor(S.acc.y, x, kWave),
-                                   __shfl_xor(S.acc.z, x, kWave), __shfl_xor(S.acc.w, x, kWave));
-      S.fold(v, y);
-    }
-    if (lane < C) S.write(out + (h0 + w) * DH);
-    return;
-  }
-  __shared__ float2 s_ml[H][R];
-  __shared__ float4 s_acc[H][R][C];
-  const int r = threadIdx.x / C;
-  for (int i = 0; i < H && h0 + i < a.Hq; ++i) {
-    const size_t f = first(h0 + i);
-    MergeState<DH> S;
-    S.take(ml + f, o + f * DH, G, n, r, R);
-    if (c == 0) s_ml[i][r] = make_float2(S.M, S.L);
-    s_acc[i][r][c] = S.acc;
+  const int c = lane % C;
+  MergeState<DH> S;
+  S.take(reinterpret_cast<const float2*>(a.ws + a.ws_ml) + f, reinterpret_cast<const float*>(a.ws) + f * DH + c * 4,
+         a.Hq / a.Hkv, n, lane / C, kWave / C);
+  S.template fold_lanes<C>();
+  if (lane < C) S.write(a.out + b * a.out_stride + head * DH + c * 4);
+}
+
+// DH / Q dimensions of a head a workgroup
+template <int DH, int Q>
+__global__ __launch_bounds__(256) void kv8_merge_wide_kernel(Kv8AttnArgs a) {
+  constexpr int C = DH / 4 / Q;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = blockIdx.x / Q, b = i / a.Hq, head = i - b * a.Hq;
+  size_t f;
+  const int n = merge_parts(a, b, head, f);
+  if (n <= 1) return;
+  const int c = lane % C, d = (blockIdx.x % Q * C + c) * 4;
+  __shared__ float2 s_ml[4];
+  __shared__ float4 s_acc[4][C];
+  MergeState<DH> S;
+  S.take(reinterpret_cast<const float2*>(a.ws + a.ws_ml) + f, reinterpret_cast<const float*>(a.ws) + f * DH + d,
+         a.Hq / a.Hkv, n, threadIdx.x / C, 256 / C);
+  S.template fold_lanes<C>();
+  if (lane < C) {
+    if (lane == 0) s_ml[w] = make_float2(S.M, S.L);
+    s_acc[w][lane] = S.acc;
   }
   __syncthreads();
-  if (w >= H || h0 + w >= a.Hq || lane >= C) return;
-  MergeState<DH> S;
-  for (int j = 0; j < R; ++j) S.fold(s_ml[w][j], s_acc[w][j][lane]);
-  S.write(out + (h0 + w) * DH);
+  if (w > 0 || lane >= C) return;
+  for (int j = 1; j < 4; ++j) S.fold(s_ml[j], s_acc[j][lane]);
+  S.write(a.out + b * a.out_stride + head * DH + d);
 }
 
 // ------------------------------------------------------------------ prefill
@@ -1228,11 +1245,13 @@ static hipError_t decode_launch(const Kv8AttnArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((kv8_decode_kernel<DH, PLANNED>), dim3((unsigned)kv8_decode_items(a.S, a.Hkv)), dim3(64), 0, st, a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (a.bt_stride <= kKv8WholePages) return hipSuccess;   // no context is cut
-  const int64_t quads = (int64_t)a.S * ((a.Hq + 3) / 4);
-  if (quads < kCus && kv8_parts(a.bt_stride, kKv8MinPages) > kMergeAlone)
-    hipLaunchKernelGGL((kv8_merge_kernel<DH, 1>), dim3((unsigned)(a.S * a.Hq)), dim3(256), 0, st, a);
+  const int64_t quads = (int64_t)a.S * ((a.Hq + 3) / 4), heads = (int64_t)a.S * a.Hq;
+  if (quads >= kCus || kv8_parts(a.bt_stride, kKv8MinPages) <= kMergeAlone)
+    hipLaunchKernelGGL((kv8_merge_kernel<DH>), dim3((unsigned)quads), dim3(256), 0, st, a);
+  else if (heads * 4 > kMergeWide)
+    hipLaunchKernelGGL((kv8_merge_wide_kernel<DH, 1>), dim3((unsigned)heads), dim3(256), 0, st, a);
   else
-    hipLaunchKernelGGL((kv8_merge_kernel<DH, 4>), dim3((unsigned)quads), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((kv8_merge_wide_kernel<DH, 4>), dim3((unsigned)heads * 4), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
