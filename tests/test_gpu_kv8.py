@@ -337,6 +337,19 @@ def test_decode_batches(B, hi, heads):
     _decode(cache, bt, ctx, hq, rng, what="batch")
 
 
+@pytest.mark.parametrize("B,hi,heads", [(10, 1300, (32, 8, 128)), (30, 1200, (14, 2, 64)), (300, 9000, (4, 2, 64)),
+                                        (70, 12000, (16, 2, 128)), (1, 30000, (4, 2, 64)), (1, 30000, (13, 1, 128))])
+def test_decode_joins_of_many_parts(B, hi, heads):
+    """One context of many parts among short ones: a wavefront, a workgroup and a quarter of a head at a time."""
+    hq, hkv, dh = heads
+    rng = np.random.default_rng(B + hi)
+    ctx = rng.integers(1, 90, B)
+    ctx[B // 3] = hi
+    ctx[-1:] = hi // 2
+    cache, bt = _attention_case(rng, ctx, hq, hkv, dh)
+    _decode(cache, bt, ctx, hq, rng, o_pad=8, what="joins")
+
+
 def test_decode_entries_that_are_no_page():
     """Entries out of range inside a context are neither read nor weighted; a context of nothing else is empty; a
     context longer than the table's row, or negative, is cut."""
