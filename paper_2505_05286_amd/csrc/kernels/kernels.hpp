@@ -302,7 +302,7 @@ struct Kv8AttnArgs {
 // cache, each (sequence, kv-head) stream of pages is cut into equal parts no longer than an even share of
 // all the pages over the wavefronts the chip holds at once (or than kKv8MinPages pages, or than kv8_part_pages
 // says); with fewer streams than those wavefronts the parts at most fill them.
-constexpr int kKv8Resident = 3072;   // three a SIMD, at 161 VGPRs
+constexpr int kKv8Resident = 3 * 1024;   // three a SIMD, at 162 VGPRs
 constexpr int kKv8MinPages = 4;
 constexpr int kKv8WholePages = 8;    // with tables this short no stream is cut, and there is no join: 20 contexts of up
                                      // to 60 tokens 4.9 us, with parts and a join 6.3
