@@ -225,12 +225,11 @@ int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_p
                                 void* stream);
 
 /* Causal prefill attention over the 8-bit cache: sequence s's queries are the rows row0[s] .. row0[s+1] - 1 of q
- * (row0 [S+1] ascending, on the device, as hxf_op_slot_map makes it; taken as in [0, T]; the
- * outputs of one that does not ascend are undefined, its rows within [0, T)) at positions
- * pos0[s], pos0[s]+1, ... (pos0 on the device); each attends to the positions up to its own through bt[s],
- * whose keys are in the cache already.  Rows of no sequence are left as they are in out.  Positions from
- * 16 bt_stride on are not in the cache: no key there is seen.  NaN in the cache (a value that
- * was not finite) reaches the queries that see it and no other.  Bad entries, strides and workspace as for
+ * (row0 [S+1] ascending, on the device, as hxf_op_slot_map makes it; taken as in [0, T]; where it does not ascend
+ * the T rows of out are undefined) at positions pos0[s], pos0[s]+1, ... (pos0 on the device); each attends to the
+ * positions up to its own through bt[s], whose keys are in the cache already.  Rows of no sequence are left as they
+ * are in out.  Positions from 16 bt_stride on are not in the cache: no key there is seen.  NaN in the cache (a value
+ * that was not finite) reaches the queries that see it and no other.  Bad entries, strides and workspace as for
  * hxf_op_decode_attention_kv8. */
 int64_t hxf_op_prefill_attention_kv8_workspace_bytes(int32_t S, int32_t T, int32_t Hq, int32_t Hkv, int32_t head_dim);
 int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_pool* pool, const int32_t* bt,

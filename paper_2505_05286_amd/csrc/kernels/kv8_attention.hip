@@ -956,7 +956,8 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     return half_swap_max(v) * scale_log2;
   };
   // NaN in V of a tile with masked keys (one that some pairs see and others do not, or a place past the context, which
-  // may hold anything): a weight of zero would spread it to pairs that do not see its key.  So the tile's NaN become zeros in LDS, and infinities are added where a pair sees one, as
+  // may hold anything): a weight of zero would spread it to pairs that do not see its key.  So the tile's NaN become
+  // zeros in LDS, and infinities are added where a pair sees one, as
   //   (2 where V is NaN)^T . (2^127 where the key is seen),
   // which the end turns into NaN: nothing else in the outputs is infinite.
   // Every wavefront looks at the whole tile, so all of them take the branch with the barriers, or none.  (V's codes are
