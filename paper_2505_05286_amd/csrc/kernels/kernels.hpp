@@ -295,7 +295,7 @@ struct Kv8AttnArgs {
   int Hq, Hkv, dh;
   float scale_log2;      // log2(e) / sqrt(dh)
   uint8_t* ws;
-  int64_t ws_ml;         // decode: offset of the partials' (maximum, sum) pairs
+  int64_t ws_ml;         // decode: offset of the shares of the parts
   int32_t* starts;       // decode: [B + 1] parts of a kv-head before each sequence
 };
 // Decode work split, made by the kernels themselves from the contexts in device memory.  As for the bf16

@@ -123,6 +123,17 @@ constexpr int kNoExp = -127;   // exponent of an entry that is no page
 __device__ __forceinline__ int exponent_of(float scale) { return (int)(__float_as_uint(scale) >> 23 & 255) - 127; }
 __device__ __forceinline__ float power_of_two(int e) { return e < -126 ? 0.f : __int_as_float((127 + e) << 23); }
 
+// A part of a stream, or of a block, leaves its outputs as the averages that they would be alone: no larger than V's values,
+// where its sums may pass fp32 (weights up to 2^15, any number of them, V scales up to 2^120).  Its share (m, l) goes with
+// them, l brought into [2^-13, 2^-12) by the power of two that m takes up: a join's sums, over fewer than 2^12 parts,
+// stay under the largest average then.  unit_share: what turns sums in units of 2^e into averages
+// (l is 1 or more).
+static_assert(kKv8Resident + 1 < 1 << 12 && kPrefillResident + 1 < 1 << 12, "parts of a stream, and of a block");
+__device__ __forceinline__ float unit_share(float l, int e) { return l == 0.f ? 0.f : __builtin_amdgcn_ldexpf(1.f, e) / l; }
+__device__ __forceinline__ float2 part_share(float m, float l) {
+  return make_float2(m + (float)__builtin_amdgcn_frexp_expf(l), __builtin_amdgcn_frexp_mantf(l) * 0x1p-12f);
+}
+
 template <int DH>
 struct Kv8State {
   f32x4 acc[DH / 16];   // tile (u, n): row r of the lane's column is dimension u*64 + r*4 + n
@@ -310,9 +321,8 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
   S.l += __shfl_xor(S.l, 32, kWave);
   if (!ok) return;
   // the lane's dimensions are u*64 + 16*rq + 4e + n: 16 successive ones for each u
-  const float unit = power_of_two(max(e_now, -126));
+  const float inv = unit_share(S.l, e_now);
   if (n_parts == 1) {
-    const float inv = S.l == 0.f ? 0.f : unit / S.l;
     uint16_t* o = a.out + b * a.out_stride + (kvh * G + col) * DH + rq * 16;
 #pragma unroll
     for (int u = 0; u < DH / 64; ++u) {
@@ -334,9 +344,9 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       *reinterpret_cast<float4*>(o + u * 64 + 4 * e) =
-          make_float4(S.acc[4 * u][e] * unit, S.acc[4 * u + 1][e] * unit, S.acc[4 * u + 2][e] * unit,
-                      S.acc[4 * u + 3][e] * unit);
-  if (rq == 0) reinterpret_cast<float2*>(a.ws + a.ws_ml)[slot] = make_float2(S.m, S.l);
+          make_float4(S.acc[4 * u][e] * inv, S.acc[4 * u + 1][e] * inv, S.acc[4 * u + 2][e] * inv,
+                      S.acc[4 * u + 3][e] * inv);
+  if (rq == 0) reinterpret_cast<float2*>(a.ws + a.ws_ml)[slot] = part_share(S.m, S.l);
 }
 
 template <int DH, bool PLANNED>
@@ -363,11 +373,14 @@ template <int DH>
 struct MergeState {
   float M = kLowest, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  // x: averages of a part, or (sums) what another stream summed up
+  template <bool SUMS>
   __device__ __forceinline__ void fold(float2 v, float4 x) {
     const float m = fmaxf(M, v.x);
-    const float sc = __builtin_amdgcn_exp2f(M - m), w = __builtin_amdgcn_exp2f(v.x - m);
+    const float sc = __builtin_amdgcn_exp2f(M - m), at_m = __builtin_amdgcn_exp2f(v.x - m);
+    const float l = at_m * v.y, w = SUMS ? at_m : l;
     M = m;
-    L = L * sc + w * v.y;
+    L = L * sc + l;
     acc.x = acc.x * sc + w * x.x;
     acc.y = acc.y * sc + w * x.y;
     acc.z = acc.z * sc + w * x.z;
@@ -386,7 +399,7 @@ struct MergeState {
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (j0 + u * R < n) fold(v[u], x[u]);
+        if (j0 + u * R < n) fold<false>(v[u], x[u]);
     }
   }
   __device__ __forceinline__ void write(uint16_t* out) const {
@@ -401,7 +414,7 @@ struct MergeState {
       const float2 v = make_float2(__shfl_xor(M, x, kWave), __shfl_xor(L, x, kWave));
       const float4 y = make_float4(__shfl_xor(acc.x, x, kWave), __shfl_xor(acc.y, x, kWave), __shfl_xor(acc.z, x, kWave),
                                    __shfl_xor(acc.w, x, kWave));
-      fold(v, y);
+      fold<true>(v, y);
     }
   }
 };
@@ -453,7 +466,7 @@ __global__ __launch_bounds__(256) void kv8_merge_wide_kernel(Kv8AttnArgs a) {
   }
   __syncthreads();
   if (w > 0 || lane >= C) return;
-  for (int j = 1; j < 4; ++j) S.fold(s_ml[j], s_acc[j][lane]);
+  for (int j = 1; j < 4; ++j) S.template fold<true>(s_ml[j], s_acc[j][lane]);
   S.write(a.out + b * a.out_stride + head * DH + d);
 }
 
@@ -496,8 +509,8 @@ struct Kv8PrefillArgs {
   PrefillHead* head;
   PrefillUnit* units;
   PrefillJob* jobs;
-  float* part_o;    // [Hkv][slots][128 pairs][dh]: unnormalized
-  float* part_ml;   // [Hkv][slots][128 pairs][2]: (maximum in log2 units, sum)
+  float* part_o;    // [Hkv][slots][128 pairs][dh]: averages (part_share)
+  float* part_ml;   // [Hkv][slots][128 pairs][2]: their shares
   int unit_cap, slots, qpi;
   bool cuts;        // whether blocks may be cut
 };
@@ -1153,7 +1166,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     for (int e = 0; e < 16; ++e) o[dt][e] = fmaf(o[dt][e], 0.f, o[dt][e]);   // infinity to NaN (see spread_nan)
   const float lt = l + __shfl_xor(l, 32, kWave);
   if (!pair_ok) return;
-  const float unit = power_of_two(max(e_now, -126));
+  const float inv = unit_share(lt, e_now);
   if (it.slot >= 0) {
     const size_t slot = ((size_t)kvh * p.slots + it.slot) * kPrefillPairs + pair;
     float* po = p.part_o + slot * DH;
@@ -1162,11 +1175,10 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
 #pragma unroll
       for (int g4 = 0; g4 < 4; ++g4)
         *reinterpret_cast<float4*>(po + dt * 32 + g4 * 8 + h * 4) =
-            make_float4(o[dt][g4 * 4] * unit, o[dt][g4 * 4 + 1] * unit, o[dt][g4 * 4 + 2] * unit, o[dt][g4 * 4 + 3] * unit);
-    if (h == 0) *reinterpret_cast<float2*>(p.part_ml + slot * 2) = make_float2(m, lt);
+            make_float4(o[dt][g4 * 4] * inv, o[dt][g4 * 4 + 1] * inv, o[dt][g4 * 4 + 2] * inv, o[dt][g4 * 4 + 3] * inv);
+    if (h == 0) *reinterpret_cast<float2*>(p.part_ml + slot * 2) = part_share(m, lt);
     return;
   }
-  const float inv = lt == 0.f ? 0.f : unit / lt;
   uint16_t* out = a.out + row * a.out_stride + col0;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -1221,13 +1233,13 @@ __global__ __launch_bounds__(256) void kv8_prefill_merge_kernel(Kv8PrefillArgs p
     s_acc[row][c] = S.acc;
     __syncthreads();
     if (row % R == 0)
-      for (int j = 1; j < R; ++j) S.fold(s_ml[row + j], s_acc[row + j][c]);
+      for (int j = 1; j < R; ++j) S.template fold<true>(s_ml[row + j], s_acc[row + j][c]);
   });
 }
 
 }  // namespace
 
-// Partial outputs [items][G][dh], then their (maximum, sum) pairs, then the starts of the sequences
+// Partial outputs [items][G][dh], then their shares (part_share), then the starts of the sequences
 static int64_t decode_ml_offset(int B, int Hq, int Hkv, int dh) { return kv8_decode_items(B, Hkv) * (Hq / Hkv) * dh * 4; }
 static int64_t decode_starts_offset(int B, int Hq, int Hkv, int dh) {
   return decode_ml_offset(B, Hq, Hkv, dh) + kv8_decode_items(B, Hkv) * (Hq / Hkv) * 8;

@@ -807,3 +807,34 @@ def test_a_captured_step_of_all_operators(hq, hkv, dh):
         raw = cap["out"].cpu().numpy().reshape(T, -1)
         assert np.all(raw[~live] == 0x1234)
         start = ctx
+
+
+@pytest.mark.parametrize("spread", [122, -91])
+@pytest.mark.parametrize("flat", [False, True])
+@pytest.mark.parametrize("heads,ctx", [((8, 2, 128), [700, 3]), ((4, 2, 64), [3000, 40]), ((13, 1, 128), [30000]),
+                                       ((32, 8, 128), [1300, 20, 8, 500, 1, 16, 17, 90, 30, 1200])])
+def test_decode_of_the_largest_and_smallest_values_in_many_parts(heads, ctx, flat, spread):
+    """V scales up to 2^119 and down to 2^-100 in contexts that are cut, by each of the joins: the sums of a part may be far
+    larger than any value.  flat: all weights alike, so that they are largest."""
+    hq, hkv, dh = heads
+    rng = np.random.default_rng(sum(ctx) + flat)
+    cache, bt = _attention_case(rng, ctx, hq, hkv, dh)
+    cache.scale["v"][:] *= 2.0 ** spread
+    if flat:
+        cache.scale["k"][:] *= 2.0 ** -40
+    _decode(cache, bt, np.array(ctx), hq, rng, what=f"v 2^{spread}")
+
+
+@pytest.mark.parametrize("spread", [122, -91])
+@pytest.mark.parametrize("flat", [False, True])
+@pytest.mark.parametrize("heads,places", [((8, 2, 128), 0), ((4, 2, 64), 300), ((32, 8, 128), 300)])
+def test_prefill_of_the_largest_and_smallest_values_in_many_parts(heads, places, flat, spread):
+    """The same for blocks that are cut, planned by the workgroups and by a launch."""
+    hq, hkv, dh = heads
+    rng = np.random.default_rng(hq + places + flat)
+    pos0, n = np.array([700, 2900, 60] + [0] * places), np.array([20, 60, 9] + [0] * places)
+    cache, bt = _attention_case(rng, pos0 + n, hq, hkv, dh)
+    cache.scale["v"][:] *= 2.0 ** spread
+    if flat:
+        cache.scale["k"][:] *= 2.0 ** -40
+    _prefill(cache, bt, pos0, n, hq, rng, what=f"v 2^{spread}")
