@@ -243,21 +243,25 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
   const float* ksp = a.pool.ks + kvh * a.pool.n_blocks;
   const float* vsp = a.pool.vs + kvh * a.pool.n_blocks;
   // Tables of 64 pages, one page a lane: the numbers of the pages being loaded and of the 64 after them, and the
-  // scales of the pages being loaded and of those being multiplied.  A scale of 0 marks an entry that is no page.
+  // scales of the pages being loaded and of those being multiplied.  An entry that is no page reads page 0, whose tokens do
+  // not count.
   auto entries = [&](int r0) { return r0 + lane < np ? bt[r0 + lane] : -1; };
   int blk = entries(0), blk_next = entries(kWave);
   float ks_next, vs_next;
+  uint64_t gone_next;    // the entries that are no page
   int e_next = kNoExp;   // E of the tables being loaded; of those multiplied: e_now
   auto scales = [&]() {
     const bool there = (uint32_t)blk < (uint64_t)a.pool.n_blocks;
+    gone_next = __ballot(!there);
     if (!there) blk = 0;
-    ks_next = there ? ksp[blk] : 0.f;
+    ks_next = ksp[blk];
     const int e = there ? exponent_of(vsp[blk]) : kNoExp;
     e_next = max(e_next, wave_max(e));
     vs_next = power_of_two(e - e_next);
   };
   scales();
   float ks_now = ks_next, vs_now = vs_next;
+  uint64_t gone_now = gone_next;
   int e_now = e_next;
   Kv8State<DH> S;
 #pragma unroll
@@ -284,6 +288,7 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
     if (r && r % kWave == 0) {
       ks_now = ks_next;
       vs_now = vs_next;
+      gone_now = gone_next;
       if (e_now != e_next) {
         const float f = power_of_two(e_now - e_next);
 #pragma unroll
@@ -295,11 +300,10 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
     int cnt[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int s = __builtin_amdgcn_readlane(__float_as_int(ks_now), r % kWave + h);
-      const bool there = s != 0 && r + h < np;
-      ks[h] = there ? __int_as_float(s) : 1.f;
-      vs[h] = there ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs_now), r % kWave + h)) : 1.f;
-      cnt[h] = there ? min(kPage, n - (p0 + r + h) * kPage) : 0;
+      const int i = r % kWave + h;   // (past the part's last page: an entry that is none)
+      ks[h] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ks_now), i));
+      vs[h] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs_now), i));
+      cnt[h] = gone_now >> i & 1 ? 0 : min(kPage, n - (p0 + r + h) * kPage);
     }
     kv8_pair<DH>(S, P, qf, ks, vs, cnt, a.scale_log2, lane);
   };

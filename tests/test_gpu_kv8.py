@@ -838,3 +838,19 @@ def test_prefill_of_the_largest_and_smallest_values_in_many_parts(heads, places,
     if flat:
         cache.scale["k"][:] *= 2.0 ** -40
     _prefill(cache, bt, pos0, n, hq, rng, what=f"v 2^{spread}")
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(8, 2, 128), (4, 2, 64)])
+def test_pages_whose_scale_is_zero(hq, hkv, dh):
+    """A page whose stored scale is 0 (a pool that began as zeros) holds zeros: its keys score 0 and have their weight, its
+    values add nothing.  Only an entry that is no page has no weight."""
+    rng = np.random.default_rng(dh + 7)
+    ctx = np.array([1300, 16, 40, 33])
+    cache, bt = _attention_case(rng, ctx, hq, hkv, dh)
+    for s, p, kinds in ((0, 0, "k"), (0, 3, "kv"), (0, 64, "k"), (0, 70, "v"), (0, 81, "k"), (1, 0, "k"), (2, 1, "k"),
+                        (2, 2, "v"), (3, 0, "v"), (3, 1, "v"), (3, 2, "kv")):
+        for kind in kinds:
+            cache.scale[kind][:, bt[s, p]] = 0
+    bt[0, 5], bt[2, 0] = -1, cache.nb
+    _decode(cache, bt, ctx, hq, rng, what="scales of 0")
+    _prefill(cache, bt, ctx - np.array([30, 16, 17, 1]), np.array([30, 16, 17, 1]), hq, rng, what="scales of 0")
