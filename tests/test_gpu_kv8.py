@@ -854,3 +854,18 @@ def test_pages_whose_scale_is_zero(hq, hkv, dh):
     bt[0, 5], bt[2, 0] = -1, cache.nb
     _decode(cache, bt, ctx, hq, rng, what="scales of 0")
     _prefill(cache, bt, ctx - np.array([30, 16, 17, 1]), np.array([30, 16, 17, 1]), hq, rng, what="scales of 0")
+
+
+@pytest.mark.parametrize("S,hi_pos,hi_n,heads", [(300, 200, 20, (32, 8, 128)), (300, 2500, 2, (4, 2, 64)),
+                                                 (2, 900, 4300, (32, 8, 128))])
+def test_prefill_planned_by_a_launch_repeats_to_the_bit(S, hi_pos, hi_n, heads):
+    """The planning launch lists units in an order that atomics make: it does not show in the result."""
+    hq, hkv, dh = heads
+    rng = np.random.default_rng(S + hi_n)
+    pos0, n = rng.integers(0, hi_pos + 1, S), rng.integers(0, hi_n + 1, S)
+    pos0[0], n[0] = hi_pos, hi_n
+    if hi_n == 2:
+        pos0[5:], n[5:] = 0, 0                          # few queries over long contexts: cut
+    cache, bt = _attention_case(rng, pos0 + n, hq, hkv, dh)
+    out = [_outputs(cache, bt, pos0, n, hq, np.random.default_rng(5), False)[1] for _ in range(4)]
+    assert all(np.array_equal(o, out[0]) for o in out)
