@@ -206,7 +206,8 @@ int hxf_op_slot_map(const int32_t* start, const int32_t* n_new, int32_t S, const
  * before them stay: the scale is the larger of the page's and the new rows', and where it grows the old codes
  * are requantised.  Tokens behind the new rows are left as they are.  A row whose slot is not in [0, 16 n_blocks), or
  * (with a table) whose pos is not in [0, max_pos), is skipped, its q_out row included.
- * qkv and q_out 16-byte aligned, strides multiples of 8, T < 2^30; no buffer may overlap another. */
+ * qkv and q_out 16-byte aligned, strides multiples of 8, T <= 2^28 - 16, Hq + 2 Hkv < 2^16; no buffer may overlap
+ * another. */
 int hxf_op_rope_kv8_write(const void* qkv, int64_t qkv_stride, const int32_t* pos, const int32_t* slot,
                           const void* rope_table, int32_t max_pos, void* q_out, int64_t q_stride,
                           const hxf_kv8_pool* pool, int32_t T, int32_t Hq, int32_t Hkv, int32_t head_dim, void* stream);
@@ -217,7 +218,8 @@ int hxf_op_rope_kv8_write(const void* qkv, int64_t qkv_stride, const int32_t* po
  * zeros.  Tokens of a block-table entry that is no page of the pool are not read and have no weight.  Entries past
  * the context are not read.  q, out, the pool and the workspace must not overlap.  workspace:
  * hxf_op_decode_attention_kv8_workspace_bytes bytes, 16-byte aligned, whose contents need not be kept between
- * calls; calls that may overlap need one each. */
+ * calls; calls that may overlap need one each.  B * Hq < 2^29; B * Hkv < 2^26 - 3072; and, with bt_stride > 8,
+ * B * ceil(Hq / 4) < 2^24. */
 int64_t hxf_op_decode_attention_kv8_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t head_dim);
 int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_pool* pool, const int32_t* bt,
                                 int32_t bt_stride, const int32_t* ctx, void* out, int64_t out_stride, int32_t B,
@@ -230,7 +232,8 @@ int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_p
  * positions up to its own through bt[s], whose keys are in the cache already.  Rows of no sequence are left as they
  * are in out.  Positions from 16 bt_stride on are not in the cache: no key there is seen.  NaN in the cache (a value
  * that was not finite) reaches the queries that see it and no other.  Bad entries, strides and workspace as for
- * hxf_op_decode_attention_kv8. */
+ * hxf_op_decode_attention_kv8.  (S + T) * Hq < 2^29; and, with Q = floor(128 / (Hq / Hkv)) queries a block,
+ * (floor(T / Q) + S + 1) * Hkv < 2^24. */
 int64_t hxf_op_prefill_attention_kv8_workspace_bytes(int32_t S, int32_t T, int32_t Hq, int32_t Hkv, int32_t head_dim);
 int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_pool* pool, const int32_t* bt,
                                  int32_t bt_stride, const int32_t* row0, const int32_t* pos0, void* out,

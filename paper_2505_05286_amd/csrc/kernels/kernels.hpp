@@ -250,6 +250,9 @@ struct Kv8Pool {
 __host__ __device__ inline int k8_offset(int d, int t) { return ((d >> 4) * kPage + t) * 16 + (d & 15); }
 __host__ __device__ inline int v8_offset(int d, int t, int dh) { return ((t >> 2) * dh + d) * 4 + (t & 3); }
 
+// A launch counts its threads of each dimension in 32 bits
+inline bool launch_fits(int64_t groups, int threads) { return groups <= (int64_t)UINT32_MAX / threads; }
+
 constexpr int kSlotMapMaxSeqs = 4096;
 struct SlotMapArgs {
   const int32_t* start;
@@ -278,6 +281,11 @@ struct Kv8WriteArgs {
   Kv8Pool pool;
   int T, Hq, Hkv, dh;
 };
+constexpr int kWriteRows = 16;   // rows of a workgroup
+// (a workgroup of 256 for them and a head, or some q heads)
+inline bool kv8_write_fits(int64_t T, int64_t Hq, int64_t Hkv) {
+  return launch_fits((T + kWriteRows - 1) / kWriteRows, 256) && Hq + 2 * Hkv < (1 << 16);
+}
 hipError_t kv8_write_launch(const Kv8WriteArgs& a, hipStream_t st);
 
 struct Kv8AttnArgs {
@@ -332,6 +340,11 @@ inline int64_t kv8_decode_items(int64_t n_seqs, int hkv) {
   const int64_t pairs = n_seqs * hkv;
   return pairs < kKv8Resident ? kKv8Resident : kKv8Resident + pairs;
 }
+// Whether the launches hold a batch: the attention's, and the join's of four heads a workgroup
+inline bool kv8_decode_fits(int64_t n_seqs, int hkv) { return launch_fits(kv8_decode_items(n_seqs, hkv), 64); }
+inline bool kv8_decode_join_fits(int64_t n_seqs, int hq, int bt_stride) {
+  return bt_stride <= kKv8WholePages || launch_fits(n_seqs * ((hq + 3) / 4), 256);
+}
 // Prefill work split, made by a kernel from the rows and positions in device memory.  A block of up to 128 / G queries
 // of a sequence is one unit of work for every kv-head, over its key tiles of 32 positions (taken in pairs).  Where
 // whole blocks would be fewer than kPrefillCutUnits, all of a head's pairs, block after block, are dealt out in equal
@@ -385,6 +398,9 @@ inline int64_t kv8_prefill_unit_cap(int64_t S, int64_t T, int queries, int hkv) 
 inline int64_t kv8_prefill_slots(int64_t S, int64_t T, int queries, int hkv) {
   const int64_t cut = (kPrefillCutUnits + kPrefillResident) / hkv, whole = T / queries + S + kv8_prefill_streams(hkv);
   return (cut < whole ? cut : whole) + 1;
+}
+inline bool kv8_prefill_fits(int64_t S, int64_t T, int queries, int hkv) {
+  return launch_fits(kv8_prefill_unit_cap(S, T, queries, hkv) * hkv, 256);
 }
 int64_t kv8_decode_ws_bytes(int B, int Hq, int Hkv, int dh);
 hipError_t kv8_decode_launch(const Kv8AttnArgs& a, hipStream_t st);

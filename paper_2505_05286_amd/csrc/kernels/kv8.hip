@@ -259,8 +259,6 @@ __device__ __forceinline__ void kv8_write_run(const Kv8WriteArgs& a, int slot, i
   if (lane == 0) *scale = s;
 }
 
-constexpr int kWriteRows = 16;   // rows of a workgroup
-
 // The same for up to four runs of one row each (decode rows), side by side in the wavefront: K takes dh/16 lanes a row, V
 // 16.  mine: this lane has a row; slot, t, ps: its place, row and position.
 template <int DH>

@@ -449,6 +449,10 @@ bool rows_ok(const void* p, int64_t stride, int64_t width) {
 // (row, page, wavefront and grid indices are 32 bits wide)
 bool count_ok(int32_t n) { return n >= 0 && n < (1 << 30); }
 bool batch_ok(int64_t n, int Hq) { return n * Hq < (int64_t(1) << 29); }
+bool decode_ok(int32_t B, int Hq, int Hkv) { return batch_ok(B, Hq) && kv8_decode_fits(B, Hkv); }
+bool prefill_ok(int32_t S, int32_t T, int Hq, int Hkv) {
+  return batch_ok((int64_t)S + T, Hq) && kv8_prefill_fits(S, T, prefill_queries_per_item(Hq / Hkv), Hkv);
+}
 
 bool table_ok(const int32_t* bt, int32_t bt_stride) { return bt && bt_stride > 0 && bt_stride < (1 << 26); }
 
@@ -483,7 +487,8 @@ int hxf_op_slot_map(const int32_t* start, const int32_t* n_new, int32_t S, const
 int hxf_op_rope_kv8_write(const void* qkv, int64_t qkv_stride, const int32_t* pos, const int32_t* slot,
                           const void* rope_table, int32_t max_pos, void* q_out, int64_t q_stride,
                           const hxf_kv8_pool* pool, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh, void* stream) {
-  if (!count_ok(T) || !shapes_ok(Hq, Hkv, dh) || !pool_ok(pool) || !slot) return HXF_EINVAL;
+  if (!count_ok(T) || !shapes_ok(Hq, Hkv, dh) || !kv8_write_fits(T, Hq, Hkv) || !pool_ok(pool) || !slot)
+    return HXF_EINVAL;
   if (!rows_ok(qkv, qkv_stride, (int64_t)(Hq + 2 * Hkv) * dh) || (q_out && !rows_ok(q_out, q_stride, (int64_t)Hq * dh)))
     return HXF_EINVAL;
   if (rope_table && (!pos || max_pos <= 0 || !aligned16(rope_table))) return HXF_EINVAL;
@@ -506,7 +511,7 @@ int hxf_op_rope_kv8_write(const void* qkv, int64_t qkv_stride, const int32_t* po
 }
 
 int64_t hxf_op_decode_attention_kv8_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t dh) {
-  if (B < 0 || !shapes_ok(Hq, Hkv, dh) || !batch_ok(B, Hq)) return -1;
+  if (B < 0 || !shapes_ok(Hq, Hkv, dh) || !decode_ok(B, Hq, Hkv)) return -1;
   return kv8_decode_ws_bytes(B, Hq, Hkv, dh);
 }
 
@@ -514,7 +519,8 @@ int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_p
                                 int32_t bt_stride, const int32_t* ctx, void* out, int64_t out_stride, int32_t B,
                                 int32_t Hq, int32_t Hkv, int32_t dh, void* workspace, int64_t ws_bytes, void* stream) {
   if (B < 0 || !shapes_ok(Hq, Hkv, dh) || !pool_ok(pool) || !table_ok(bt, bt_stride) || !ctx ||
-      !rows_ok(q, q_stride, (int64_t)Hq * dh) || !rows_ok(out, out_stride, (int64_t)Hq * dh) || !batch_ok(B, Hq))
+      !rows_ok(q, q_stride, (int64_t)Hq * dh) || !rows_ok(out, out_stride, (int64_t)Hq * dh) ||
+      !decode_ok(B, Hq, Hkv) || !kv8_decode_join_fits(B, Hq, bt_stride))
     return HXF_EINVAL;
   if (B == 0) return HXF_OK;
   if (!workspace || !aligned16(workspace) || ws_bytes < kv8_decode_ws_bytes(B, Hq, Hkv, dh)) return HXF_ENOMEM;
@@ -537,7 +543,7 @@ int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_p
 }
 
 int64_t hxf_op_prefill_attention_kv8_workspace_bytes(int32_t S, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh) {
-  if (S < 0 || T < 0 || !shapes_ok(Hq, Hkv, dh) || !batch_ok((int64_t)S + T, Hq)) return -1;
+  if (S < 0 || T < 0 || !shapes_ok(Hq, Hkv, dh) || !prefill_ok(S, T, Hq, Hkv)) return -1;
   return kv8_prefill_ws_bytes(S, T, Hq, Hkv, dh);
 }
 
@@ -547,7 +553,7 @@ int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_
                                  void* workspace, int64_t ws_bytes, void* stream) {
   if (S < 0 || T < 0 || !shapes_ok(Hq, Hkv, dh) || !pool_ok(pool) || !table_ok(bt, bt_stride) || !row0 || !pos0 ||
       !rows_ok(q, q_stride, (int64_t)Hq * dh) || !rows_ok(out, out_stride, (int64_t)Hq * dh) ||
-      !batch_ok((int64_t)S + T, Hq))
+      !prefill_ok(S, T, Hq, Hkv))
     return HXF_EINVAL;
   if (S == 0 || T == 0) return HXF_OK;
   if (!workspace || !aligned16(workspace) || ws_bytes < kv8_prefill_ws_bytes(S, T, Hq, Hkv, dh)) return HXF_ENOMEM;

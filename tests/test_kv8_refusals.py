@@ -190,3 +190,32 @@ def test_attention_of_one_key_is_its_value():
     np.testing.assert_allclose(o[0, 1], c.values("v", 0, [1])[0], rtol=1e-15)
     o, _ = U.attend(np.ones((1, 2, 64)), c, [-1], 16, 2)
     assert np.all(o == 0)
+
+
+# ------------------------------------------------------------------ launches
+def test_launch_limits(tmp_path):
+    """tests/kv8_limits.cpp: the batches that the operators accept are those that their launches hold."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "kv8_limits")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                    "-I" + os.path.join(root, "paper_2505_05286_amd", "csrc"),
+                    os.path.join(root, "tests", "kv8_limits.cpp"), "-o", exe], check=True, capture_output=True,
+                   timeout=300)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
+def test_batches_whose_launch_would_pass_32_bits_of_threads_are_refused():
+    """With HXF_EINVAL, before anything is enqueued, and with no size of a workspace for them."""
+    wide = dict(qkv_stride=1 << 30, q_stride=1 << 30)
+    for bad in (dict(T=(1 << 28) - 15), dict(T=1 << 29), dict(Hq=1 << 16, Hkv=1 << 16, **wide),
+                dict(Hq=1 << 30, Hkv=1 << 30, qkv_stride=1 << 40, q_stride=1 << 40)):
+        _refused(hxf.EINVAL, _write, **bad)
+    one = dict(Hq=1, Hkv=1, dh=64)
+    _refused(hxf.EINVAL, _decode, B=(1 << 26) - 3072, bt_stride=4, **one)
+    _refused(hxf.EINVAL, _decode, B=1 << 24, bt_stride=9, **one)
+    _refused(hxf.EINVAL, _prefill, S=(1 << 24) - 1, T=1, **one)
+    assert hxf.op_decode_attention_kv8_workspace_bytes((1 << 26) - 3072, 1, 1, 64) == -1
+    assert hxf.op_decode_attention_kv8_workspace_bytes((1 << 26) - 3073, 1, 1, 64) > 0
+    assert hxf.op_prefill_attention_kv8_workspace_bytes((1 << 24) - 1, 1, 1, 1, 64) == -1
+    assert hxf.op_prefill_attention_kv8_workspace_bytes((1 << 24) - 2, 1, 1, 1, 64) > 0
