@@ -395,6 +395,11 @@ inline int64_t kv8_prefill_unit_cap(int64_t S, int64_t T, int queries, int hkv) 
   const int64_t cut = (kPrefillCutUnits + kPrefillResident) / hkv, whole = T / queries + S;
   return (cut > whole ? cut : whole) + 1;
 }
+// Blocks that the planning launch takes from its next sequences, which have `more`, after `before` others: all of them where
+// row0 ascends.  Where it does not they might pass any count (each sequence may have T rows): they end with the units.
+__host__ __device__ inline int kv8_prefill_take(int before, int more, int unit_cap) {
+  return more < unit_cap - before ? more : unit_cap - before;
+}
 inline int64_t kv8_prefill_slots(int64_t S, int64_t T, int queries, int hkv) {
   const int64_t cut = (kPrefillCutUnits + kPrefillResident) / hkv, whole = T / queries + S + kv8_prefill_streams(hkv);
   return (cut < whole ? cut : whole) + 1;

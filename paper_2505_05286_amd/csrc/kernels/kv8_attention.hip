@@ -734,6 +734,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
       const int before = plan_scan(lds, (n + p.qpi - 1) / p.qpi, total);
       lds.pre[tid] = before;
       __syncthreads();
+      total = kv8_prefill_take(base, total, p.unit_cap);
       for (int i = tid; i < total; i += kPlanThreads) {
         const int s = last_at(lds.pre, min(kPlanThreads, a.S - s0), i);
         const int m = plan_rows(a, s0 + s, r0);
@@ -760,15 +761,14 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
       at += n;
     }
     __syncthreads();
-    const int n_units = min(n_blocks, p.unit_cap);
-    const int half = kPrefillResident / 2 / a.Hkv, window = min(n_units, kPrefillResident / a.Hkv);
+    const int half = kPrefillResident / 2 / a.Hkv, window = min(n_blocks, kPrefillResident / a.Hkv);
     blocks([&](const PrefillUnit& u, int) {
       int i = atomicAdd(&bins[bin_of(u.t1)], 1);
       if (i >= half && i < window) i = half + window - 1 - i;
-      if (i < p.unit_cap) p.units[i] = u;
+      p.units[i] = u;
     });
     if (tid == 0) {
-      p.head->n_units = n_units;
+      p.head->n_units = n_blocks;
       p.head->n_jobs = 0;
     }
     return;

@@ -28,5 +28,22 @@ int main() {
   // prefill: four wavefronts for each unit and head
   CHECK(kv8_prefill_fits(k24 - 2, 0, 128, 1) && !kv8_prefill_fits(k24 - 1, 0, 128, 1));
   CHECK(kv8_prefill_fits(1000, 32 * (k24 / 8 - 1002), 32, 8) && !kv8_prefill_fits(1000, 32 * (k24 / 8 - 1001), 32, 8));
+  // the planning launch's blocks where row0 goes up and down between 0 and T: S / 2 sequences of T rows
+  const int64_t S = 1 << 15, T = 1 << 20;
+  const int q = 8, cap = (int)kv8_prefill_unit_cap(S, T, q, 1);
+  int64_t all = 0;
+  int base = 0;
+  for (int64_t s = 0; s < S; s += 256) {
+    const int more = (int)(128 * (T / q));
+    all += more;
+    base += kv8_prefill_take(base, more, cap);
+    CHECK(base >= 0 && base <= cap);
+  }
+  CHECK(all > INT32_MAX && base == cap);
+  // and where it ascends: all of them, whatever the lengths are
+  for (int64_t n = 1; n < 3000; n = n * 3 + 1) {
+    const int64_t rows = n * 300, blocks = 300 * ((n + q - 1) / q);
+    CHECK(kv8_prefill_take(0, (int)blocks, (int)kv8_prefill_unit_cap(300, rows, q, 8)) == blocks);
+  }
   std::puts("ok");
 }

@@ -869,3 +869,33 @@ def test_prefill_planned_by_a_launch_repeats_to_the_bit(S, hi_pos, hi_n, heads):
     cache, bt = _attention_case(rng, pos0 + n, hq, hkv, dh)
     out = [_outputs(cache, bt, pos0, n, hq, np.random.default_rng(5), False)[1] for _ in range(4)]
     assert all(np.array_equal(o, out[0]) for o in out)
+
+
+@pytest.mark.parametrize("hi_ctx", [100, 2500])
+def test_prefill_planned_blocks_of_a_row0_that_goes_up_and_down_are_bounded(hi_ctx):
+    """A thousand sequences that each claim all rows: the planning launch takes no more blocks than it has units for,
+    nothing is written past the workspace or out, and the next call on the same workspace is right."""
+    t = torch()
+    rng = np.random.default_rng(hi_ctx)
+    S, T, heads = 2000, 2048, (16, 1, 64)
+    cache, bt = _attention_case(rng, [hi_ctx] * 2, *heads)
+    bt = bt[np.arange(S) % 2]
+    dev = DevCache(cache)
+    bits, qf = rand_bf16(rng, (T, 16, 64))
+    q, d_bt, pos0 = dev_bits(bits), i32(bt), i32(np.full(S, hi_ctx - 90))
+    out = dev_bits(np.full((T + 8, 1024), 0x1234, np.uint16))
+    m = hxf.op_prefill_attention_kv8_workspace_bytes(S, T, *heads)
+    ws = t.full((m + (16 << 20),), 0x5A, dtype=t.uint8, device="cuda:0")
+    up_down, up = np.arange(S + 1) % 2 * T, np.minimum(np.arange(S + 1), 90)
+    for row0 in (up_down, up):
+        d_row0 = i32(row0)
+        log(f"prefill kv8 row0 up and down: S={S} T={T} rows {row0[:3].tolist()}")
+        hxf.op_prefill_attention_kv8(q.data_ptr(), 1024, dev.pool, d_bt.data_ptr(), bt.shape[1], d_row0.data_ptr(),
+                                     pos0.data_ptr(), out.data_ptr(), 1024, S, T, *heads, ws.data_ptr(), m)
+        t.cuda.synchronize()
+    assert bool((ws[m:] == 0x5A).all())
+    assert np.all(out.cpu().numpy().view(np.uint16)[T:] == 0x1234)
+    got = host_f64(out).reshape(-1, 16, 64)
+    for s in (0, 1, 57, 89):
+        ref, size = U.attend(qf[s:s + 1], cache, bt[s], hi_ctx - 89, 16, first=hi_ctx - 90)
+        U.assert_attention(got[s:s + 1], ref, size, f"sequence {s}")
