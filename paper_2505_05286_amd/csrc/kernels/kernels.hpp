@@ -246,9 +246,8 @@ struct Kv8Pool {
   float* vs;
   int64_t n_blocks;
 };
-// Offset of (dimension d, token t) inside a page of K, and of V
+// Offset of (dimension d, token t) inside a page of K
 __host__ __device__ inline int k8_offset(int d, int t) { return ((d >> 4) * kPage + t) * 16 + (d & 15); }
-__host__ __device__ inline int v8_offset(int d, int t, int dh) { return ((t >> 2) * dh + d) * 4 + (t & 3); }
 
 // A launch counts its threads of each dimension in 32 bits
 inline bool launch_fits(int64_t groups, int threads) { return groups <= (int64_t)UINT32_MAX / threads; }
