@@ -167,7 +167,9 @@ int hxf_op_prefill_attention(const void* q, const void* k_pool, const void* v_po
  * Scales: fp32 [Hkv][n_blocks] for K and for V; an element stands for its e4m3 value (OCP: largest 448, NaN, no
  * infinity) times the scale of its page.  A scale is a POWER OF TWO in [2^-100, 2^120] (hxf_op_rope_kv8_write
  * makes no other; of any other value the attention uses the exponent alone, 0 being 2^-127), so a dequantised element is
- * exactly a bf16 value and a page whose scale grows keeps its codes up to their exponents.  (The attention holds V to
+ * exactly a bf16 value and a page whose scale grows keeps its codes up to their exponents.  (But at 2^120, in a
+ * page with |x| > 1.75 * 2^127, the codes from 256 on, for |x| from 1.9375 * 2^127 on, stand for values beyond bf16 and
+ * fp32: outputs of queries that see one are undefined.)  (The attention holds V to
  * 2^-25 of the largest V scale among a sequence's pages of a head: exactly where scales are within 2^15 of it.)
  * k and v must be 16-byte aligned; 0 < n_blocks < 2^27.  The struct is read during the call only. */
 typedef struct hxf_kv8_pool {

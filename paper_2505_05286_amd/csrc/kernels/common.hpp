@@ -46,7 +46,7 @@ __device__ __forceinline__ f32x4 mfma16x16x32(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// Four e4m3 codes times a power of two (the exponent of `scale`) as bf16, exactly
+// Four e4m3 codes times a power of two (the exponent of `scale`) as bf16, exactly where they are below 2^128
 __device__ __forceinline__ uint2 e4m3x4_to_bf16(uint32_t c, float scale) {
   const auto lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false);
   const auto hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true);

@@ -219,3 +219,17 @@ def test_batches_whose_launch_would_pass_32_bits_of_threads_are_refused():
     assert hxf.op_decode_attention_kv8_workspace_bytes((1 << 26) - 3073, 1, 1, 64) > 0
     assert hxf.op_prefill_attention_kv8_workspace_bytes((1 << 24) - 1, 1, 1, 1, 64) == -1
     assert hxf.op_prefill_attention_kv8_workspace_bytes((1 << 24) - 2, 1, 1, 1, 64) > 0
+
+
+def test_dequantised_values_are_bf16_values_up_to_scales_of_2_119():
+    """Every code times every scale that the write makes below 2^120 is a finite bf16 value; at 2^120 those of codes under 256
+    are, and |x| under 1.9375 * 2^127 gets no other code."""
+    v = np.delete(U.VALUES, [0x7F, 0xFF])
+    for e in range(-100, 121):
+        x = (v if e < 120 else v[np.abs(v) < 256]) * 2.0 ** e
+        f = x.astype(np.float32)
+        assert np.all(np.isfinite(f)) and np.array_equal(f.astype(np.float64), x)
+        assert not np.any(f.view(np.uint32) & 0xFFFF)
+    assert U.scale_for(1.75 * 2.0 ** 127) == 2.0 ** 119 and U.scale_for(1.76 * 2.0 ** 127) == 2.0 ** 120
+    top = np.nextafter(np.float32(1.9375 * 2.0 ** 127), np.float32(0)).astype(np.float64)
+    assert U.VALUES[U.encode(top / 2.0 ** 120)] == 240 and U.VALUES[U.encode(248.0)] == 256
