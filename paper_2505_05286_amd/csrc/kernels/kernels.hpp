@@ -309,10 +309,12 @@ struct Kv8AttnArgs {
 // cache, each (sequence, kv-head) stream of pages is cut into equal parts no longer than an even share of
 // all the pages over the wavefronts the chip holds at once (or than kKv8MinPages pages, or than kv8_part_pages
 // says); with fewer streams than those wavefronts the parts at most fill them.
-constexpr int kKv8Resident = 3 * 1024;   // three a SIMD, at 162 VGPRs
+constexpr int kKv8Resident = 3 * 1024;   // three a SIMD, at the 160 VGPRs of head size 128; 64, at 103, is split likewise,
+                                         // and its fourth place is left empty
 constexpr int kKv8MinPages = 4;
 constexpr int kKv8WholePages = 8;    // with tables this short no stream is cut, and there is no join: 20 contexts of up
-                                     // to 60 tokens 4.9 us, with parts and a join 6.3
+                                     // to 60 tokens 4.7 us, with parts and a join 6.3.  (A property of the table, which the
+                                     // host knows: short contexts in wide tables are cut.)
 __host__ __device__ inline int64_t kv8_target_pages(int64_t total_pages, int64_t n_seqs, int hkv, int bt_stride) {
   const int least = bt_stride <= kKv8WholePages ? kKv8WholePages : kKv8MinPages;
   const int64_t pairs = n_seqs * hkv;
@@ -320,10 +322,11 @@ __host__ __device__ inline int64_t kv8_target_pages(int64_t total_pages, int64_t
   const int64_t t = (total_pages * hkv + slots - 1) / slots;
   return t > least ? t : least;
 }
-// Length of a part of a stream of `pages` pages, and the number of them: at most ceil(pages / target).  With few streams
-// a part takes as long as its pages, the join as its parts: their sum is least near sqrt(pages / 8) pages a part.  One
-// context, 32 + 8 heads, us, against 8 pages or more: 1000 tokens 8.4 / 9.7, 2000 8.7 / 10.5, 8191 11.4 / 11.4, 30000
-// 20.6 / 24.0, 64000 32.7 / 39.4; 16 of 100 to 1500 10.4 / 11.4; 8 of 500 to 3000, 64 + 8 heads, 13.4 / 12.0.
+// Length of a part of a stream of `pages` pages, and the number of them: at most ceil(pages / target).  A part takes as
+// long as its pages, the join as its parts: for a stream alone their sum is least near sqrt(pages / 8) pages a part.  The rule
+// does not look at the number of heads and streams, with which the join grows.  One context, 32 + 8 heads, us, against 8
+// pages or more: 1000 tokens 7.9 / 9.0, 2000 8.1 / 9.8, 8191 11.2 / 11.2, 30000 17.5 / 19.0, 64000 29.2 / 31.9; 16 of 100 to
+// 1500 10.2 / 11.3; 8 of 500 to 3000, 64 + 8 heads, 13.1 / 11.7.
 __host__ __device__ inline int kv8_part_pages(int pages, int target) {
   const int least = (int)sqrtf((float)(pages / 8)), t = target > least ? target : least;
   const int n = (pages + t - 1) / t;
@@ -350,8 +353,10 @@ inline bool kv8_decode_join_fits(int64_t n_seqs, int hq, int bt_stride) {
 // shares to the workgroups resident at once: a block is cut where a share ends, unless it exceeds one by
 // kPrefillMinTiles pairs at most, or the piece would be shorter than kPrefillMinTiles / 4.  32 + 8 heads, us, against
 // equal parts of each block, of no more than a share and so more of them than are resident: 512 queries at 8192 104 / 137,
-// 640 at 9000 140 / 163, 800 at 20000 310 / 402.  With 304 blocks 153 cut, 163 whole; 264 104 / 116; 256 blocks of up to
-// 1500 keys 46 / 44; 352 of 4000 keys 178 / 157, 384 of 8700 265 / 258.
+// 640 at 9000 140 / 163, 800 at 20000 310 / 402.  Cut / whole, us: 128 blocks (512 queries at 8192) 107 / 188, 264 (1056 at
+// 6000) 154 / 178, 304 (1216 at 8192) 210 / 238, 352 (44 times 32 at 4000) 157 / 146, 352 (16 times 5 to 256 at 4000, 40 + 8
+// heads) 139 / 132, 384 (1536 at 8192) 262 / 253.  The rule counts blocks and not their lengths: a first chunk of 2048
+// queries, 512 blocks of 2 to 64 tiles, lasts as long as its longest (65 us).
 constexpr int kCus = 256;
 constexpr int kPrefillCutUnits = 320;
 __host__ __device__ inline bool kv8_prefill_cuts(int64_t blocks, int hkv) {

@@ -18,7 +18,7 @@ __device__ __forceinline__ int pages_of(int n) { return (n + kPage - 1) / kPage;
 // The longest part of this batch (kv8_target_pages), found by every wavefront for itself from the contexts: with few
 // sequences a load and a scan or two, against a launch and a round trip through memory.  Above kKv8DecodeScan
 // sequences a launch of its own does it once (a.starts); us for contexts of 64 to 128 tokens, 32 + 8 heads, every
-// wavefront / one launch: 64 sequences 9.4 / 12.2, 128 12.0 / 12.4, 256 20 / 18, 1024 111 / 52, 4096 1016 / 194.
+// wavefront / one launch: 64 sequences 9.5 / 12.1, 128 14.1 / 16.0, 256 16.0 / 16.8, 1024 87 / 48.5, 4096 615 / 184.
 __device__ __forceinline__ int decode_target(const Kv8AttnArgs& a, int lane) {
   int64_t total = 0;
   for (int i0 = 0; i0 < a.S; i0 += kWave) {
@@ -268,9 +268,10 @@ __device__ __forceinline__ void decode_part(const Kv8AttnArgs& a, int lane) {
   for (int i = 0; i < DH / 16; ++i) S.acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   S.m = kLowest;
   S.l = 0.f;
-  // Pairs of pages in registers: one multiplied, one on its way.  A third takes the registers of a third wavefront
-  // on the SIMD, whose loads hide more: 128 contexts of 1.5-3k tokens, 32 + 8 heads, 109 us against 118, 97 of
-  // 4.5-9k 226 against 238.
+  // Pairs of pages in registers: one multiplied, one asked for.  The loads stand under a branch, so the compiler counts them
+  // as if they had not been issued: of the two pairs of a turn the first waits for both, and it is the other wavefronts of
+  // the SIMD that hide this.  (So does the first pair for the scales.)  A third pair takes the registers of a third wavefront,
+  // which hides more: 128 contexts of 1.5-3k tokens, 32 + 8 heads, 109 us against 118, 97 of 4.5-9k 226 against 238.
   constexpr int NB = 2;
   Kv8Pair<DH> R[NB];
   auto issue = [&](Kv8Pair<DH>& P, int r) __attribute__((always_inline)) {
@@ -369,8 +370,9 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a) {
 // running maximum; the streams of a wavefront meet by exchanges between lanes, those of wavefronts in LDS.  A wavefront
 // takes a head, unless that would leave CUs without a workgroup and the tables are long enough for more than kMergeAlone
 // parts: then a workgroup takes a head, or, with up to kMergeWide such workgroups, a quarter of its dimensions.
-// 64 sequences of up to 11 parts: 4.7 us (a workgroup a head: 7.7).  Both launches for a context of 30000 tokens (118
-// parts): 17.8 us with quarters, 19.9 with whole heads; 64000 29.5 / 32.7; 16 contexts of 100 to 1500 11.2 / 10.4.
+// Both launches, 32 + 8 heads, us: 64 sequences of up to 12 parts, a wavefront a head 83.0, a workgroup 83.3; a context of
+// 30000 tokens (125 parts), quarters 17.9, whole heads 20.2, a wavefront 29.7; 64000 (182 parts) 30.1 / 33.2 / 46.1; 8191 (64
+// parts) 11.3 / 12.0 / 16.5; 16 contexts of 100 to 1500, a workgroup a head 10.2, a wavefront 11.3.
 constexpr int kMergeAlone = 16;
 constexpr int kMergeWide = 1024;
 template <int DH>
@@ -793,15 +795,15 @@ __global__ __launch_bounds__(kPlanThreads) void kv8_prefill_plan_kernel(Kv8Prefi
 //   S^T[32 keys x 32 pairs] = K[32 x dh] . Q^T[dh x 32]       (v_mfma_f32_32x32x16_bf16)
 //   O^T[32 dims x 32 pairs] += V^T[32 x 32 keys] . P^T[32 x 32]   (in fp16)
 // with 32 pairs per wavefront.  Every wavefront multiplies every key, so a tile of 32 keys is converted once for the
-// workgroup, on its way into LDS: a thread loads DH/8 bytes of K and of V, two tiles ahead, into registers, and writes
+// workgroup, on its way into LDS: a thread loads DH/8 bytes of K and of V, up to two tiles ahead, into registers, and writes
 // them, K as exact bf16 (the page's power of two is applied by the conversion), V's codes as fp16, in the order of the
 // matrix operands.  A step multiplies K of tile t + 1 and V of tile t, so that the scores of the next tile and the
 // exponentials of this one run side by side; the conversions run beside the product with V.
 //
-// What bounds it: at 6144 + 2048 the power limit (13% more cycles than the bf16 cache's kernel in less time) and the
-// wavefronts' waits (MFMA busy 46% of the cycles, LDS ports 35%); 2048 queries there 247 us, 0.97 PFLOP/s, where the
-// bf16 cache's kernel takes 257.  17 queries over 30k keys: 28 us, 2.2 TB/s, of which four are the plan and the first
-// loads, and the steps' latency the rest.
+// What bounds it: at 6144 + 2048 the wavefronts' waits (28% of their cycles, MFMA busy 46%, LDS ports 35%), of which one is
+// for all loads in flight, every second step (see the loop); how much of it that makes, and how much the power limit, was not
+// taken apart.  2048 queries there 239-252 us by card, 0.95-1.0 PFLOP/s, where the bf16 cache's kernel takes 257.  17
+// queries over 30k keys: 28 us, 2.2 TB/s, of which four are the plan and the first loads, and the steps' latency the rest.
 template <int DH, bool SMALL>
 __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
   constexpr int KS = DH / 16;      // 16-dim steps of QK^T
@@ -1116,7 +1118,8 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
     __syncthreads();
     // a step: V of tile t + 1 and K of t + 2 into LDS, V of t + 3 and K of t + 4 on their way, scores of t + 1, output of t.
     // Past the last tile it moves and scores the last page again, which nothing uses: no step has a branch around
-    // its loads, so that those in flight stay counted.
+    // its loads, so that the second of a turn's two steps counts those in flight.  The first begins with a wait for all of
+    // them: turn_stores chooses among scales whose loads may be the newest, from between two rounds of the loop.
     auto step = [&](words_t& rk, words_t& rv, bf16_t* k_now, bf16_t* k_next, bf16_t* v_now, bf16_t* v_next, int t)
         __attribute__((always_inline)) {
       turn_stores(t + 2);
@@ -1151,7 +1154,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
       load_k(rk, t + 4);
       __syncthreads();
     };
-    // (the tables turn outside of the loop over steps, whose loads stay counted; ntiles is even)
+    // (the tables turn outside of the loop over steps; ntiles is even)
     for (int t = 0;;) {
       const int stop = min(ntiles, ((t + 4) | 31) - 3);   // the next t with t + 4 a multiple of 32
       do {
@@ -1195,7 +1198,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
 
 // Joins the parts of cut blocks: DH/4 threads a (query, head) pair; the workgroups walk the pairs of all jobs, so that a
 // launch with nothing to join (the host does not know) is short.  With few jobs, of many parts then, R streams of parts
-// share a pair (17 queries over 30k keys 34 us; with one 41); with more than kMergeWalk rounds of that, a pair has one
+// share a pair (17 queries over 30k keys 33 us; with one 41); with more than kMergeWalk rounds of that, a pair has one
 // (512 queries at 8192 107 us; with R 120).
 constexpr int kMergeWalk = 2;
 template <int DH>
