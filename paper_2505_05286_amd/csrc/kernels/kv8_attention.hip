@@ -117,7 +117,9 @@ __device__ __forceinline__ uint32_t keep_bytes(int n) { return n >= 4 ? ~0u : n 
 // in units of 2^E, which moves (upwards) with the tables of 64 pages.  Codes of a page under 2^-15 of the largest scale
 // become fp16 subnormals, off by up to 2^-25 of 2^E.  The weights are 2^(x - m): the reference m is set kRefBelow under
 // the largest score so far and moves only when one exceeds it by kRefRange, so that they stay under 2^15, the largest is
-// 2^7 or more, and one is rounded to 2^-11 of itself or to 2^-32 of the largest, whichever is more.
+// 2^7 or more, and one is rounded to 2^-11 of itself or to 2^-32 of the largest, whichever is more.  (Far scores count in
+// coarse steps: mx - m is exact where it decides, m + kRefRange would be rounded.  Prefill's exponents, whose x is not rounded
+// to fp32 as mx is, stay under 16 for scores up to 2^28.)
 constexpr float kRefBelow = 7.f, kRefRange = 15.f;
 constexpr int kNoExp = -127;   // exponent of an entry that is no page
 __device__ __forceinline__ int exponent_of(float scale) { return (int)(__float_as_uint(scale) >> 23 & 255) - 127; }
@@ -165,7 +167,7 @@ __device__ __forceinline__ void kv8_pair(Kv8State<DH>& S, const Kv8Pair<DH>& R, 
   }
   float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
   mx = half_swap_max(row_swap_max(mx));
-  if (__any(mx > S.m + kRefRange)) {
+  if (__any(mx - S.m > kRefRange)) {
     const float m_new = fmaxf(S.m, mx - kRefBelow);
     const float alpha = __builtin_amdgcn_exp2f(S.m - m_new);
     S.m = m_new;
@@ -1025,7 +1027,7 @@ __global__ __launch_bounds__(256, 2) void kv8_prefill_kernel(Kv8PrefillArgs p) {
       mx = score_max(x);
       spread_nan(v_now, k0, miss);
     }
-    if (__any(mx > m + kRefRange)) {
+    if (__any(mx - m > kRefRange)) {
       const float m_new = fmaxf(m, mx - kRefBelow);
       const float alpha = __builtin_amdgcn_exp2f(m - m_new);
       m = m_new;

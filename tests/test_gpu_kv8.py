@@ -899,3 +899,47 @@ def test_prefill_planned_blocks_of_a_row0_that_goes_up_and_down_are_bounded(hi_c
     for s in (0, 1, 57, 89):
         ref, size = U.attend(qf[s:s + 1], cache, bt[s], hi_ctx - 89, 16, first=hi_ctx - 90)
         U.assert_attention(got[s:s + 1], ref, size, f"sequence {s}")
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(2, 1, 64), (4, 2, 128)])
+def test_scores_far_beyond_the_steps_of_their_references(hq, hkv, dh):
+    """Scores of 2^16 to 2^28, where fp32 counts in steps of up to 16, that climb by a few such steps from key to key: no
+    weight may pass fp16.  Every value of V is 1, and so is every average of them."""
+    t = torch()
+    n_keys, rows = 700, 3
+    cases = [(e, m, s) for e in range(16, 29) for m in (1.0, 1.25, 1.6875) for s in (1, 2, 3)]
+    S = len(cases)
+    pages = -(-n_keys // 16)
+    cache = U.Cache(hkv, S * pages, dh)
+    cache.codes["k"][:], cache.codes["v"][:] = 0, U.encode(256.0)
+    cache.scale["k"][:], cache.scale["v"][:] = 1, 2.0 ** -8
+    q = np.zeros((S, dh), np.float32)
+    log2_unit = 1.4426950408889634 / np.sqrt(dh)
+    for i, (e, m, s) in enumerate(cases):
+        at = slice(i * pages, (i + 1) * pages)
+        # dimension 0 makes the size, 256 q0; dimension 1 climbs, by s steps of its fp32 products in 16 keys, from 0 to 240
+        q[i, 0] = m * 2.0 ** (e - 8) / log2_unit
+        q[i, 1] = s * 2.0 ** (e - 24) / log2_unit
+        cache.codes["k"][:, at, :, 0] = U.encode(256.0)
+        climb = np.minimum(np.arange(pages * 16) // 16 + 1, 15).reshape(pages, 16) * 1.0
+        cache.codes["k"][:, at, :, 1] = U.encode(climb)
+    bits = synth.f32_to_bf16_bits(np.repeat(q[:, None], hq, 1).reshape(S, hq, dh)).reshape(S, hq * dh)
+    dev = DevCache(cache)
+    bt = i32(np.arange(S * pages).reshape(S, pages))
+    ctx, dq, out = i32(np.full(S, n_keys)), dev_bits(bits), dev_bits(np.zeros((S, hq * dh), np.uint16))
+    ws = t.empty(hxf.op_decode_attention_kv8_workspace_bytes(S, hq, hkv, dh), dtype=t.uint8, device="cuda:0")
+    log(f"scores far beyond: {hq}/{hkv}x{dh}")
+    hxf.op_decode_attention_kv8(dq.data_ptr(), hq * dh, dev.pool, bt.data_ptr(), pages, ctx.data_ptr(), out.data_ptr(),
+                                hq * dh, S, hq, hkv, dh, ws.data_ptr(), ws.numel())
+    T = S * rows
+    dq2, out2 = dev_bits(np.repeat(bits, rows, 0)), dev_bits(np.zeros((T, hq * dh), np.uint16))
+    row0, pos0 = i32(np.arange(S + 1) * rows), i32(np.full(S, n_keys - rows))
+    ws2 = t.empty(hxf.op_prefill_attention_kv8_workspace_bytes(S, T, hq, hkv, dh), dtype=t.uint8, device="cuda:0")
+    hxf.op_prefill_attention_kv8(dq2.data_ptr(), hq * dh, dev.pool, bt.data_ptr(), pages, row0.data_ptr(),
+                                 pos0.data_ptr(), out2.data_ptr(), hq * dh, S, T, hq, hkv, dh, ws2.data_ptr(), ws2.numel())
+    t.cuda.synchronize()
+    for what, o in (("decode", out), ("prefill", out2)):
+        got = host_f64(o).reshape(S, -1)
+        # the weights' roundings to fp16 (2^-11) and the output's to bf16 (2^-8)
+        bad = [cases[i] for i in range(S) if not np.all(np.abs(got[i] - 1) <= 2.0 ** -8 + 2.0 ** -10)]
+        assert not bad, (what, bad)
