@@ -220,7 +220,7 @@ int hxf_op_rope_kv8_write(const void* qkv, int64_t qkv_stride, const int32_t* po
  * zeros.  Tokens of a block-table entry that is no page of the pool are not read and have no weight.  Entries past
  * the context are not read.  q, out, the pool and the workspace must not overlap.  workspace:
  * hxf_op_decode_attention_kv8_workspace_bytes bytes, 16-byte aligned, whose contents need not be kept between
- * calls; calls that may overlap need one each.  B * Hq < 2^29; B * Hkv < 2^26 - 3072; and, with bt_stride > 8,
+ * calls; calls that may overlap need one each.  B * Hq < 2^29; B * Hkv < 2^26 - 3 * 2^10; and, with bt_stride > 8,
  * B * ceil(Hq / 4) < 2^24. */
 int64_t hxf_op_decode_attention_kv8_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t head_dim);
 int hxf_op_decode_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_pool* pool, const int32_t* bt,

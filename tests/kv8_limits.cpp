@@ -21,8 +21,8 @@ int main() {
   CHECK(kv8_write_fits(k28 - 16, 1, 1) && !kv8_write_fits(k28 - 15, 1, 1));
   CHECK(kv8_write_fits(1, 65533, 1) && !kv8_write_fits(1, 65534, 1) && !kv8_write_fits(1, int64_t(1) << 30, int64_t(1) << 30));
   // decode: a wavefront for each item; heads four to a workgroup of the join, which short tables do without
-  CHECK(kv8_decode_fits(k26 - 3073, 1) && !kv8_decode_fits(k26 - 3072, 1));
-  CHECK(kv8_decode_fits((k26 - 3073) / 8, 8) && !kv8_decode_fits(k26 / 8, 8));
+  CHECK(kv8_decode_fits(k26 - kKv8Resident - 1, 1) && !kv8_decode_fits(k26 - kKv8Resident, 1));
+  CHECK(kv8_decode_fits((k26 - kKv8Resident - 1) / 8, 8) && !kv8_decode_fits(k26 / 8, 8));
   CHECK(kv8_decode_join_fits(k24 - 1, 4, 9) && !kv8_decode_join_fits(k24, 1, 9) && kv8_decode_join_fits(k24, 4, 8));
   CHECK(kv8_decode_join_fits(k24 / 8 - 1, 32, 1000) && !kv8_decode_join_fits(k24 / 8, 32, 1000));
   // prefill: four wavefronts for each unit and head

@@ -212,11 +212,11 @@ def test_batches_whose_launch_would_pass_32_bits_of_threads_are_refused():
                 dict(Hq=1 << 30, Hkv=1 << 30, qkv_stride=1 << 40, q_stride=1 << 40)):
         _refused(hxf.EINVAL, _write, **bad)
     one = dict(Hq=1, Hkv=1, dh=64)
-    _refused(hxf.EINVAL, _decode, B=(1 << 26) - 3072, bt_stride=4, **one)
+    _refused(hxf.EINVAL, _decode, B=(1 << 26) - 3 * 1024, bt_stride=4, **one)
     _refused(hxf.EINVAL, _decode, B=1 << 24, bt_stride=9, **one)
     _refused(hxf.EINVAL, _prefill, S=(1 << 24) - 1, T=1, **one)
-    assert hxf.op_decode_attention_kv8_workspace_bytes((1 << 26) - 3072, 1, 1, 64) == -1
-    assert hxf.op_decode_attention_kv8_workspace_bytes((1 << 26) - 3073, 1, 1, 64) > 0
+    assert hxf.op_decode_attention_kv8_workspace_bytes((1 << 26) - 3 * 1024, 1, 1, 64) == -1
+    assert hxf.op_decode_attention_kv8_workspace_bytes((1 << 26) - 3 * 1024 - 1, 1, 1, 64) > 0
     assert hxf.op_prefill_attention_kv8_workspace_bytes((1 << 24) - 1, 1, 1, 1, 64) == -1
     assert hxf.op_prefill_attention_kv8_workspace_bytes((1 << 24) - 2, 1, 1, 1, 64) > 0
 
