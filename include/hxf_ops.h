@@ -242,6 +242,50 @@ int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_
                                  int64_t out_stride, int32_t S, int32_t T, int32_t Hq, int32_t Hkv, int32_t head_dim,
                                  void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ---- Linear layers in 8-bit integers: the rows of a matrix [R, K] (the output channels of a weight, the tokens
+ * of the activations) as codes of -127..127 with one fp32 scale a row; an element stands for its code times the
+ * scale of its row.  No call waits for the stream or reads device values on the host, so all of them can be captured.
+ *
+ * Codes are kept in tiles of 16 rows x 64 columns (1 KB), row-tiles outermost, zero padded to whole tiles: element
+ * (r, k) is at
+ *   ((r/16) * ceil(K/64) + k/64) * 1024 + ((k%64)/16) * 256 + (r%16) * 16 + k%16,
+ * the operand order of the 16x16x64 i8 MFMA.  hxf_i8_codes_bytes(R, K) bytes (-1 for sizes the operators refuse),
+ * 16-byte aligned.  0 < K < 2^17, so that no sum of products passes 32 bits; 0 <= R < 2^24. */
+int64_t hxf_i8_codes_bytes(int32_t R, int32_t K);
+
+/* Codes and scales of bf16 rows (weights once when they are loaded, activations in each step): x bf16, R rows of
+ * x_stride elements, K of them used.  With m = max|x| of a row: scale = m / 127, code = x * (127 / m) rounded to the
+ * nearest whole number, ties to even; both divisions and the product in fp32.  A row with m < 2^-119 is zeros with
+ * the scale 0; one that holds NaN or an infinity has zero codes and the scale NaN, so that every output it takes
+ * part in is NaN and no other.  codes: hxf_i8_codes_bytes(R, K) bytes, the padding written as zeros; scale fp32
+ * [R].  x 16-byte aligned, x_stride >= K and both multiples of 8.  No buffer may overlap another. */
+int hxf_op_quant_i8(const void* x, int64_t x_stride, int32_t R, int32_t K, void* codes, float* scale, void* stream);
+
+/* RMSNorm into codes: row r is y = x[rows[r]] * g / sqrt(mean(x[rows[r]]^2) + eps), without a rounding to bf16 in
+ * between (rows may be NULL: row r itself).  The codes are those of x * g, formed in fp32, as hxf_op_quant_i8 makes them;
+ * scale = max|x g| / 127 / sqrt(mean(x^2) + eps), the sum of squares in fp32.  A row whose index is not in
+ * [0, x_rows) (an empty place of a padded batch) is zeros with the scale 0.  x fp32 [x_rows, d], 16-byte aligned,
+ * g bf16 [d], 8-byte aligned, d % 4 == 0, d < 2^17; codes and scale as above, for [n_rows, d]; n_rows < 2^24.
+ * Without rows, n_rows <= x_rows.  No output may overlap another buffer. */
+int hxf_op_rmsnorm_i8(const float* x, const int32_t* rows, int32_t x_rows, const void* g, void* codes, float* scale,
+                      int32_t n_rows, int32_t d, float eps, void* stream);
+
+/* C from acc = A[M,K] . B[N,K]^T of codes, summed exactly in 32-bit integers; y = (float(acc) * a_scale[m]) * b_scale[n].
+ *   HXF_EPI_BF16:   C bf16 [M, ldc]            C = bf16(y)
+ *   HXF_EPI_RESID:  C fp32 [M, ldc]            C += y            (residual stream)
+ *   HXF_EPI_SWIGLU: B, b_scale = W_gate [F,K], B2, b2_scale = W_up [F,K], N = 2F; C bf16 [M, ldc],
+ *                   C[:, f] = bf16(silu(gate_f) * up_f), silu(z) = z / (1 + e^-z)
+ *   HXF_EPI_F32:    C fp32 [M, ldc]            C = y
+ * A and B (and B2): codes as above, 16-byte aligned.  B2 and b2_scale are unused but for SwiGLU.  ldc >= N (SwiGLU: F);
+ * elements behind a row's columns are left as they are.  M < 2^24, 0 < N < 2^24, 0 < K < 2^17, M * N < 2^40.
+ * workspace: hxf_op_gemm_i8_workspace_bytes(M, N, K) bytes (enough for every epilogue; may be 0), 16-byte
+ * aligned, whose contents need not be kept between calls; calls that may overlap need one each.  No buffer may
+ * overlap another. */
+int64_t hxf_op_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K);
+int hxf_op_gemm_i8(const void* A, const float* a_scale, const void* B, const float* b_scale, const void* B2,
+                   const float* b2_scale, void* C, int32_t ldc, int32_t M, int32_t N, int32_t K, int32_t epilogue,
+                   void* workspace, int64_t workspace_bytes, void* stream);
+
 /* out[r] = argmax over v of logits fp32 [R, V]; the lowest index wins ties. */
 int hxf_op_argmax(const float* logits, int32_t* out, int32_t R, int32_t V, void* stream);
 

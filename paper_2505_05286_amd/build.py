@@ -35,6 +35,8 @@ SOURCES = [
     "kernels/attention.hip",
     "kernels/kv8.hip",
     "kernels/kv8_attention.hip",
+    "kernels/quant_i8.hip",
+    "kernels/gemm_i8.hip",
     "kernels/misc.hip",
 ]
 

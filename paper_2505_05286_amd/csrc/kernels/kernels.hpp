@@ -77,6 +77,31 @@ hipError_t gemm_wide_split(const GemmArgs& a, const GemmPlan& p, hipStream_t st,
 size_t packed_weight_elems(int N, int K);
 hipError_t pack_weight_launch(const uint16_t* W, int N, int K, uint16_t* out, hipStream_t st);
 
+// ------------------------------------------------------------------ 8-bit linear layers
+// Codes of an int8 matrix [R, K] in tiles of 16 rows x 64 columns (1 KB), kt = ceil(K / 64) tiles per row tile,
+// inside a tile [k%64 / 16][r%16][k%16]: the operand order of the 16x16x64 i8 MFMA, the same bytes as a bf16 tile.
+__host__ __device__ inline size_t i8_elem(int r, int k, int kt) {
+  return ((size_t)(r >> 4) * kt + (k >> 6)) * 1024 + ((k >> 4) & 3) * 256 + (r & 15) * 16 + (k & 15);
+}
+inline size_t i8_codes_bytes(int R, int K) { return (size_t)((R + 15) / 16) * ((K + 63) / 64) * 1024; }
+
+// codes and scales of bf16 rows x [R, K], row stride in elements
+hipError_t quant_i8_launch(const uint16_t* x, int64_t stride, int R, int K, int8_t* codes, float* scale, hipStream_t st);
+// codes and scales of rmsnorm(x[rows ? rows[r] : r]) * g; x fp32 [x_rows, d]; zeros where rows[r] is none of them
+hipError_t rmsnorm_i8_launch(const float* x, const int32_t* rows, int x_rows, const uint16_t* g, int8_t* codes,
+                             float* scale, int n_rows, int d, float eps, hipStream_t st);
+
+struct GemmI8Args {
+  const int8_t *A, *B, *B2;        // codes of A [M, K], B [N, K] (SwiGLU: gate) and the up weight
+  const float *sa, *sb, *sb2;      // scales of their rows
+  void* C;                         // bf16 or fp32, row stride ldc
+  int32_t* partial;                // split-K partials
+  int M, N, ldc;                   // N: output columns
+  int kt;                          // K tiles, ceil(K / 64)
+};
+int64_t gemm_i8_ws_bytes(int M, int N, int K);   // N as the caller counts it (SwiGLU: 2F)
+hipError_t gemm_i8_launch(const GemmI8Args& a, int epi, hipStream_t st);
+
 // ------------------------------------------------------------------ norms / embedding
 // out[r] = bf16(rmsnorm(x[rows ? rows[r] : r]) * g); x fp32 [*, d]
 hipError_t rmsnorm_launch(const float* x, const int32_t* rows, const uint16_t* g, uint16_t* out,

@@ -577,6 +577,70 @@ int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_
   return dev_rc(kv8_prefill_launch(a, (hipStream_t)stream));
 }
 
+namespace {
+
+bool i8_matrix_ok(int32_t R, int32_t K) { return R >= 0 && R < (1 << 24) && K > 0 && K < (1 << 17); }
+
+}  // namespace
+
+int64_t hxf_i8_codes_bytes(int32_t R, int32_t K) { return i8_matrix_ok(R, K) ? (int64_t)i8_codes_bytes(R, K) : -1; }
+
+int hxf_op_quant_i8(const void* x, int64_t x_stride, int32_t R, int32_t K, void* codes, float* scale, void* stream) {
+  if (!i8_matrix_ok(R, K) || K % 8 || !rows_ok(x, x_stride, K) || !codes || !aligned16(codes) || !scale)
+    return HXF_EINVAL;
+  if (R == 0) return HXF_OK;
+  return dev_rc(quant_i8_launch((const uint16_t*)x, x_stride, R, K, (int8_t*)codes, scale, (hipStream_t)stream));
+}
+
+int hxf_op_rmsnorm_i8(const float* x, const int32_t* rows, int32_t x_rows, const void* g, void* codes, float* scale,
+                      int32_t n_rows, int32_t d, float eps, void* stream) {
+  if (!i8_matrix_ok(n_rows, d) || d % 4 || !x || !aligned16(x) || !g || (reinterpret_cast<uintptr_t>(g) & 7) || !codes ||
+      !aligned16(codes) || !scale || x_rows < 0 || (!rows && n_rows > x_rows))
+    return HXF_EINVAL;
+  if (n_rows == 0) return HXF_OK;
+  return dev_rc(rmsnorm_i8_launch(x, rows, x_rows, (const uint16_t*)g, (int8_t*)codes, scale, n_rows, d, eps,
+                                  (hipStream_t)stream));
+}
+
+namespace {
+
+bool gemm_i8_ok(int32_t M, int32_t N, int32_t K) {
+  return i8_matrix_ok(M, K) && N > 0 && i8_matrix_ok(N, K) && (int64_t)M * N < (int64_t(1) << 40);
+}
+
+}  // namespace
+
+int64_t hxf_op_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K) {
+  return gemm_i8_ok(M, N, K) ? gemm_i8_ws_bytes(M, N, K) : -1;
+}
+
+int hxf_op_gemm_i8(const void* A, const float* a_scale, const void* B, const float* b_scale, const void* B2,
+                   const float* b2_scale, void* C, int32_t ldc, int32_t M, int32_t N, int32_t K, int32_t epilogue,
+                   void* workspace, int64_t ws_bytes, void* stream) {
+  const bool sw = epilogue == HXF_EPI_SWIGLU;
+  if (!gemm_i8_ok(M, N, K) || epilogue < 0 || epilogue > 3 || !A || !aligned16(A) || !a_scale || !B || !aligned16(B) ||
+      !b_scale || !C || ldc < (sw ? N / 2 : N) || (sw && (N % 2 || !B2 || !aligned16(B2) || !b2_scale)))
+    return HXF_EINVAL;
+  if (reinterpret_cast<uintptr_t>(C) & (epilogue == HXF_EPI_BF16 || sw ? 1 : 3)) return HXF_EINVAL;
+  if (M == 0) return HXF_OK;
+  const int64_t need = gemm_i8_ws_bytes(M, N, K);
+  if (need > 0 && (!workspace || !aligned16(workspace) || ws_bytes < need)) return HXF_ENOMEM;
+  GemmI8Args a{};
+  a.A = (const int8_t*)A;
+  a.B = (const int8_t*)B;
+  a.B2 = sw ? (const int8_t*)B2 : nullptr;
+  a.sa = a_scale;
+  a.sb = b_scale;
+  a.sb2 = sw ? b2_scale : nullptr;
+  a.C = C;
+  a.partial = (int32_t*)workspace;
+  a.M = M;
+  a.N = sw ? N / 2 : N;
+  a.ldc = ldc;
+  a.kt = (K + 63) / 64;
+  return dev_rc(gemm_i8_launch(a, epilogue, (hipStream_t)stream));
+}
+
 int hxf_op_argmax(const float* logits, int32_t* out, int32_t R, int32_t V, void* stream) {
   if (!logits || !out || R < 0 || V <= 0 || V % 4) return HXF_EINVAL;
   return dev_rc(argmax_launch(logits, out, R, V, (hipStream_t)stream));

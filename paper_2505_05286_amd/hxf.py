@@ -190,6 +190,12 @@ _SIGS = {
     "hxf_op_prefill_attention_kv8": (C.c_int, [C.c_void_p, C.c_int64, C.POINTER(Kv8Pool), C.c_void_p, C.c_int32,
                                                C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_int32,
                                                C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]),
+    "hxf_i8_codes_bytes": (C.c_int64, [C.c_int32, C.c_int32]),
+    "hxf_op_quant_i8": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "hxf_op_rmsnorm_i8": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                    C.c_int32, C.c_float, C.c_void_p]),
+    "hxf_op_gemm_i8_workspace_bytes": (C.c_int64, [C.c_int32, C.c_int32, C.c_int32]),
+    "hxf_op_gemm_i8": (C.c_int, [C.c_void_p] * 7 + [C.c_int32] * 5 + [C.c_void_p, C.c_int64, C.c_void_p]),
     "hxf_op_argmax": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]),
     "hxf_op_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "hxf_op_read": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
@@ -591,6 +597,31 @@ def op_prefill_attention_kv8(q, q_stride, pool, bt, bt_stride, row0, pos0, out, 
     """Causal prefill attention over the 8-bit cache; row0 and pos0 are device addresses."""
     _op(lib().hxf_op_prefill_attention_kv8(q, q_stride, pool, bt, bt_stride, row0, pos0, out, out_stride, S, T, Hq,
                                            Hkv, dh, ws, ws_bytes, stream or None), "hxf_op_prefill_attention_kv8")
+
+
+def i8_codes_bytes(R, K):
+    return lib().hxf_i8_codes_bytes(R, K)
+
+
+def op_quant_i8(x, x_stride, R, K, codes, scale, stream=0):
+    """8-bit codes (in tiles) and a scale for each of R bf16 rows of K elements."""
+    _op(lib().hxf_op_quant_i8(x, x_stride, R, K, codes, scale, stream or None), "hxf_op_quant_i8")
+
+
+def op_rmsnorm_i8(x, rows, x_rows, g, codes, scale, n_rows, d, eps, stream=0):
+    """RMSNorm of rows of an fp32 [x_rows, d] as 8-bit codes and scales; rows 0: the first n_rows of them."""
+    _op(lib().hxf_op_rmsnorm_i8(x, rows or None, x_rows, g, codes, scale, n_rows, d, eps, stream or None),
+        "hxf_op_rmsnorm_i8")
+
+
+def op_gemm_i8_workspace_bytes(M, N, K):
+    return lib().hxf_op_gemm_i8_workspace_bytes(M, N, K)
+
+
+def op_gemm_i8(A, a_scale, B, b_scale, B2, b2_scale, Cp, ldc, M, N, K, epi, ws=0, ws_bytes=0, stream=0):
+    """The product of two matrices of 8-bit codes, scaled back, with one of the EPI_ epilogues."""
+    _op(lib().hxf_op_gemm_i8(A, a_scale, B, b_scale, B2 or None, b2_scale or None, Cp, ldc, M, N, K, epi, ws or None,
+                             ws_bytes, stream or None), "hxf_op_gemm_i8")
 
 
 def op_argmax(logits, out, R, V, stream=0):
