@@ -29,6 +29,12 @@ SOURCES = [
     "kernels/gemm_wide_resid.hip",
     "kernels/gemm_wide_f32.hip",
     "kernels/gemm_wide_split.hip",
+    "kernels/gemm_i8_swiglu.hip",
+    "kernels/gemm_i8_bf16.hip",
+    "kernels/gemm_i8_resid.hip",
+    "kernels/gemm_i8_f32.hip",
+    "kernels/gemm_i8_split.hip",
+    "kernels/gemm_i8_split_swiglu.hip",
     "kernels/gemm.hip",
     "kernels/norm.hip",
     "kernels/rope_kv.hip",

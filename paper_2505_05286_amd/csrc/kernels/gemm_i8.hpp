@@ -1,0 +1,292 @@
+// The product of 8-bit codes C[M,N] = A[M,K] * B[N,K]^T with the weights read straight into registers.
+// Instantiated by gemm_i8_*.hip, one epilogue each.
+#pragma once
+
+#include "gemm_util.hpp"
+
+namespace hxf {
+
+namespace {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ i32x4 mfma16x16x64(uint4 a, uint4 b, i32x4 c) {
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+}
+
+// Epilogues of four columns of one row from col on; y = float(acc) * sa * sb, in this order: the first product has
+// the size of a sum of activations, while that of the two scales may pass below fp32's range.
+__device__ __forceinline__ float4 load_scales(const float* s, int col, int n) {
+  if (col + 3 < n) return make_float4(s[col], s[col + 1], s[col + 2], s[col + 3]);
+  float v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = s[min(col + e, n - 1)];
+  return make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ f32x4 scaled(i32x4 acc, float sa, float4 sb) {
+  return f32x4{(float)acc[0] * sa * sb.x, (float)acc[1] * sa * sb.y, (float)acc[2] * sa * sb.z,
+               (float)acc[3] * sa * sb.w};
+}
+__device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + __expf(-g)) * u; }
+
+// vec: the four columns lie inside the row and their address is aligned to them
+template <int EPI>
+__device__ __forceinline__ void store4(const GemmI8Args& a, int row, int col, f32x4 y, bool vec) {
+  const size_t o = (size_t)row * a.ldc + col;
+  if constexpr (EPI == EPI_BF16 || EPI == EPI_SWIGLU) {
+    bf16_t* c = reinterpret_cast<bf16_t*>(a.C) + o;
+    if (vec) {
+      *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3]));
+    } else {
+      for (int e = 0; e < 4 && col + e < a.N; ++e) c[e] = f2bf(y[e]);
+    }
+  } else {
+    float* c = reinterpret_cast<float*>(a.C) + o;
+    constexpr bool ADD = EPI == EPI_RESID;
+    if (vec) {
+      const float4 x = ADD ? *reinterpret_cast<const float4*>(c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      *reinterpret_cast<float4*>(c) = ADD ? make_float4(x.x + y[0], x.y + y[1], x.z + y[2], x.w + y[3])
+                                          : make_float4(y[0], y[1], y[2], y[3]);
+    } else {
+      for (int e = 0; e < 4 && col + e < a.N; ++e) c[e] = ADD ? c[e] + y[e] : y[e];
+    }
+  }
+}
+template <int EPI>
+__device__ __forceinline__ bool aligned4(const GemmI8Args& a) {
+  constexpr uintptr_t mask = EPI == EPI_BF16 || EPI == EPI_SWIGLU ? 7 : 15;
+  return ((a.ldc | a.N) & 3) == 0 && ((uintptr_t)a.C & mask) == 0;
+}
+
+// Macro tiles of 16 TM rows x 16 NW WV columns on the 16x16x64 i8 MFMA: WV wavefronts, each owning all the tile's
+// rows and 16 NW of its columns.  A tile of codes is a kilobyte in operand order like a packed bf16 tile, but of 64 of
+// K: the weights go straight from memory to registers, R steps of 64 of K ahead, and only the activations pass
+// through LDS, stages of 128 of K by buffer DMA, NS in flight.  Steps past the end of K multiply weights of zero, so
+// what the activations hold there does not matter.
+// SwiGLU: half of a wavefront's column tiles are gate and half the same columns of up, so one lane holds both.
+// Weights are the first MFMA operand: a lane ends up with 4 consecutive columns of one row.
+// SPLIT: grid.y cuts K into pieces of a.piece steps (even); each writes its int32 partial [M][N] (SwiGLU: gate, then
+// up columns) to slot blockIdx.y of a.partial.
+template <int TM, int NW, int R, int EPI, bool SPLIT, int WV, int OCC, int CACHE>
+__global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
+  constexpr bool SW = EPI == EPI_SWIGLU;
+  constexpr int HALF = SW ? NW / 2 : NW;                         // column tiles of the output per wavefront
+  constexpr int BM = 16 * TM, BN = 16 * HALF * WV, NS = 4;
+  constexpr int A_BLK = TM * 2, A_PW = (A_BLK + WV - 1) / WV, STAGE = A_BLK * 1024;   // 1 KB blocks per stage, per wavefront
+  // outstanding loads allowed when stage s + 1 must have landed: the younger stages' DMAs and the weight loads
+  // issued since its own DMAs (the first step's of the same pass may have been scheduled before those)
+  constexpr int WAIT = (NS - 3) * A_PW + 2 * NW * (NS - 2) - NW;
+  static_assert((2 * NS) % R == 0 && WAIT < 64 && NW * R + (NS - 2) * A_PW < 64, "pipeline");
+  static_assert(!SW || NW % 2 == 0, "a wavefront holds as many up columns as gate columns");
+  static_assert(NS * STAGE <= 160 * 1024, "stage layout");
+  __shared__ __attribute__((aligned(1024))) uint8_t L0[STAGE], L1[STAGE], L2[STAGE], L3[STAGE];
+  auto slot = [&](auto ic) -> uint8_t* {
+    constexpr int I = decltype(ic)::value % NS;
+    if constexpr (I == 0) return L0; else if constexpr (I == 1) return L1; else if constexpr (I == 2) return L2;
+    else return L3;
+  };
+  const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
+  const int L = xcd_remap(blockIdx.x, tiles_m * tiles_n);
+  const int tn = L / tiles_m, tm = L % tiles_m, m0 = tm * BM;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kb = SPLIT ? blockIdx.y * a.piece : 0;                 // first step
+  const int kt = (SPLIT ? min(a.kt, kb + a.piece) : a.kt) - kb;    // steps
+  const int nst = (kt + 1) / 2;                                    // stages
+
+  // activation DMA: block (row tile, half) of the stage; row tiles past M repeat the last one (never stored)
+  const int last_tile = (a.M - m0 - 1) / 16;
+  const rsrc_t ra = make_rsrc(a.A + (size_t)(m0 / 16) * a.kt * 1024, (uint32_t)min(TM, last_tile + 1) * a.kt * 1024);
+  int a_off[A_PW], a_dst[A_PW];
+#pragma unroll
+  for (int u = 0; u < A_PW; ++u) {
+    const int b = min(w * A_PW + u, A_BLK - 1), rt = b >> 1, kk = b & 1;
+    a_dst[u] = b * 1024;
+    a_off[u] = (min(rt, last_tile) * a.kt + kk) * 1024 + lane * 16;
+  }
+  auto issue_a = [&](int s, uint8_t* base) __attribute__((always_inline)) {
+    const int past = s >= nst ? kOutOfRange : 0;   // past the last stage nothing is read; by or-ing, without a branch
+#pragma unroll
+    for (int u = 0; u < A_PW; ++u)
+      buf_dma16(ra, a_off[u] | past, (kb + 2 * min(s, nst - 1)) * 1024, base + a_dst[u]);
+  };
+  const int c0 = tn * BN + w * 16 * HALF;                          // the wavefront's first output column
+  const int b_tiles = (a.N + 15) / 16, bt = min(c0 / 16, b_tiles - 1);
+  const uint32_t b_bytes = (uint32_t)min(HALF, b_tiles - bt) * a.kt * 1024;
+  const rsrc_t rb0 = make_rsrc(a.B + (size_t)bt * a.kt * 1024, b_bytes);
+  const rsrc_t rb1 = SW ? make_rsrc(a.B2 + (size_t)bt * a.kt * 1024, b_bytes) : rb0;
+  int b_off[HALF];
+#pragma unroll
+  for (int j = 0; j < HALF; ++j) b_off[j] = lane * 16 + j * a.kt * 1024;
+  uint4 fb[R][NW];
+  auto load_b = [&](auto rc, int k) __attribute__((always_inline)) {
+    constexpr int r = decltype(rc)::value % R;
+    const int kk = kb + min(k, kt - 1), past = k < kt ? 0 : kOutOfRange;
+#pragma unroll
+    for (int j = 0; j < NW; ++j)   // past the last step: zeros
+      fb[r][j] = buf_load16<CACHE>(j < HALF ? rb0 : rb1, b_off[j % HALF] | past, kk * 1024);
+  };
+  i32x4 acc[TM][NW];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < NW; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  uint4 fa[TM];
+  auto read_a = [&](const uint8_t* base, int i, int h) __attribute__((always_inline)) {
+    return *reinterpret_cast<const uint4*>(base + i * 2048 + h * 1024 + lane * 16);
+  };
+  // one step with the weights of ring slot r; reads the next step's fragments as it goes
+  auto step = [&](auto rc, const uint8_t* next, int h) __attribute__((always_inline)) {
+    constexpr int r = decltype(rc)::value % R;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+      for (int j = 0; j < NW; ++j) acc[i][j] = mfma16x16x64(fb[r][j], fa[i], acc[i][j]);
+      fa[i] = read_a(next, i, h);
+    }
+    static_for<TM>([&](auto) {
+      __builtin_amdgcn_sched_group_barrier(0x008, NW, 0);   // MFMAs
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);    // one LDS read
+    });
+  };
+  static_for<NS - 1>([&](auto ic) {
+    issue_a(decltype(ic)::value, slot(ic));
+    __builtin_amdgcn_sched_barrier(0);   // the waits below count in this order
+  });
+  static_for<R>([&](auto ic) { load_b(ic, decltype(ic)::value); });
+  __builtin_amdgcn_sched_barrier(0);
+  wait_vmcnt<NW * R + (NS - 2) * A_PW>();
+  __builtin_amdgcn_s_barrier();
+#pragma unroll
+  for (int i = 0; i < TM; ++i) fa[i] = read_a(L0, i, 0);
+  step(std::integral_constant<int, 0>{}, L0, 1);
+  load_b(std::integral_constant<int, 0>{}, R);
+  __builtin_amdgcn_sched_barrier(0);
+  // pass s: the second step of stage s (it reads stage s + 1's first fragments) and the first of stage s + 1.
+  // Every LDS read follows, without a branch, the wait for its stage's DMA, and the loop has one exit: otherwise
+  // the compiler adds waits for everything in flight.  Whole trips of 2 NS steps; a last trip that has at least three
+  // steps of its own runs on over zeros, which costs less than so many single steps.
+  const int s_end = (kt - 1 + 2 * NS - 3) / (2 * NS) * NS;
+  int s0 = 0;
+  for (; s0 < s_end; s0 += NS) {
+    static_for<NS>([&](auto ic) {
+      constexpr int J = decltype(ic)::value;
+      wait_vmcnt<WAIT>();
+      __builtin_amdgcn_s_barrier();
+      issue_a(s0 + J + NS - 1, slot(std::integral_constant<int, J + NS - 1>{}));
+      const uint8_t* next = slot(std::integral_constant<int, J + 1>{});
+      step(std::integral_constant<int, 2 * J + 1>{}, next, 0);
+      load_b(std::integral_constant<int, 2 * J + 1>{}, (s0 + J) * 2 + 1 + R);
+      __builtin_amdgcn_sched_barrier(0);
+      step(std::integral_constant<int, 2 * J + 2>{}, next, 1);
+      load_b(std::integral_constant<int, 2 * J + 2>{}, (s0 + J) * 2 + 2 + R);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  }
+  // one or two remaining steps singly, the ring shifted by copies
+  auto dyn_slot = [&](int i) -> uint8_t* {
+    i %= NS;
+    return i == 0 ? L0 : i == 1 ? L1 : i == 2 ? L2 : L3;
+  };
+  for (int k = 2 * s0 + 1; k < kt; ++k) {
+    if (k & 1) {
+      wait_vmcnt<0>();
+      __builtin_amdgcn_s_barrier();
+      issue_a((k >> 1) + NS - 1, dyn_slot((k >> 1) + NS - 1));
+    }
+    step(std::integral_constant<int, 1>{}, dyn_slot((k >> 1) + (k & 1)), (k & 1) ^ 1);
+#pragma unroll
+    for (int j = 0; j < NW; ++j) {
+#pragma unroll
+      for (int r = 1; r < R; ++r) fb[r][j] = fb[(r + 1) % R][j];
+    }
+    load_b(std::integral_constant<int, 0>{}, k + R);
+  }
+  wait_vmcnt<0>();
+
+  // lane holds row l % 16 and columns 4 (l / 16) .. + 3 of each 16 x 16 tile
+  const int col4 = (lane >> 4) * 4;
+  if constexpr (SPLIT) {
+    const int n_all = SW ? 2 * a.N : a.N;
+    int32_t* P = a.partial + (size_t)blockIdx.y * a.M * n_all;
+    const bool vec = (a.N & 3) == 0;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int row = m0 + i * 16 + (lane & 15);
+      if (row >= a.M) continue;
+#pragma unroll
+      for (int j = 0; j < NW; ++j) {
+        const int col = c0 + (j % HALF) * 16 + col4;
+        if (col >= a.N) continue;
+        int32_t* p = P + (size_t)row * n_all + (j < HALF ? 0 : a.N) + col;
+        if (vec) *reinterpret_cast<i32x4*>(p) = acc[i][j];
+        else for (int e = 0; e < 4 && col + e < a.N; ++e) p[e] = acc[i][j][e];
+      }
+    }
+  } else {
+    const bool vec = aligned4<EPI>(a);
+    float4 sb[NW];
+#pragma unroll
+    for (int j = 0; j < NW; ++j) {
+      const int col = min(c0 + (j % HALF) * 16 + col4, a.N - 1);
+      sb[j] = load_scales(j < HALF ? a.sb : a.sb2, col, a.N);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int row = m0 + i * 16 + (lane & 15);
+      if (row >= a.M) continue;
+      const float sa = a.sa[row];
+#pragma unroll
+      for (int j = 0; j < HALF; ++j) {
+        const int col = c0 + j * 16 + col4;
+        if (col >= a.N) continue;
+        f32x4 y = scaled(acc[i][j], sa, sb[j]);
+        if constexpr (SW) {
+          const f32x4 u = scaled(acc[i][j + HALF], sa, sb[j + HALF]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = swiglu(y[e], u[e]);
+        }
+        store4<EPI>(a, row, col, y, vec);
+      }
+    }
+  }
+}
+
+template <int TM, int NW, int WV, int CACHE, int EPI, bool SPLIT>
+hipError_t launch_i8(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st) {
+  constexpr int BM = 16 * TM, BN = 16 * (EPI == EPI_SWIGLU ? NW / 2 : NW) * WV, R = WV == 8 ? 2 : NW == 2 ? 8 : 4;
+  const unsigned nb = (unsigned)((a.M + BM - 1) / BM) * (unsigned)((a.N + BN - 1) / BN);
+  hipLaunchKernelGGL((gemm_i8_kernel<TM, NW, R, EPI, SPLIT, WV, WV / 4, CACHE>), dim3(nb, p.splits), dim3(64 * WV), 0,
+                     st, a);
+  return hipGetLastError();
+}
+
+template <int EPI, bool SPLIT>
+hipError_t launch_i8_cfg(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st) {
+#define HXF_I8(T, NW, WV, CACHE) \
+  case T: return launch_i8<T, NW, WV, CACHE, EPI, SPLIT>(a, p, st);
+  if (p.nw == 2 && p.once) switch (p.tm) {
+      HXF_I8(1, 2, 4, 2) HXF_I8(2, 2, 4, 2) HXF_I8(4, 2, 4, 2) HXF_I8(8, 2, 4, 2)
+    }
+  else if (p.nw == 2) switch (p.tm) {
+      HXF_I8(3, 2, 4, 0) HXF_I8(4, 2, 4, 0) HXF_I8(5, 2, 4, 0) HXF_I8(6, 2, 4, 0) HXF_I8(7, 2, 4, 0)
+      HXF_I8(8, 2, 4, 0) HXF_I8(9, 2, 4, 0) HXF_I8(10, 2, 4, 0) HXF_I8(11, 2, 4, 0) HXF_I8(12, 2, 4, 0)
+    }
+  else if (p.wv == 4 && p.once) switch (p.tm) {
+      HXF_I8(1, 4, 4, 2) HXF_I8(2, 4, 4, 2) HXF_I8(4, 4, 4, 2) HXF_I8(6, 4, 4, 2) HXF_I8(8, 4, 4, 2)
+      HXF_I8(10, 4, 4, 2) HXF_I8(12, 4, 4, 2) HXF_I8(14, 4, 4, 2) HXF_I8(16, 4, 4, 2)
+    }
+  else if (p.wv == 4) switch (p.tm) {
+      HXF_I8(4, 4, 4, 0) HXF_I8(5, 4, 4, 0) HXF_I8(6, 4, 4, 0) HXF_I8(7, 4, 4, 0) HXF_I8(8, 4, 4, 0)
+      HXF_I8(9, 4, 4, 0) HXF_I8(10, 4, 4, 0) HXF_I8(11, 4, 4, 0) HXF_I8(12, 4, 4, 0) HXF_I8(13, 4, 4, 0)
+      HXF_I8(14, 4, 4, 0) HXF_I8(15, 4, 4, 0) HXF_I8(16, 4, 4, 0)
+    }
+  else switch (p.tm) {
+      HXF_I8(9, 4, 8, 0)
+    }
+#undef HXF_I8
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+}  // namespace hxf

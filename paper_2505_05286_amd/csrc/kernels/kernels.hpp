@@ -98,7 +98,23 @@ struct GemmI8Args {
   int32_t* partial;                // split-K partials
   int M, N, ldc;                   // N: output columns
   int kt;                          // K tiles, ceil(K / 64)
+  int piece;                       // K tiles of a piece (even)
 };
+struct GemmI8Plan {
+  int tm = 4, nw = 4, wv = 4;   // a workgroup's row tiles, column tiles per wavefront, wavefronts
+  bool once = false;            // one row of tiles: the weights are read once (non-temporal loads)
+  int splits = 1;
+  int piece = 0;                // K tiles of a piece (even)
+};
+GemmI8Plan gemm_i8_plan(int M, int N, int kt, bool swiglu);   // N output columns
+hipError_t gemm_i8_run(GemmI8Args a, int epi, const GemmI8Plan& p, hipStream_t st);
+// The kernel with one epilogue each (gemm_i8_*.hip)
+hipError_t gemm_i8_bf16(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
+hipError_t gemm_i8_resid(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
+hipError_t gemm_i8_swiglu(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
+hipError_t gemm_i8_f32(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
+hipError_t gemm_i8_split(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
+hipError_t gemm_i8_split_swiglu(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
 int64_t gemm_i8_ws_bytes(int M, int N, int K);   // N as the caller counts it (SwiGLU: 2F)
 hipError_t gemm_i8_launch(const GemmI8Args& a, int epi, hipStream_t st);
 
