@@ -4,9 +4,16 @@
 // what the norm divides by, which cancels in the codes.  Every step of a code is one correctly rounded fp32
 // operation, so the codes do not depend on how a row is shared out.
 //
-// Memory is the bound (3 bytes a value, 5 with the norm).  A workgroup takes four rows; a wavefront's unit is four
-// rows x 256 columns, a lane's 16 successive values of one row: they are one 16-byte piece of a tile, and the four
-// rows' pieces are neighbours there.  A row's values stay in registers between the maximum and the codes.
+// Memory is the bound (3 bytes a value, 5 with the norm).  A workgroup takes ROWS rows, 64 / ROWS lanes of a wavefront
+// each: successive lanes load successive 16 bytes of a row (sixteen values of one row a lane, in whole pieces of a
+// tile, stored 16 bytes at once but loaded from four rows' lines by every four lanes, took 20.4 us instead of 16.3 for
+// the norm of 2080 x 5120), and the rows' pieces are neighbours in the tile.  A row's values stay in registers between
+// the maximum and the codes (read twice instead: 2080 x 28672 in 57 us instead of 46).
+//
+// ROWS = 4 up to K of 8192, 4096 with the norm, where a workgroup is small: 2 above, where four rows would fill a CU's
+// registers and no other row is loaded while one is written (us with 4 and with 2 rows, wavefronts chosen for each:
+// 2080 x 28672 48.6 / 46.2, 64 x 28672 9.9 / 6.5, 2080 x 14336 25.8 / 22.9; the norm of 2080 x 8192 25.9 / 22.3, of
+// 256 x 8192 8.1 / 6.1; but 16000 x 512 7.5 / 9.9 and 6144 x 4096 17.9 / 17.4).
 #include "common.hpp"
 #include "gemm_util.hpp"
 #include "kernels.hpp"
@@ -16,7 +23,6 @@ namespace hxf {
 namespace {
 
 constexpr float kTiny = 0x1p-119f;   // below it 127 / m may be no fp32 number
-constexpr int kRows = 4, kUnit = 256;
 
 struct RowMax {
   float inv, unit;   // 127 / m and m / 127
@@ -48,49 +54,50 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, f
   return lo | hi;
 }
 
-// Maximum of a row over the workgroup (NWV wavefronts; a lane's row is lane % 4), and the sum of s
-template <int NWV, bool SUM>
+// Maximum of a row over the workgroup (NWV wavefronts; a lane's row is lane / (64 / ROWS)), and the sum of s
+template <int ROWS, int NWV, bool SUM>
 __device__ __forceinline__ uint32_t rows_reduce(uint32_t m, float& s, uint32_t* red, float* sums) {
-  const int lane = threadIdx.x & 63, row = lane & (kRows - 1);
+  const int lane = threadIdx.x & 63, row = lane / (64 / ROWS);
 #pragma unroll
-  for (int o = 32; o >= kRows; o >>= 1) {
+  for (int o = 32 / ROWS; o >= 1; o >>= 1) {
     m = max(m, (uint32_t)__shfl_xor((int)m, o, kWave));
     if constexpr (SUM) s += __shfl_xor(s, o, kWave);
   }
-  if (lane < kRows) {
-    red[(threadIdx.x >> 6) * kRows + lane] = m;
-    if constexpr (SUM) sums[(threadIdx.x >> 6) * kRows + lane] = s;
+  if ((lane & (64 / ROWS - 1)) == 0) {
+    red[(threadIdx.x >> 6) * ROWS + row] = m;
+    if constexpr (SUM) sums[(threadIdx.x >> 6) * ROWS + row] = s;
   }
   __syncthreads();
   m = red[row];
 #pragma unroll
-  for (int w = 1; w < NWV; ++w) m = max(m, red[w * kRows + row]);
+  for (int w = 1; w < NWV; ++w) m = max(m, red[w * ROWS + row]);
   if constexpr (SUM) {
     s = sums[row];
 #pragma unroll
-    for (int w = 1; w < NWV; ++w) s += sums[w * kRows + row];
+    for (int w = 1; w < NWV; ++w) s += sums[w * ROWS + row];
   }
   return m;
 }
 
 __device__ __forceinline__ uint4 load16(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
 
-// V: units of a wavefront held in registers; 0: any number of them, read twice.
-template <int NWV, int V>
+// V: units (ROWS rows x 1024 / ROWS columns) of a wavefront held in registers; 0: any number of them, read twice.
+template <int ROWS, int NWV, int V>
 __global__ __launch_bounds__(64 * NWV) void quant_i8_kernel(const uint16_t* x, int64_t stride, int R, int K,
                                                             int8_t* codes, float* scale) {
-  __shared__ uint32_t red[NWV * kRows];
+  __shared__ uint32_t red[NWV * ROWS];
+  constexpr int LPR = 64 / ROWS, UNIT = 16 * LPR;
   const int kt = (K + 63) / 64, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int r = xcd_remap(blockIdx.x, gridDim.x) * kRows + (lane & (kRows - 1));
-  const int c0 = w * kUnit + (lane / kRows) * 16;   // the lane's first column of the wavefront's first unit
+  const int r = xcd_remap(blockIdx.x, gridDim.x) * ROWS + lane / LPR;
+  const int c0 = w * UNIT + (lane & (LPR - 1)) * 8;
   const bool live = r < R;
   const uint16_t* row = x + (int64_t)min(r, R - 1) * stride;
   struct Vals {
     uint32_t v[8];
   };
   auto load = [&](int k) {   // what is outside the matrix is zero
-    const bool in0 = live && k < K, in1 = live && k + 8 < K;
-    const uint4 p = load16(row + (in0 ? k : 0)), q = load16(row + (in1 ? k + 8 : 0));
+    const bool in0 = live && k < K, in1 = live && k + LPR * 8 < K;
+    const uint4 p = load16(row + (in0 ? k : 0)), q = load16(row + (in1 ? k + LPR * 8 : 0));
     return Vals{{in0 ? p.x : 0, in0 ? p.y : 0, in0 ? p.z : 0, in0 ? p.w : 0, in1 ? q.x : 0, in1 ? q.y : 0,
                  in1 ? q.z : 0, in1 ? q.w : 0}};
   };
@@ -103,45 +110,50 @@ __global__ __launch_bounds__(64 * NWV) void quant_i8_kernel(const uint16_t* x, i
   uint32_t m = 0;
   if constexpr (V > 0) {
 #pragma unroll
-    for (int u = 0; u < V; ++u) held[u] = load(c0 + u * NWV * kUnit);
+    for (int u = 0; u < V; ++u) held[u] = load(c0 + u * NWV * UNIT);
 #pragma unroll
     for (int u = 0; u < V; ++u) m = largest(held[u], m);
   } else {
-    for (int k = c0; k < K; k += NWV * kUnit) m = largest(load(k), m);
+    for (int k = c0; k < K; k += NWV * UNIT) m = largest(load(k), m);
   }
   float none = 0.f;
-  const RowMax q = row_max(rows_reduce<NWV, false>(max(m << 16, m & 0xFFFF0000u), none, red, nullptr));
+  const RowMax q = row_max(rows_reduce<ROWS, NWV, false>(max(m << 16, m & 0xFFFF0000u), none, red, nullptr));
   const uint32_t keep = q.inv != 0.f ? ~0u : 0u;   // 0 times an infinity is none
   int8_t* out = codes + i8_elem(r, 0, kt);
   auto store = [&](const Vals& a, int k) {
-    if (k >= kt * 64) return;
-    uint32_t o[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t p = a.v[2 * e], s = a.v[2 * e + 1];
-      o[e] = codes4(__uint_as_float(p << 16), __uint_as_float(p & 0xFFFF0000u), __uint_as_float(s << 16),
-                    __uint_as_float(s & 0xFFFF0000u), q.inv) & keep;
+    for (int h = 0; h < 2; ++h) {
+      const int kk = k + LPR * 8 * h;
+      if (kk >= kt * 64) return;
+      uint32_t o[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t p = a.v[4 * h + 2 * e], s = a.v[4 * h + 2 * e + 1];
+        o[e] = codes4(__uint_as_float(p << 16), __uint_as_float(p & 0xFFFF0000u), __uint_as_float(s << 16),
+                      __uint_as_float(s & 0xFFFF0000u), q.inv) & keep;
+      }
+      *reinterpret_cast<uint2*>(out + (kk >> 6) * 1024 + ((kk >> 4) & 3) * 256 + (kk & 15)) = make_uint2(o[0], o[1]);
     }
-    *reinterpret_cast<uint4*>(out + (k >> 6) * 1024 + ((k >> 4) & 3) * 256) = make_uint4(o[0], o[1], o[2], o[3]);
   };
   if constexpr (V > 0) {
 #pragma unroll
-    for (int u = 0; u < V; ++u) store(held[u], c0 + u * NWV * kUnit);
+    for (int u = 0; u < V; ++u) store(held[u], c0 + u * NWV * UNIT);
   } else {
-    for (int k = c0; k < kt * 64; k += NWV * kUnit) store(load(k), k);
+    for (int k = c0; k < kt * 64; k += NWV * UNIT) store(load(k), k);
   }
-  if (live && threadIdx.x < kRows) scale[r] = q.unit;
+  if (live && w == 0 && (lane & (LPR - 1)) == 0) scale[r] = q.unit;
 }
 
-template <int NWV, int V>
+template <int ROWS, int NWV, int V>
 __global__ __launch_bounds__(64 * NWV) void rmsnorm_i8_kernel(const float* x, const int32_t* rows, int x_rows,
                                                               const uint16_t* g, int8_t* codes, float* scale,
                                                               int n_rows, int d, float eps) {
-  __shared__ uint32_t red[NWV * kRows];
-  __shared__ float sums[NWV * kRows];
+  __shared__ uint32_t red[NWV * ROWS];
+  __shared__ float sums[NWV * ROWS];
+  constexpr int LPR = 64 / ROWS, UNIT = 16 * LPR;
   const int kt = (d + 63) / 64, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int r = xcd_remap(blockIdx.x, gridDim.x) * kRows + (lane & (kRows - 1));
-  const int c0 = w * kUnit + (lane / kRows) * 16;
+  const int r = xcd_remap(blockIdx.x, gridDim.x) * ROWS + lane / LPR;
+  const int c0 = w * UNIT + (lane & (LPR - 1)) * 4;
   int src = r < n_rows ? r : -1;
   if (rows && r < n_rows) src = rows[r];
   const bool live = src >= 0 && src < x_rows;
@@ -155,9 +167,9 @@ __global__ __launch_bounds__(64 * NWV) void rmsnorm_i8_kernel(const float* x, co
     Vals a;
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
-      const bool in = live && k + 4 * h < d;
+      const bool in = live && k + LPR * 4 * h < d;
       float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (in) p = *reinterpret_cast<const float4*>(row + k + 4 * h);
+      if (in) p = *reinterpret_cast<const float4*>(row + k + LPR * 4 * h);
       a.v[4 * h] = p.x, a.v[4 * h + 1] = p.y, a.v[4 * h + 2] = p.z, a.v[4 * h + 3] = p.w;
     }
     return a;
@@ -165,7 +177,7 @@ __global__ __launch_bounds__(64 * NWV) void rmsnorm_i8_kernel(const float* x, co
   auto gain = [&](Vals& a, int k) {   // x * g
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
-      const uint2 p = *reinterpret_cast<const uint2*>(g + (k + 4 * h < d ? k + 4 * h : 0));
+      const uint2 p = *reinterpret_cast<const uint2*>(g + (k + LPR * 4 * h < d ? k + LPR * 4 * h : 0));
       a.v[4 * h] *= __uint_as_float(p.x << 16);
       a.v[4 * h + 1] *= __uint_as_float(p.x & 0xFFFF0000u);
       a.v[4 * h + 2] *= __uint_as_float(p.y << 16);
@@ -182,79 +194,69 @@ __global__ __launch_bounds__(64 * NWV) void rmsnorm_i8_kernel(const float* x, co
   Vals held[V ? V : 1];
   if constexpr (V > 0) {
 #pragma unroll
-    for (int u = 0; u < V; ++u) held[u] = load(c0 + u * NWV * kUnit);
+    for (int u = 0; u < V; ++u) held[u] = load(c0 + u * NWV * UNIT);
 #pragma unroll
-    for (int u = 0; u < V; ++u) take(held[u], c0 + u * NWV * kUnit);
+    for (int u = 0; u < V; ++u) take(held[u], c0 + u * NWV * UNIT);
   } else {
-    for (int k = c0; k < d; k += NWV * kUnit) {
+    for (int k = c0; k < d; k += NWV * UNIT) {
       Vals a = load(k);
       take(a, k);
     }
   }
-  const RowMax q = row_max(rows_reduce<NWV, true>(m, ss, red, sums));
+  const RowMax q = row_max(rows_reduce<ROWS, NWV, true>(m, ss, red, sums));
   const uint32_t keep = q.inv != 0.f ? ~0u : 0u;
   int8_t* out = codes + i8_elem(r, 0, kt);
   auto store = [&](const Vals& a, int k) {
-    if (k >= kt * 64) return;
-    uint32_t o[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      o[e] = codes4(a.v[4 * e], a.v[4 * e + 1], a.v[4 * e + 2], a.v[4 * e + 3], q.inv) & keep;
-    *reinterpret_cast<uint4*>(out + (k >> 6) * 1024 + ((k >> 4) & 3) * 256) = make_uint4(o[0], o[1], o[2], o[3]);
+    for (int e = 0; e < 4; ++e) {
+      const int kk = k + LPR * 4 * e;
+      if (kk >= kt * 64) return;
+      *reinterpret_cast<uint32_t*>(out + (kk >> 6) * 1024 + ((kk >> 4) & 3) * 256 + (kk & 15)) =
+          codes4(a.v[4 * e], a.v[4 * e + 1], a.v[4 * e + 2], a.v[4 * e + 3], q.inv) & keep;
+    }
   };
   if constexpr (V > 0) {
 #pragma unroll
-    for (int u = 0; u < V; ++u) store(held[u], c0 + u * NWV * kUnit);
+    for (int u = 0; u < V; ++u) store(held[u], c0 + u * NWV * UNIT);
   } else {
-    for (int k = c0; k < kt * 64; k += NWV * kUnit) {
+    for (int k = c0; k < kt * 64; k += NWV * UNIT) {
       Vals a = load(k);
       gain(a, k);
       store(a, k);
     }
   }
-  if (r < n_rows && threadIdx.x < kRows) scale[r] = live ? q.unit * rsqrtf(ss / (float)d + eps) : 0.f;
+  if (r < n_rows && w == 0 && (lane & (LPR - 1)) == 0)
+    scale[r] = live ? q.unit * rsqrtf(ss / (float)d + eps) : 0.f;
 }
 
 }  // namespace
 
 hipError_t quant_i8_launch(const uint16_t* x, int64_t stride, int R, int K, int8_t* codes, float* scale,
                            hipStream_t st) {
-  const dim3 grid((R + 15) / 16 * (16 / kRows));
-#define HXF_Q(W, V)                                                                                            \
-  do {                                                                                                         \
-    hipLaunchKernelGGL((quant_i8_kernel<W, V>), grid, dim3(64 * W), 0, st, x, stride, R, K, codes, scale);     \
-    return hipGetLastError();                                                                                  \
-  } while (0)
-  const int units = (K + kUnit - 1) / kUnit;
-  if (units <= 4) HXF_Q(4, 1);
-  if (units <= 8) HXF_Q(4, 2);
-  if (units <= 16) HXF_Q(4, 4);
-  if (units <= 32) HXF_Q(8, 4);
-  if (units <= 56) HXF_Q(8, 7);
-  if (units <= 80) HXF_Q(8, 10);
-  if (units <= 112) HXF_Q(8, 14);
-  HXF_Q(8, 0);
+#define HXF_Q(ROWS, W, V)                                                                                           \
+  if (K <= ROWS_K(ROWS, W, V)) {                                                                                    \
+    hipLaunchKernelGGL((quant_i8_kernel<ROWS, W, V>), dim3((R + 15) / 16 * (16 / ROWS)), dim3(64 * W), 0, st, x,    \
+                       stride, R, K, codes, scale);                                                                 \
+    return hipGetLastError();                                                                                       \
+  }
+#define ROWS_K(ROWS, W, V) (V ? W * V * 1024 / ROWS : INT32_MAX)
+  HXF_Q(4, 4, 1) HXF_Q(4, 8, 1) HXF_Q(4, 8, 2) HXF_Q(4, 8, 4) HXF_Q(2, 16, 2) HXF_Q(2, 16, 4) HXF_Q(2, 16, 0)
+  return hipErrorInvalidValue;
 #undef HXF_Q
 }
 
 hipError_t rmsnorm_i8_launch(const float* x, const int32_t* rows, int x_rows, const uint16_t* g, int8_t* codes,
                              float* scale, int n_rows, int d, float eps, hipStream_t st) {
-  const dim3 grid((n_rows + 15) / 16 * (16 / kRows));
-#define HXF_N(W, V)                                                                                                 \
-  do {                                                                                                              \
-    hipLaunchKernelGGL((rmsnorm_i8_kernel<W, V>), grid, dim3(64 * W), 0, st, x, rows, x_rows, g, codes, scale, n_rows, \
-                       d, eps);                                                                                     \
+#define HXF_N(ROWS, W, V)                                                                                           \
+  if (d <= ROWS_K(ROWS, W, V)) {                                                                                    \
+    hipLaunchKernelGGL((rmsnorm_i8_kernel<ROWS, W, V>), dim3((n_rows + 15) / 16 * (16 / ROWS)), dim3(64 * W), 0, st, \
+                       x, rows, x_rows, g, codes, scale, n_rows, d, eps);                                           \
     return hipGetLastError();                                                                                       \
-  } while (0)
-  const int units = (d + kUnit - 1) / kUnit;
-  if (units <= 4) HXF_N(4, 1);
-  if (units <= 8) HXF_N(4, 2);
-  if (units <= 16) HXF_N(8, 2);
-  if (units <= 24) HXF_N(8, 3);
-  if (units <= 32) HXF_N(8, 4);
-  if (units <= 56) HXF_N(8, 7);
-  HXF_N(8, 0);
+  }
+  HXF_N(4, 4, 1) HXF_N(4, 8, 1) HXF_N(2, 8, 1) HXF_N(2, 16, 1) HXF_N(2, 16, 2) HXF_N(2, 16, 0)
+  return hipErrorInvalidValue;
 #undef HXF_N
+#undef ROWS_K
 }
 
 }  // namespace hxf

@@ -579,7 +579,8 @@ int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_
 
 namespace {
 
-bool i8_matrix_ok(int32_t R, int32_t K) { return R >= 0 && R < (1 << 24) && K > 0 && K < (1 << 17); }
+// (at most 512 threads a row: under 2^32 of them)
+bool i8_matrix_ok(int32_t R, int32_t K) { return R >= 0 && R < (1 << 22) && K > 0 && K < (1 << 17); }
 
 }  // namespace
 
@@ -605,7 +606,7 @@ int hxf_op_rmsnorm_i8(const float* x, const int32_t* rows, int32_t x_rows, const
 namespace {
 
 bool gemm_i8_ok(int32_t M, int32_t N, int32_t K) {
-  return i8_matrix_ok(M, K) && N > 0 && i8_matrix_ok(N, K) && (int64_t)M * N < (int64_t(1) << 40);
+  return i8_matrix_ok(M, K) && N > 0 && i8_matrix_ok(N, K) && (int64_t)M * N < (int64_t(1) << 36);
 }
 
 }  // namespace
