@@ -42,6 +42,7 @@ SOURCES = [
     "kernels/kv8.hip",
     "kernels/kv8_attention.hip",
     "kernels/quant_i8.hip",
+    "kernels/gemm_i8_thin.hip",
     "kernels/gemm_i8.hip",
     "kernels/misc.hip",
 ]

@@ -16,12 +16,12 @@ __global__ __launch_bounds__(256) void gemm_i8_join_kernel(GemmI8Args a, int S) 
   if (idx >= (int64_t)a.M * quads) return;
   const int row = (int)(idx / quads), col = (int)(idx % quads) * 4;
   const size_t MN = (size_t)a.M * n_all;
-  const bool wide = (a.N & 3) == 0;
+  const bool whole = col + 3 < a.N;
   auto sum = [&](int c) {
     const int32_t* p = a.partial + (size_t)row * n_all + c;
     i32x4 s = {0, 0, 0, 0};
-    if (wide) {
-      for (int z = 0; z < S; ++z) s += *reinterpret_cast<const i32x4*>(p + z * MN);
+    if (whole) {
+      for (int z = 0; z < S; ++z) s += load4<i32x4>(p + z * MN);
     } else {
       for (int z = 0; z < S; ++z)
         for (int e = 0; e < 4 && col + e < a.N; ++e) s[e] += p[z * MN + e];
@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256) void gemm_i8_join_kernel(GemmI8Args a, int S) 
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = swiglu(y[e], u[e]);
   }
-  store4<EPI>(a, row, col, y, aligned4<EPI>(a));
+  store4<EPI>(a, row, col, y);
 }
 
 template <int EPI>

@@ -14,10 +14,22 @@ __device__ __forceinline__ i32x4 mfma16x16x64(uint4 a, uint4 b, i32x4 c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }
 
+// Four values at an address aligned to one of them: global memory takes 8 and 16 bytes at any address.
+template <typename V, typename T>
+__device__ __forceinline__ V load4(const T* p) {
+  V v;
+  __builtin_memcpy(&v, p, sizeof(V));
+  return v;
+}
+template <typename V, typename T>
+__device__ __forceinline__ void put4(T* p, V v) {
+  __builtin_memcpy(p, &v, sizeof(V));
+}
+
 // Epilogues of four columns of one row from col on; y = float(acc) * sa * sb, in this order: the first product has
 // the size of a sum of activations, while that of the two scales may pass below fp32's range.
 __device__ __forceinline__ float4 load_scales(const float* s, int col, int n) {
-  if (col + 3 < n) return make_float4(s[col], s[col + 1], s[col + 2], s[col + 3]);
+  if (col + 3 < n) return load4<float4>(s + col);
   float v[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] = s[min(col + e, n - 1)];
@@ -27,35 +39,29 @@ __device__ __forceinline__ f32x4 scaled(i32x4 acc, float sa, float4 sb) {
   return f32x4{(float)acc[0] * sa * sb.x, (float)acc[1] * sa * sb.y, (float)acc[2] * sa * sb.z,
                (float)acc[3] * sa * sb.w};
 }
-__device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + __expf(-g)) * u; }
+// (the reciprocal's last place is far below bf16's: a division takes ten instructions more)
+__device__ __forceinline__ float swiglu(float g, float u) { return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)) * u; }
 
-// vec: the four columns lie inside the row and their address is aligned to them
 template <int EPI>
-__device__ __forceinline__ void store4(const GemmI8Args& a, int row, int col, f32x4 y, bool vec) {
+__device__ __forceinline__ void store4(const GemmI8Args& a, int row, int col, f32x4 y) {
   const size_t o = (size_t)row * a.ldc + col;
+  const bool whole = col + 3 < a.N;
   if constexpr (EPI == EPI_BF16 || EPI == EPI_SWIGLU) {
     bf16_t* c = reinterpret_cast<bf16_t*>(a.C) + o;
-    if (vec) {
-      *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3]));
+    if (whole) {
+      put4(c, make_uint2(pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3])));
     } else {
       for (int e = 0; e < 4 && col + e < a.N; ++e) c[e] = f2bf(y[e]);
     }
   } else {
     float* c = reinterpret_cast<float*>(a.C) + o;
     constexpr bool ADD = EPI == EPI_RESID;
-    if (vec) {
-      const float4 x = ADD ? *reinterpret_cast<const float4*>(c) : make_float4(0.f, 0.f, 0.f, 0.f);
-      *reinterpret_cast<float4*>(c) = ADD ? make_float4(x.x + y[0], x.y + y[1], x.z + y[2], x.w + y[3])
-                                          : make_float4(y[0], y[1], y[2], y[3]);
+    if (whole) {
+      put4(c, ADD ? load4<f32x4>(c) + y : y);
     } else {
       for (int e = 0; e < 4 && col + e < a.N; ++e) c[e] = ADD ? c[e] + y[e] : y[e];
     }
   }
-}
-template <int EPI>
-__device__ __forceinline__ bool aligned4(const GemmI8Args& a) {
-  constexpr uintptr_t mask = EPI == EPI_BF16 || EPI == EPI_SWIGLU ? 7 : 15;
-  return ((a.ldc | a.N) & 3) == 0 && ((uintptr_t)a.C & mask) == 0;
 }
 
 // Macro tiles of 16 TM rows x 16 NW WV columns on the 16x16x64 i8 MFMA: WV wavefronts, each owning all the tile's
@@ -208,7 +214,6 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
   if constexpr (SPLIT) {
     const int n_all = SW ? 2 * a.N : a.N;
     int32_t* P = a.partial + (size_t)blockIdx.y * a.M * n_all;
-    const bool vec = (a.N & 3) == 0;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int row = m0 + i * 16 + (lane & 15);
@@ -218,12 +223,11 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
         const int col = c0 + (j % HALF) * 16 + col4;
         if (col >= a.N) continue;
         int32_t* p = P + (size_t)row * n_all + (j < HALF ? 0 : a.N) + col;
-        if (vec) *reinterpret_cast<i32x4*>(p) = acc[i][j];
+        if (col + 3 < a.N) put4(p, acc[i][j]);
         else for (int e = 0; e < 4 && col + e < a.N; ++e) p[e] = acc[i][j][e];
       }
     }
   } else {
-    const bool vec = aligned4<EPI>(a);
     float4 sb[NW];
 #pragma unroll
     for (int j = 0; j < NW; ++j) {
@@ -245,7 +249,7 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) y[e] = swiglu(y[e], u[e]);
         }
-        store4<EPI>(a, row, col, y, vec);
+        store4<EPI>(a, row, col, y);
       }
     }
   }
@@ -281,7 +285,7 @@ hipError_t launch_i8_cfg(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t s
       HXF_I8(14, 4, 4, 0) HXF_I8(15, 4, 4, 0) HXF_I8(16, 4, 4, 0)
     }
   else switch (p.tm) {
-      HXF_I8(9, 4, 8, 0)
+      HXF_I8(5, 4, 8, 0) HXF_I8(6, 4, 8, 0) HXF_I8(7, 4, 8, 0) HXF_I8(8, 4, 8, 0) HXF_I8(9, 4, 8, 0)
     }
 #undef HXF_I8
   return hipErrorInvalidValue;

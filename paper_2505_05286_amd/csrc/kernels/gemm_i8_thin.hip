@@ -1,0 +1,101 @@
+// The product of 8-bit codes for one or two row tiles (a decode step of a few sequences) in one launch: the wavefronts
+// of a workgroup share out K and join their sums in LDS.
+#include "gemm_i8.hpp"
+
+namespace hxf {
+
+namespace {
+
+// A workgroup owns 16 HALF output columns and all rows (TM tiles of 16); wavefront w multiplies the steps (64 of K)
+// w, w + WV, .. of both operands, which go straight to registers, R steps ahead.  Steps past the end are zeros that
+// no memory is read for.
+template <int TM, int HALF, int R, int EPI, int WV>
+__global__ __launch_bounds__(64 * WV) void gemm_i8_thin_kernel(GemmI8Args a) {
+  constexpr bool SW = EPI == EPI_SWIGLU;
+  constexpr int NW = SW ? 2 * HALF : HALF;
+  __shared__ __attribute__((aligned(16))) i32x4 part[WV][TM * NW][64];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c0 = blockIdx.x * 16 * HALF, b_tiles = (a.N + 15) / 16, bt = c0 / 16;
+  const uint32_t b_bytes = (uint32_t)min(HALF, b_tiles - bt) * a.kt * 1024;
+  const rsrc_t ra = make_rsrc(a.A, (uint32_t)((a.M + 15) / 16) * a.kt * 1024);
+  const rsrc_t rb0 = make_rsrc(a.B + (size_t)bt * a.kt * 1024, b_bytes);
+  const rsrc_t rb1 = SW ? make_rsrc(a.B2 + (size_t)bt * a.kt * 1024, b_bytes) : rb0;
+  uint4 fa[R][TM], fb[R][NW];
+  auto load = [&](auto rc, int s) __attribute__((always_inline)) {
+    constexpr int r = decltype(rc)::value;
+    const int k = w + s * WV, past = k < a.kt ? 0 : kOutOfRange, at = min(k, a.kt - 1) * 1024;
+#pragma unroll
+    for (int j = 0; j < NW; ++j)
+      fb[r][j] = buf_load16<2>(j < HALF ? rb0 : rb1, (lane * 16 + (j % HALF) * a.kt * 1024) | past, at);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) fa[r][i] = buf_load16(ra, (lane * 16 + i * a.kt * 1024) | past, at);
+  };
+  i32x4 acc[TM][NW];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < NW; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  const int n = (a.kt + WV - 1) / WV;
+  static_for<R>([&](auto rc) { load(rc, decltype(rc)::value); });
+  for (int s = 0; s < n; s += R) {
+    static_for<R>([&](auto rc) {
+      constexpr int r = decltype(rc)::value;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < NW; ++j) acc[i][j] = mfma16x16x64(fb[r][j], fa[r][i], acc[i][j]);
+      load(rc, s + R + r);
+    });
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < NW; ++j) part[w][i * NW + j][lane] = acc[i][j];
+  __syncthreads();
+  for (int t = w; t < TM * HALF; t += WV) {
+    const int i = t / HALF, j = t % HALF;
+    const int row = i * 16 + (lane & 15), col = c0 + j * 16 + (lane >> 4) * 4;
+    if (row >= a.M || col >= a.N) continue;
+    auto sum = [&](int tile) {
+      i32x4 s = part[0][tile][lane];
+#pragma unroll
+      for (int v = 1; v < WV; ++v) s += part[v][tile][lane];
+      return s;
+    };
+    const float sa = a.sa[row];
+    f32x4 y = scaled(sum(i * NW + j), sa, load_scales(a.sb, col, a.N));
+    if constexpr (SW) {
+      const f32x4 u = scaled(sum(i * NW + HALF + j), sa, load_scales(a.sb2, col, a.N));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = swiglu(y[e], u[e]);
+    }
+    store4<EPI>(a, row, col, y);
+  }
+}
+
+template <int TM, int HALF, int R, int WV>
+hipError_t launch_thin(const GemmI8Args& a, int epi, hipStream_t st) {
+  const dim3 grid((a.N + 16 * HALF - 1) / (16 * HALF)), block(64 * WV);
+  switch (epi) {
+    case EPI_BF16: hipLaunchKernelGGL((gemm_i8_thin_kernel<TM, HALF, R, EPI_BF16, WV>), grid, block, 0, st, a); break;
+    case EPI_RESID: hipLaunchKernelGGL((gemm_i8_thin_kernel<TM, HALF, R, EPI_RESID, WV>), grid, block, 0, st, a); break;
+    case EPI_SWIGLU: hipLaunchKernelGGL((gemm_i8_thin_kernel<TM, HALF, R, EPI_SWIGLU, WV>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((gemm_i8_thin_kernel<TM, HALF, R, EPI_F32, WV>), grid, block, 0, st, a); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// plan: tm row tiles, nw columns tiles, wv wavefronts
+hipError_t gemm_i8_thin(const GemmI8Args& a, int epi, const GemmI8Plan& p, hipStream_t st) {
+#define HXF_THIN(T, N, R, W) \
+  if (p.tm == T && p.nw == N && p.wv == W) return launch_thin<T, N, R, W>(a, epi, st);
+  HXF_THIN(1, 1, 8, 8) HXF_THIN(1, 1, 4, 16) HXF_THIN(1, 1, 8, 4) HXF_THIN(1, 2, 8, 8) HXF_THIN(1, 2, 4, 16)
+  HXF_THIN(2, 1, 8, 8) HXF_THIN(2, 1, 4, 16) HXF_THIN(2, 2, 4, 8) HXF_THIN(2, 2, 4, 16)
+  HXF_THIN(4, 1, 4, 8) HXF_THIN(4, 1, 4, 16) HXF_THIN(4, 2, 4, 8)
+#undef HXF_THIN
+  return hipErrorInvalidValue;
+}
+
+}  // namespace hxf

@@ -114,6 +114,7 @@ hipError_t gemm_i8_resid(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t s
 hipError_t gemm_i8_swiglu(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
 hipError_t gemm_i8_f32(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
 hipError_t gemm_i8_split(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
+hipError_t gemm_i8_thin(const GemmI8Args& a, int epi, const GemmI8Plan& p, hipStream_t st);
 hipError_t gemm_i8_split_swiglu(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
 int64_t gemm_i8_ws_bytes(int M, int N, int K);   // N as the caller counts it (SwiGLU: 2F)
 hipError_t gemm_i8_launch(const GemmI8Args& a, int epi, hipStream_t st);
