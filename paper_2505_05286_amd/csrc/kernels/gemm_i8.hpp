@@ -84,7 +84,7 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
   constexpr int WAIT = (NS - 3) * A_PW + 2 * NW * (NS - 2) - NW;
   static_assert((2 * NS) % R == 0 && WAIT < 64 && NW * R + (NS - 2) * A_PW < 64, "pipeline");
   static_assert(!SW || NW % 2 == 0, "a wavefront holds as many up columns as gate columns");
-  static_assert(NS * STAGE <= 160 * 1024, "stage layout");
+  static_assert(NS * STAGE + WV * 16 * (16 * HALF * 4 + 16) <= 160 * 1024, "stage layout");
   __shared__ __attribute__((aligned(1024))) uint8_t L0[STAGE], L1[STAGE], L2[STAGE], L3[STAGE];
   auto slot = [&](auto ic) -> uint8_t* {
     constexpr int I = decltype(ic)::value % NS;
@@ -209,48 +209,112 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
   }
   wait_vmcnt<0>();
 
-  // lane holds row l % 16 and columns 4 (l / 16) .. + 3 of each 16 x 16 tile
-  const int col4 = (lane >> 4) * 4;
-  if constexpr (SPLIT) {
-    const int n_all = SW ? 2 * a.N : a.N;
-    int32_t* P = a.partial + (size_t)blockIdx.y * a.M * n_all;
+  // A lane holds row l % 16 and columns 4 (l / 16) .. + 3 of each 16 x 16 tile.  A row tile's values pass through LDS
+  // (the wavefront's own part of it), so that a store covers whole rows of the wavefront's columns instead of 16 rows'
+  // pieces of 8 or 16 bytes.
+  constexpr bool WIDE = SPLIT || EPI == EPI_RESID || EPI == EPI_F32;       // 4 bytes a value, or 2
+  constexpr int COLS = 16 * HALF, SIZE = WIDE ? 4 : 2, PER = 16 / SIZE;    // columns, bytes a value, values per 16 bytes
+  constexpr int LPR = COLS / PER, RPI = 64 / LPR < 16 ? 64 / LPR : 16;      // lanes per row, rows per store
+  constexpr int INSTS = 16 / RPI;                                           // stores per row tile
+  constexpr int PITCH = COLS * SIZE + 16;                                  // bytes: rows start in different banks
+  __shared__ __attribute__((aligned(16))) uint8_t stage[WV][16 * PITCH];
+  uint8_t* mine = stage[w];
+  const int in_row = (lane & 15) * PITCH + (lane >> 4) * 4 * SIZE;          // where the lane writes, tile 0
+  const int out_row = lane / LPR % RPI, out_col = lane % LPR * PER, col0 = c0 + out_col;
+  const int n_all = SPLIT && SW ? 2 * a.N : a.N;
+  const size_t ld = SPLIT ? n_all : a.ldc;
+  uint8_t* const C = SPLIT ? reinterpret_cast<uint8_t*>(a.partial + (size_t)blockIdx.y * a.M * n_all)
+                           : reinterpret_cast<uint8_t*>(a.C);
+  const bool whole = col0 + PER <= a.N;
+  // put(i, shift): row tile i from LDS to its rows, `shift` columns to the right (up columns of a partial)
+  constexpr bool ADD = !SPLIT && EPI == EPI_RESID;
+  f32x4 old[ADD ? INSTS : 1];
+  auto place = [&](int i, int h, int shift) {
+    return C + ((size_t)(m0 + i * 16 + h * RPI + out_row) * ld + col0 + shift) * SIZE;
+  };
+  auto in_rows = [&](int i, int h) { return lane < RPI * LPR && m0 + i * 16 + h * RPI + out_row < a.M; };
+  auto fetch = [&](int i) {   // what the residual holds, one row tile ahead of its use
+    if constexpr (ADD) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int row = m0 + i * 16 + (lane & 15);
-      if (row >= a.M) continue;
+      for (int h = 0; h < INSTS; ++h)
+        if (in_rows(i, h) && whole) old[h] = load4<f32x4>(reinterpret_cast<const float*>(place(i, h, 0)));
+    }
+  };
+  // Other lanes of the wavefront read what a lane has written: without this the compiler takes a value that its own
+  // lane does not read as never read, and leaves it out
+  auto exchange = [] {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  auto put = [&](int i, int shift) {
+    exchange();
+    uint4 v[INSTS];
 #pragma unroll
-      for (int j = 0; j < NW; ++j) {
-        const int col = c0 + (j % HALF) * 16 + col4;
-        if (col >= a.N) continue;
-        int32_t* p = P + (size_t)row * n_all + (j < HALF ? 0 : a.N) + col;
-        if (col + 3 < a.N) put4(p, acc[i][j]);
-        else for (int e = 0; e < 4 && col + e < a.N; ++e) p[e] = acc[i][j][e];
+    for (int h = 0; h < INSTS; ++h)
+      v[h] = *reinterpret_cast<const uint4*>(mine + (h * RPI + out_row) * PITCH + out_col * SIZE);
+    exchange();
+    f32x4 was[ADD ? INSTS : 1];
+    if constexpr (ADD) {
+#pragma unroll
+      for (int h = 0; h < INSTS; ++h) was[h] = old[h];
+      if (i + 1 < TM) fetch(i + 1);
+    }
+#pragma unroll
+    for (int h = 0; h < INSTS; ++h) {
+      if (!in_rows(i, h)) continue;
+      uint8_t* c = place(i, h, shift);
+      if constexpr (WIDE) {
+        const f32x4 y = __builtin_bit_cast(f32x4, v[h]);
+        float* f = reinterpret_cast<float*>(c);
+        if (whole) {
+          if constexpr (ADD) put4(f, was[h] + y); else put4(f, v[h]);
+        } else {
+          for (int e = 0; e < 4 && col0 + e < a.N; ++e) f[e] = ADD ? f[e] + y[e] : y[e];
+        }
+      } else {
+        bf16_t* f = reinterpret_cast<bf16_t*>(c);
+        const uint32_t u[4] = {v[h].x, v[h].y, v[h].z, v[h].w};
+        if (whole) put4(f, v[h]);
+        else for (int e = 0; e < 8 && col0 + e < a.N; ++e) f[e] = (bf16_t)(u[e >> 1] >> (16 * (e & 1)));
       }
     }
+  };
+  if constexpr (SPLIT) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int g = 0; g < NW / HALF; ++g) {
+#pragma unroll
+        for (int j = 0; j < HALF; ++j)
+          *reinterpret_cast<i32x4*>(mine + in_row + j * 64) = acc[i][g * HALF + j];
+        put(i, g * a.N);
+      }
   } else {
+    fetch(0);
     float4 sb[NW];
 #pragma unroll
     for (int j = 0; j < NW; ++j) {
-      const int col = min(c0 + (j % HALF) * 16 + col4, a.N - 1);
+      const int col = min(c0 + (j % HALF) * 16 + (lane >> 4) * 4, a.N - 1);
       sb[j] = load_scales(j < HALF ? a.sb : a.sb2, col, a.N);
     }
+    float sa[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = a.sa[min(m0 + i * 16 + (lane & 15), a.M - 1)];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const int row = m0 + i * 16 + (lane & 15);
-      if (row >= a.M) continue;
-      const float sa = a.sa[row];
 #pragma unroll
       for (int j = 0; j < HALF; ++j) {
-        const int col = c0 + j * 16 + col4;
-        if (col >= a.N) continue;
-        f32x4 y = scaled(acc[i][j], sa, sb[j]);
+        f32x4 y = scaled(acc[i][j], sa[i], sb[j]);
         if constexpr (SW) {
-          const f32x4 u = scaled(acc[i][j + HALF], sa, sb[j + HALF]);
+          const f32x4 u = scaled(acc[i][j + HALF], sa[i], sb[j + HALF]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) y[e] = swiglu(y[e], u[e]);
         }
-        store4<EPI>(a, row, col, y);
+        if constexpr (WIDE) *reinterpret_cast<f32x4*>(mine + in_row + j * 64) = y;
+        else *reinterpret_cast<uint2*>(mine + in_row + j * 32) = make_uint2(pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3]));
       }
+      put(i, 0);
     }
   }
 }
@@ -258,8 +322,9 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
 template <int TM, int NW, int WV, int CACHE, int EPI, bool SPLIT>
 hipError_t launch_i8(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st) {
   constexpr int BM = 16 * TM, BN = 16 * (EPI == EPI_SWIGLU ? NW / 2 : NW) * WV, R = WV == 8 ? 2 : NW == 2 ? 8 : 4;
+  constexpr int OCC = WV == 8 || TM <= 7 ? 2 : 1;   // wavefronts a SIMD that the registers are to leave room for
   const unsigned nb = (unsigned)((a.M + BM - 1) / BM) * (unsigned)((a.N + BN - 1) / BN);
-  hipLaunchKernelGGL((gemm_i8_kernel<TM, NW, R, EPI, SPLIT, WV, WV / 4, CACHE>), dim3(nb, p.splits), dim3(64 * WV), 0,
+  hipLaunchKernelGGL((gemm_i8_kernel<TM, NW, R, EPI, SPLIT, WV, OCC, CACHE>), dim3(nb, p.splits), dim3(64 * WV), 0,
                      st, a);
   return hipGetLastError();
 }
