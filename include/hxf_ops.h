@@ -282,6 +282,11 @@ int hxf_op_rmsnorm_i8(const float* x, const int32_t* rows, int32_t x_rows, const
  * aligned, whose contents need not be kept between calls; calls that may overlap need one each.  No buffer may
  * overlap another. */
 int64_t hxf_op_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K);
+/* Introspection (host only, no device work): the plan hxf_op_gemm_i8 takes for these sizes:
+ * plan = {row tiles of 16, column tiles of 16 per wavefront, wavefronts, 1 if the weights are fetched as read once,
+ * pieces of K, tiles of 64 of K per piece, 1 if the wavefronts of a workgroup share out K (column tiles are then the
+ * workgroup's)}. */
+int hxf_op_gemm_i8_plan(int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t plan[7]);
 int hxf_op_gemm_i8(const void* A, const float* a_scale, const void* B, const float* b_scale, const void* B2,
                    const float* b2_scale, void* C, int32_t ldc, int32_t M, int32_t N, int32_t K, int32_t epilogue,
                    void* workspace, int64_t workspace_bytes, void* stream);

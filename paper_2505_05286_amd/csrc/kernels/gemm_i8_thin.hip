@@ -91,9 +91,7 @@ hipError_t launch_thin(const GemmI8Args& a, int epi, hipStream_t st) {
 hipError_t gemm_i8_thin(const GemmI8Args& a, int epi, const GemmI8Plan& p, hipStream_t st) {
 #define HXF_THIN(T, N, R, W) \
   if (p.tm == T && p.nw == N && p.wv == W) return launch_thin<T, N, R, W>(a, epi, st);
-  HXF_THIN(1, 1, 8, 8) HXF_THIN(1, 1, 4, 16) HXF_THIN(1, 1, 8, 4) HXF_THIN(1, 2, 8, 8) HXF_THIN(1, 2, 4, 16)
-  HXF_THIN(2, 1, 8, 8) HXF_THIN(2, 1, 4, 16) HXF_THIN(2, 2, 4, 8) HXF_THIN(2, 2, 4, 16)
-  HXF_THIN(4, 1, 4, 8) HXF_THIN(4, 1, 4, 16) HXF_THIN(4, 2, 4, 8)
+  HXF_THIN(1, 1, 8, 4) HXF_THIN(1, 2, 4, 16) HXF_THIN(2, 1, 4, 16) HXF_THIN(2, 2, 4, 8) HXF_THIN(4, 1, 4, 8) HXF_THIN(4, 2, 4, 8)
 #undef HXF_THIN
   return hipErrorInvalidValue;
 }

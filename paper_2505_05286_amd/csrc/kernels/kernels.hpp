@@ -105,8 +105,9 @@ struct GemmI8Plan {
   bool once = false;            // one row of tiles: the weights are read once (non-temporal loads)
   int splits = 1;
   int piece = 0;                // K tiles of a piece (even)
+  bool thin = false;            // gemm_i8_thin: wavefronts share K, nw column tiles a workgroup
 };
-GemmI8Plan gemm_i8_plan(int M, int N, int kt, bool swiglu);   // N output columns
+GemmI8Plan gemm_i8_plan(int M, int N, int kt, int epi);   // N output columns
 hipError_t gemm_i8_run(GemmI8Args a, int epi, const GemmI8Plan& p, hipStream_t st);
 // The kernel with one epilogue each (gemm_i8_*.hip)
 hipError_t gemm_i8_bf16(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
@@ -117,7 +118,8 @@ hipError_t gemm_i8_split(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t s
 hipError_t gemm_i8_thin(const GemmI8Args& a, int epi, const GemmI8Plan& p, hipStream_t st);
 hipError_t gemm_i8_split_swiglu(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
 int64_t gemm_i8_ws_bytes(int M, int N, int K);   // N as the caller counts it (SwiGLU: 2F)
-hipError_t gemm_i8_launch(const GemmI8Args& a, int epi, hipStream_t st);
+// hipErrorOutOfMemory (nothing enqueued) where the plan's partials need more than ws_bytes
+hipError_t gemm_i8_launch(const GemmI8Args& a, int epi, int64_t ws_bytes, hipStream_t st);
 
 // ------------------------------------------------------------------ norms / embedding
 // out[r] = bf16(rmsnorm(x[rows ? rows[r] : r]) * g); x fp32 [*, d]

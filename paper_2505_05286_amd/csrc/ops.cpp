@@ -615,6 +615,15 @@ int64_t hxf_op_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K) {
   return gemm_i8_ok(M, N, K) ? gemm_i8_ws_bytes(M, N, K) : -1;
 }
 
+int hxf_op_gemm_i8_plan(int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t plan[7]) {
+  const bool sw = epilogue == HXF_EPI_SWIGLU;
+  if (!gemm_i8_ok(M, N, K) || M == 0 || epilogue < 0 || epilogue > 3 || (sw && N % 2) || !plan) return HXF_EINVAL;
+  const GemmI8Plan p = gemm_i8_plan(M, sw ? N / 2 : N, (K + 63) / 64, epilogue);
+  const int32_t v[7] = {p.tm, p.nw, p.wv, p.once ? 1 : 0, p.splits, p.piece, p.thin ? 1 : 0};
+  std::copy(v, v + 7, plan);
+  return HXF_OK;
+}
+
 int hxf_op_gemm_i8(const void* A, const float* a_scale, const void* B, const float* b_scale, const void* B2,
                    const float* b2_scale, void* C, int32_t ldc, int32_t M, int32_t N, int32_t K, int32_t epilogue,
                    void* workspace, int64_t ws_bytes, void* stream) {
@@ -624,8 +633,6 @@ int hxf_op_gemm_i8(const void* A, const float* a_scale, const void* B, const flo
     return HXF_EINVAL;
   if (reinterpret_cast<uintptr_t>(C) & (epilogue == HXF_EPI_BF16 || sw ? 1 : 3)) return HXF_EINVAL;
   if (M == 0) return HXF_OK;
-  const int64_t need = gemm_i8_ws_bytes(M, N, K);
-  if (need > 0 && (!workspace || !aligned16(workspace) || ws_bytes < need)) return HXF_ENOMEM;
   GemmI8Args a{};
   a.A = (const int8_t*)A;
   a.B = (const int8_t*)B;
@@ -639,7 +646,8 @@ int hxf_op_gemm_i8(const void* A, const float* a_scale, const void* B, const flo
   a.N = sw ? N / 2 : N;
   a.ldc = ldc;
   a.kt = (K + 63) / 64;
-  return dev_rc(gemm_i8_launch(a, epilogue, (hipStream_t)stream));
+  const hipError_t e = gemm_i8_launch(a, epilogue, workspace && aligned16(workspace) ? ws_bytes : 0, (hipStream_t)stream);
+  return e == hipErrorOutOfMemory ? HXF_ENOMEM : dev_rc(e);
 }
 
 int hxf_op_argmax(const float* logits, int32_t* out, int32_t R, int32_t V, void* stream) {

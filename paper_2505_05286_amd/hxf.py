@@ -195,6 +195,7 @@ _SIGS = {
     "hxf_op_rmsnorm_i8": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
                                     C.c_int32, C.c_float, C.c_void_p]),
     "hxf_op_gemm_i8_workspace_bytes": (C.c_int64, [C.c_int32, C.c_int32, C.c_int32]),
+    "hxf_op_gemm_i8_plan": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32)]),
     "hxf_op_gemm_i8": (C.c_int, [C.c_void_p] * 7 + [C.c_int32] * 5 + [C.c_void_p, C.c_int64, C.c_void_p]),
     "hxf_op_argmax": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]),
     "hxf_op_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
@@ -616,6 +617,13 @@ def op_rmsnorm_i8(x, rows, x_rows, g, codes, scale, n_rows, d, eps, stream=0):
 
 def op_gemm_i8_workspace_bytes(M, N, K):
     return lib().hxf_op_gemm_i8_workspace_bytes(M, N, K)
+
+
+def op_gemm_i8_plan(M, N, K, epi):
+    """{row tiles, column tiles per wavefront, wavefronts, read once, pieces of K, K tiles per piece, K shared out} of op_gemm_i8."""
+    plan = (C.c_int32 * 7)()
+    _op(lib().hxf_op_gemm_i8_plan(M, N, K, epi, plan), "hxf_op_gemm_i8_plan")
+    return tuple(plan)
 
 
 def op_gemm_i8(A, a_scale, B, b_scale, B2, b2_scale, Cp, ldc, M, N, K, epi, ws=0, ws_bytes=0, stream=0):

@@ -80,13 +80,14 @@ def test_sizes_of_buffers():
         assert hxf.op_gemm_i8_workspace_bytes(*bad) == -1
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 6144, 4096), (64, 4096, 14336), (17, 512, 256)])
+@pytest.mark.parametrize("m,n,k", [(64, 4096, 14336), (256, 8192, 28672)])
 def test_a_short_workspace_is_refused(m, n, k):
+    """Products whose K is cut need their partials, four bytes an output and piece."""
     need = hxf.op_gemm_i8_workspace_bytes(m, n, k)
-    assert need >= 0
-    if need:
-        for bad in (dict(ws_bytes=need - 1), dict(ws=0), dict(ws=A + 8)):
-            _refused(hxf.ENOMEM, _gemm, M=m, N=n, K=k, ldc=n, **bad)
+    assert need > 0 and need % (4 * m * n) == 0
+    for bad in (dict(ws_bytes=0), dict(ws=0), dict(ws=A + 8), dict(ws_bytes=4 * m * n)):
+        for epi in (hxf.EPI_BF16, hxf.EPI_RESID, hxf.EPI_F32):
+            _refused(hxf.ENOMEM, _gemm, M=m, N=n, K=k, ldc=n, epi=epi, **bad)
 
 
 def test_empty_batches_are_done_without_a_launch():
