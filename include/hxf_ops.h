@@ -277,7 +277,7 @@ int hxf_op_rmsnorm_i8(const float* x, const int32_t* rows, int32_t x_rows, const
  *                   C[:, f] = bf16(silu(gate_f) * up_f), silu(z) = z / (1 + e^-z)
  *   HXF_EPI_F32:    C fp32 [M, ldc]            C = y
  * A and B (and B2): codes as above, 16-byte aligned.  B2 and b2_scale are unused but for SwiGLU.  ldc >= N (SwiGLU: F);
- * elements behind a row's columns are left as they are.  M < 2^22, 0 < N < 2^22, 0 < K < 2^17, M * N < 2^36.
+ * elements behind a row's columns are left as they are.  M < 2^22, 0 < N < 2^22, 0 < K < 2^17, M * N < 2^34.
  * workspace: hxf_op_gemm_i8_workspace_bytes(M, N, K) bytes (enough for every epilogue; may be 0), 16-byte
  * aligned, whose contents need not be kept between calls; calls that may overlap need one each.  No buffer may
  * overlap another. */

@@ -606,7 +606,7 @@ int hxf_op_rmsnorm_i8(const float* x, const int32_t* rows, int32_t x_rows, const
 namespace {
 
 bool gemm_i8_ok(int32_t M, int32_t N, int32_t K) {
-  return i8_matrix_ok(M, K) && N > 0 && i8_matrix_ok(N, K) && (int64_t)M * N < (int64_t(1) << 36);
+  return i8_matrix_ok(M, K) && N > 0 && i8_matrix_ok(N, K) && (int64_t)M * N < (int64_t(1) << 34);
 }
 
 }  // namespace

@@ -281,6 +281,93 @@ def test_gemm_swiglu_at_large_gates():
     p.check()
 
 
+def _tile_dev(x):
+    """Row-major int8 codes on the GPU as padded tiles."""
+    t = torch()
+    r, k = x.shape
+    p = t.zeros(U.up(r, 16), U.up(k, 64), dtype=t.int8, device=DEV)
+    p[:r, :k] = x
+    return p.view(-1, 16, p.shape[1] // 64, 4, 16).permute(0, 2, 3, 1, 4).contiguous().view(-1)
+
+
+@pytest.mark.parametrize("M,N,K", U.PLANS)
+def test_gemm_in_every_plan(M, N, K):
+    """Each instance of the kernels, all epilogues; the whole numbers by products in 64 bits (exact below 2^53)."""
+    t = torch()
+    g = t.Generator(device=DEV)
+    g.manual_seed(M * 7 + N)
+    rand = lambda n: t.randint(-127, 128, (n, K), generator=g, device=DEV, dtype=t.int8)   # noqa: E731
+    a, b, b2 = rand(M), rand(N), rand(N)
+    sa = t.rand(M, generator=g, device=DEV) + 0.5
+    sb = (t.rand(N, generator=g, device=DEV) + 0.5) / (5000 * K ** 0.5)
+    dev = [_tile_dev(v) for v in (a, b, b2)]
+    y, up = (((a.double() @ v.double().T) * sa.double()[:, None]) * sb.double() for v in (b, b2))
+    rel = 3.001 * U32
+    for epi in EPI:
+        cols = 2 * N if epi == "swiglu" else N
+        print(epi, M, cols, K, hxf.op_gemm_i8_plan(M, cols, K, EPI[epi]), flush=True)
+        wide = epi in ("resid", "f32")
+        c = t.randn(M, N + 1, generator=g, device=DEV).to(t.float32 if wide else t.bfloat16)
+        c0 = c.double()
+        n = hxf.op_gemm_i8_workspace_bytes(M, cols, K)
+        ws = t.full((n + GUARD,), 0x5A, dtype=t.uint8, device=DEV)
+        hxf.op_gemm_i8(dev[0].data_ptr(), sa.data_ptr(), dev[1].data_ptr(), sb.data_ptr(), dev[2].data_ptr(),
+                       sb.data_ptr(), c.data_ptr(), N + 1, M, cols, K, EPI[epi], ws.data_ptr(), n)
+        t.cuda.synchronize()
+        assert bool((ws[n:] == 0x5A).all()) and t.equal(c[:, N].double(), c0[:, N])
+        got, old = c[:, :N].double(), c0[:, :N]
+        if epi == "swiglu":
+            want = y * t.sigmoid(y) * up
+            tol = (UB16 + (6 * y.abs() + 16) * 2 * U32) * want.abs() + 1e-30
+        elif epi == "resid":
+            want = y + old
+            tol = rel * y.abs() + 1.001 * U32 * (want.abs() + rel * y.abs())
+        else:
+            want, tol = y, (rel + (0 if wide else UB16 + rel)) * y.abs()
+        bad = ~((got - want).abs() <= tol)
+        assert not bool(bad.any()), (epi, int(bad.sum()), bad.nonzero()[:4].tolist())
+
+
+def test_gemm_outputs_and_weights_beyond_32_bits_of_offset():
+    """4.6 GB of outputs, then 4.5 GB of codes; rows and columns at the ends and around 2^31 and 2^32 bytes."""
+    t = torch()
+    g = t.Generator(device=DEV)
+    g.manual_seed(3)
+    for M, N, K, epi in ((70001, 32770, 64, "bf16"), (3, 262147, 17000, "f32")):
+        a = t.randint(-127, 128, (M, K), generator=g, device=DEV, dtype=t.int8)
+        b = t.randint(-127, 128, (N, K), generator=g, device=DEV, dtype=t.int8)
+        ta, tb = _tile_dev(a), _tile_dev(b)
+        sa, sb = t.ones(M, device=DEV), t.ones(N, device=DEV)
+        c = t.zeros(M, N, device=DEV, dtype=t.bfloat16 if epi == "bf16" else t.float32)
+        ws = t.empty(hxf.op_gemm_i8_workspace_bytes(M, N, K) + 16, dtype=t.uint8, device=DEV)
+        print(M, N, K, hxf.op_gemm_i8_plan(M, N, K, EPI[epi]), flush=True)
+        hxf.op_gemm_i8(ta.data_ptr(), sa.data_ptr(), tb.data_ptr(), sb.data_ptr(), 0, 0, c.data_ptr(), N, M, N, K,
+                       EPI[epi], ws.data_ptr(), ws.numel())
+        t.cuda.synchronize()
+        rows = t.tensor(sorted({0, M // 2, M - 1, min(M - 1, 2 ** 30 // N + 1), min(M - 1, 2 ** 31 // N + 1)}), device=DEV)
+        for lo in (0, N // 2, N - 40, min(N - 40, 2 ** 31 // 17024), min(N - 40, 2 ** 32 // 17024)):
+            want = a[rows].double() @ b[lo:lo + 40].double().T
+            off = (c[rows][:, lo:lo + 40].double() - want).abs()
+            assert bool((off <= (UB16 if epi == "bf16" else U32) * want.abs()).all())
+        del a, b, ta, tb, c
+
+
+def test_quant_beyond_32_bits_of_offset():
+    t = torch()
+    R, K = 140001, 16392
+    x = t.randn(R, 8, device=DEV).repeat(1, K // 8).to(t.bfloat16)
+    codes = t.empty(hxf.i8_codes_bytes(R, K), dtype=t.int8, device=DEV)
+    scale = t.empty(R, device=DEV)
+    hxf.op_quant_i8(x.data_ptr(), K, R, K, codes.data_ptr(), scale.data_ptr())
+    t.cuda.synchronize()
+    kt = U.up(K, 64) // 64
+    for r in (0, 65537, 2 ** 31 // (2 * K) + 1, 2 ** 32 // (2 * K) + 1, 2 ** 31 // (kt * 64) + 3, R - 1):
+        want, unit = U.codes_of(x[r:r + 1].float().cpu().numpy())
+        tile = codes[(r // 16) * kt * 1024:(r // 16 + 1) * kt * 1024].view(kt * 4, 16, 16)[:, r % 16].reshape(-1)
+        assert np.array_equal(tile.cpu().numpy()[:K], want[0]) and not bool(tile[K:].any())
+        assert float(scale[r]) == float(unit[0])
+
+
 def test_calls_repeat_to_the_bit():
     """Sums of whole numbers do not depend on an order."""
     t = torch()

@@ -112,3 +112,27 @@ def test_the_model_by_hand():
     p = U.product(np.array([[1, -2]], np.int8), [0.5], np.array([[3, 4], [127, -127]], np.int8), [2.0, 1.0])
     assert p.tolist() == [[-5.0, 190.5]]
     assert U.silu(np.array([0.0, 800.0, -800.0])).tolist() == [0.0, 800.0, -0.0]
+
+
+def test_plans_report_what_the_shapes_of_the_gpu_test_take():
+    """Every kernel instance that the table stands for is taken, whole and cut K alike, and pieces cover K."""
+    seen = set()
+    for m, n, k in U.PLANS:
+        for epi in range(4):
+            tm, nw, wv, once, splits, piece, thin = hxf.op_gemm_i8_plan(m, 2 * n if epi == hxf.EPI_SWIGLU else n, k, epi)
+            kt = -(-k // 64)
+            assert piece % 2 == 0 and splits == (1 if thin else -(-kt // piece)) and (thin or (splits - 1) * piece < kt)
+            seen.add((tm, nw, wv, once, thin, splits > 1))
+    assert len(seen) >= 70
+    assert {t[4] for t in seen} == {0, 1} and {t[2] for t in seen if not t[4]} == {4, 8}
+    for bad in ((0, 64, 64, 0), (4, 0, 64, 0), (4, 63, 64, hxf.EPI_SWIGLU), (4, 64, 0, 0), (4, 64, 64, 4)):
+        with pytest.raises(hxf.HxfError):
+            hxf.op_gemm_i8_plan(*bad)
+
+
+@pytest.mark.parametrize("m,n,k", U.PLANS)
+def test_workspace_covers_the_plan(m, n, k):
+    for epi in range(4):
+        cols = 2 * n if epi == hxf.EPI_SWIGLU else n
+        splits = hxf.op_gemm_i8_plan(m, cols, k, epi)[4]
+        assert hxf.op_gemm_i8_workspace_bytes(m, cols, k) >= (splits * m * cols * 4 if splits > 1 else 0)
