@@ -78,9 +78,14 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
   constexpr bool SW = EPI == EPI_SWIGLU;
   constexpr int HALF = SW ? NW / 2 : NW;                         // column tiles of the output per wavefront
   constexpr int BM = 16 * TM, BN = 16 * HALF * WV, NS = 4;
+  // Whether the loads of a step are spread over its matrix instructions.  A wavefront that is alone on its SIMD hides an
+  // instruction or two behind each matrix instruction but not a row of them; spread, loads come later, which costs
+  // tiles with shorter steps more than it gains (us, spread and not: 2080 x 57344 x 8192 SwiGLU in 192-row tiles
+  // 724 / 768, 2080 x 10240 x 8192 in 176 137 / 150; 2080 x 4096 x 14336 in 160 122 / 109, in 144 108 / 104).
+  constexpr bool SPREAD = WV == 4 && NW == 4 && TM >= 11;
   constexpr int A_BLK = TM * 2, A_PW = (A_BLK + WV - 1) / WV, STAGE = A_BLK * 1024;   // 1 KB blocks per stage, per wavefront
   // outstanding loads allowed when stage s + 1 must have landed: the younger stages' DMAs and the weight loads
-  // issued since its own DMAs (the first step's of the same pass may have been scheduled before those)
+  // issued since its own DMAs (without the first step's of the same pass, which may stand before the last of those)
   constexpr int WAIT = (NS - 3) * A_PW + 2 * NW * (NS - 2) - NW;
   static_assert((2 * NS) % R == 0 && WAIT < 64 && NW * R + (NS - 2) * A_PW < 64, "pipeline");
   static_assert(!SW || NW % 2 == 0, "a wavefront holds as many up columns as gate columns");
@@ -109,11 +114,16 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
     a_dst[u] = b * 1024;
     a_off[u] = (min(rt, last_tile) * a.kt + kk) * 1024 + lane * 16;
   }
+  // one block of stage s; `check`: past the last stage nothing is read (by or-ing, without a branch)
+  auto issue_a1 = [&](auto check, int u, int s, uint8_t* base) __attribute__((always_inline)) {
+    if constexpr (decltype(check)::value)
+      buf_dma16(ra, a_off[u] | (s >= nst ? kOutOfRange : 0), (kb + 2 * min(s, nst - 1)) * 1024, base + a_dst[u]);
+    else
+      buf_dma16(ra, a_off[u], (kb + 2 * s) * 1024, base + a_dst[u]);
+  };
   auto issue_a = [&](int s, uint8_t* base) __attribute__((always_inline)) {
-    const int past = s >= nst ? kOutOfRange : 0;   // past the last stage nothing is read; by or-ing, without a branch
 #pragma unroll
-    for (int u = 0; u < A_PW; ++u)
-      buf_dma16(ra, a_off[u] | past, (kb + 2 * min(s, nst - 1)) * 1024, base + a_dst[u]);
+    for (int u = 0; u < A_PW; ++u) issue_a1(std::true_type{}, u, s, base);
   };
   const int c0 = tn * BN + w * 16 * HALF;                          // the wavefront's first output column
   const int b_tiles = (a.N + 15) / 16, bt = min(c0 / 16, b_tiles - 1);
@@ -124,12 +134,18 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
 #pragma unroll
   for (int j = 0; j < HALF; ++j) b_off[j] = lane * 16 + j * a.kt * 1024;
   uint4 fb[R][NW];
-  auto load_b = [&](auto rc, int k) __attribute__((always_inline)) {
+  // `check`: past the last step zeros
+  auto load_b1 = [&](auto check, auto rc, int j, int k) __attribute__((always_inline)) {
     constexpr int r = decltype(rc)::value % R;
-    const int kk = kb + min(k, kt - 1), past = k < kt ? 0 : kOutOfRange;
+    if constexpr (decltype(check)::value)
+      fb[r][j] = buf_load16<CACHE>(j < HALF ? rb0 : rb1, b_off[j % HALF] | (k < kt ? 0 : kOutOfRange),
+                                   (kb + min(k, kt - 1)) * 1024);
+    else
+      fb[r][j] = buf_load16<CACHE>(j < HALF ? rb0 : rb1, b_off[j % HALF], (kb + k) * 1024);
+  };
+  auto load_b = [&](auto rc, int k) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < NW; ++j)   // past the last step: zeros
-      fb[r][j] = buf_load16<CACHE>(j < HALF ? rb0 : rb1, b_off[j % HALF] | past, kk * 1024);
+    for (int j = 0; j < NW; ++j) load_b1(std::true_type{}, rc, j, k);
   };
   i32x4 acc[TM][NW];
 #pragma unroll
@@ -140,20 +156,40 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
   auto read_a = [&](const uint8_t* base, int i, int h) __attribute__((always_inline)) {
     return *reinterpret_cast<const uint4*>(base + i * 2048 + h * 1024 + lane * 16);
   };
-  // one step with the weights of ring slot r; reads the next step's fragments as it goes
-  auto step = [&](auto rc, const uint8_t* next, int h) __attribute__((always_inline)) {
-    constexpr int r = decltype(rc)::value % R;
+  // One step with the weights of ring slot r; reads the next step's fragments as it goes.  SPREAD: one at a time between
+  // its matrix instructions, and with them n loads or DMAs, mem(0) .. mem(n - 1).
+  auto step = [&](auto rc, const uint8_t* next, int h, auto nc, auto&& mem) __attribute__((always_inline)) {
+    constexpr int r = decltype(rc)::value % R, n = decltype(nc)::value, PLACES = TM * (NW / 2);
+    if constexpr (SPREAD) {
+      static_for<TM * NW>([&](auto tc) {
+        constexpr int i = decltype(tc)::value / NW, j = decltype(tc)::value % NW;
+        acc[i][j] = mfma16x16x64(fb[r][j], fa[i], acc[i][j]);
+        if constexpr (j == 0 && i > 0) fa[i - 1] = read_a(next, i - 1, h);
+        if constexpr (j % 2 == 1) {
+          constexpr int q = i * (NW / 2) + j / 2;
+          static_for<(q + 1) * n / PLACES - q * n / PLACES>([&](auto oc) {
+            mem(std::integral_constant<int, q * n / PLACES + decltype(oc)::value>{});
+          });
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      fa[TM - 1] = read_a(next, TM - 1, h);
+      __builtin_amdgcn_sched_barrier(0);
+    } else {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
+      for (int i = 0; i < TM; ++i) {
 #pragma unroll
-      for (int j = 0; j < NW; ++j) acc[i][j] = mfma16x16x64(fb[r][j], fa[i], acc[i][j]);
-      fa[i] = read_a(next, i, h);
+        for (int j = 0; j < NW; ++j) acc[i][j] = mfma16x16x64(fb[r][j], fa[i], acc[i][j]);
+        fa[i] = read_a(next, i, h);
+      }
+      static_for<TM>([&](auto) {
+        __builtin_amdgcn_sched_group_barrier(0x008, NW, 0);   // MFMAs
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);    // one LDS read
+      });
     }
-    static_for<TM>([&](auto) {
-      __builtin_amdgcn_sched_group_barrier(0x008, NW, 0);   // MFMAs
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);    // one LDS read
-    });
   };
+  auto nothing = [](auto) {};
+  constexpr std::integral_constant<int, 0> none{};
   static_for<NS - 1>([&](auto ic) {
     issue_a(decltype(ic)::value, slot(ic));
     __builtin_amdgcn_sched_barrier(0);   // the waits below count in this order
@@ -164,30 +200,53 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
   __builtin_amdgcn_s_barrier();
 #pragma unroll
   for (int i = 0; i < TM; ++i) fa[i] = read_a(L0, i, 0);
-  step(std::integral_constant<int, 0>{}, L0, 1);
-  load_b(std::integral_constant<int, 0>{}, R);
+  step(none, L0, 1, none, nothing);
+  if constexpr (!SPREAD) load_b(none, R);
   __builtin_amdgcn_sched_barrier(0);
-  // pass s: the second step of stage s (it reads stage s + 1's first fragments) and the first of stage s + 1.
-  // Every LDS read follows, without a branch, the wait for its stage's DMA, and the loop has one exit: otherwise
-  // the compiler adds waits for everything in flight.  Whole trips of 2 NS steps; a last trip that has at least three
-  // steps of its own runs on over zeros, which costs less than so many single steps.
+  // Pass s: the second step of stage s (it reads stage s + 1's first fragments) and the first of stage s + 1; with SPREAD
+  // each loads the weights of the ring slot that the step before it used, otherwise its own.
+  // Every LDS read follows, without a branch, the wait for its stage's DMA, and a loop has one exit: otherwise
+  // the compiler adds waits for everything in flight.  Whole trips of 2 NS steps (with SPREAD first those that load nothing
+  // past the end); a last trip that has at least three steps of its own runs on over zeros, which costs less than so
+  // many single steps.
   const int s_end = (kt - 1 + 2 * NS - 3) / (2 * NS) * NS;
   int s0 = 0;
-  for (; s0 < s_end; s0 += NS) {
+  auto trip = [&](auto check) __attribute__((always_inline)) {
     static_for<NS>([&](auto ic) {
       constexpr int J = decltype(ic)::value;
+      constexpr std::integral_constant<int, 2 * J + 1> first{};
+      constexpr std::integral_constant<int, 2 * J + 2> second{};
       wait_vmcnt<WAIT>();
       __builtin_amdgcn_s_barrier();
-      issue_a(s0 + J + NS - 1, slot(std::integral_constant<int, J + NS - 1>{}));
+      uint8_t* fill = slot(std::integral_constant<int, J + NS - 1>{});
       const uint8_t* next = slot(std::integral_constant<int, J + 1>{});
-      step(std::integral_constant<int, 2 * J + 1>{}, next, 0);
-      load_b(std::integral_constant<int, 2 * J + 1>{}, (s0 + J) * 2 + 1 + R);
-      __builtin_amdgcn_sched_barrier(0);
-      step(std::integral_constant<int, 2 * J + 2>{}, next, 1);
-      load_b(std::integral_constant<int, 2 * J + 2>{}, (s0 + J) * 2 + 2 + R);
-      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (SPREAD) {
+        __builtin_amdgcn_sched_barrier(0);
+        step(first, next, 0, std::integral_constant<int, A_PW + NW>{}, [&](auto oc) {
+          constexpr int o = decltype(oc)::value;
+          if constexpr (o < A_PW) issue_a1(check, o, s0 + J + NS - 1, fill);
+          else load_b1(check, std::integral_constant<int, 2 * J>{}, o - A_PW, (s0 + J) * 2 + R);
+        });
+        step(second, next, 1, std::integral_constant<int, NW>{}, [&](auto oc) {
+          load_b1(check, first, decltype(oc)::value, (s0 + J) * 2 + 1 + R);
+        });
+      } else {
+        issue_a(s0 + J + NS - 1, fill);
+        step(first, next, 0, none, nothing);
+        load_b(first, (s0 + J) * 2 + 1 + R);
+        __builtin_amdgcn_sched_barrier(0);
+        step(second, next, 1, none, nothing);
+        load_b(second, (s0 + J) * 2 + 2 + R);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     });
+  };
+  if constexpr (SPREAD) {
+    const int inside = max(0, min(kt - R - 2 * NS + 1, 2 * nst - 4 * NS + 4) + 2 * NS - 1) / (2 * NS) * NS;
+    for (; s0 < inside; s0 += NS) trip(std::false_type{});
   }
+  for (; s0 < s_end; s0 += NS) trip(std::true_type{});
+  if constexpr (SPREAD) load_b(none, 2 * s0 + R);
   // one or two remaining steps singly, the ring shifted by copies
   auto dyn_slot = [&](int i) -> uint8_t* {
     i %= NS;
@@ -199,7 +258,7 @@ __global__ __launch_bounds__(64 * WV, OCC) void gemm_i8_kernel(GemmI8Args a) {
       __builtin_amdgcn_s_barrier();
       issue_a((k >> 1) + NS - 1, dyn_slot((k >> 1) + NS - 1));
     }
-    step(std::integral_constant<int, 1>{}, dyn_slot((k >> 1) + (k & 1)), (k & 1) ^ 1);
+    step(std::integral_constant<int, 1>{}, dyn_slot((k >> 1) + (k & 1)), (k & 1) ^ 1, none, nothing);
 #pragma unroll
     for (int j = 0; j < NW; ++j) {
 #pragma unroll
