@@ -74,21 +74,22 @@ namespace {
 // activations); a workgroup then stores its outputs (store us per KB; SwiGLU as if of `gated` bytes a value).  A CU runs
 // `resident` workgroups at once, which share its time but wait each by itself (start).  The weights come at tb_s at best.
 //
-// Fitted to 140,000 launches of 3,400 shapes (1 to 3,000 rows, half of them projections of d 4096-8192), weights not
-// in the caches, in graphs: the choice is 2.4% slower than the best plan on average, 27% at the worst hundredth.
+// Fitted to 190,000 launches of 4,900 shapes (1 to 3,000 rows, half of them projections of d 4096-8192), weights not
+// in the caches, in graphs: the choice is 2.2% slower than the best plan on average, 28% at the worst hundredth.
 struct WideCost {
   float t0, start, store, i0, i1, fetch[3], a_share, tb_s, gated;
   int resident;
 };
-constexpr WideCost kNarrowOnce{2.22f, 0.724f, 0.034f, 0.0347f, 0.0734f, {0.373f, 0.33f, 0.3f}, 0.782f, 5.95f, 6.53f, 1};   // 32 columns a wavefront, one row of tiles
-constexpr WideCost kNarrowLow{3.15f, 0.f, 0.0436f, 0.11f, 0.0208f, {0.35f, 0.282f, 0.224f}, 0.599f, 6.f, 5.43f, 3};   // 32 columns, up to 4 row tiles a workgroup
-constexpr WideCost kNarrow{3.39f, 0.f, 0.0422f, 0.0287f, 0.0515f, {0.209f, 0.203f, 0.173f}, 1.57f, 4.22f, 6.3f, 2};   // 32 columns, more
-constexpr WideCost kCols64Once{2.97f, 0.f, 0.0286f, 0.f, 0.047f, {0.333f, 0.33f, 0.3f}, 0.838f, 6.11f, 9.58f, 1};   // 64 columns, one row of tiles
-constexpr WideCost kCols64Low{3.22f, 0.f, 0.0389f, 0.053f, 0.044f, {0.35f, 0.151f, 0.13f}, 3.89f, 4.12f, 4.95f, 2};   // 64 columns, up to 7 row tiles: two workgroups a CU
-constexpr WideCost kCols64{0.f, 3.87f, 0.031f, 0.0211f, 0.0435f, {0.35f, 0.304f, 0.277f}, 0.747f, 6.f, 6.02f, 1};   // 64 columns, more
-constexpr WideCost kEight{0.f, 3.08f, 0.0239f, 0.267f, 0.0276f, {0.266f, 0.254f, 0.23f}, 1.07f, 3.71f, 5.94f, 1};   // eight wavefronts of 64 columns
+constexpr WideCost kNarrowOnce{2.17f, 0.753f, 0.0348f, 0.192f, 0.033f, {0.37f, 0.33f, 0.3f}, 0.792f, 5.95f, 6.74f, 1};   // 32 columns a wavefront, one row of tiles
+constexpr WideCost kNarrowLow{3.22f, 0.f, 0.0426f, 0.112f, 0.0194f, {0.35f, 0.278f, 0.226f}, 0.64f, 6.f, 5.37f, 3};   // 32 columns, up to 4 row tiles a workgroup
+constexpr WideCost kNarrow{3.4f, 0.f, 0.0425f, 0.0314f, 0.0505f, {0.209f, 0.204f, 0.173f}, 1.55f, 4.24f, 6.25f, 2};   // 32 columns, more
+constexpr WideCost kCols64Once{2.94f, 0.f, 0.0299f, 0.f, 0.0449f, {0.335f, 0.33f, 0.3f}, 0.781f, 6.08f, 9.39f, 1};   // 64 columns, one row of tiles
+constexpr WideCost kCols64Low{3.27f, 0.f, 0.0392f, 0.12f, 0.0335f, {0.35f, 0.135f, 0.115f}, 4.7f, 4.1f, 4.94f, 2};   // 64 columns, up to 7 row tiles: two workgroups a CU
+constexpr WideCost kCols64{0.f, 4.11f, 0.0292f, 0.0925f, 0.036f, {0.35f, 0.133f, 0.115f}, 2.19f, 6.f, 5.68f, 1};   // 64 columns, 8 to 10
+constexpr WideCost kCols64High{2.27f, 2.77f, 0.0301f, 0.f, 0.0413f, {0.35f, 0.33f, 0.3f}, 0.5f, 6.f, 4.42f, 1};   // 64 columns, more
+constexpr WideCost kEight{0.f, 3.16f, 0.0241f, 0.263f, 0.0276f, {0.275f, 0.255f, 0.237f}, 0.795f, 3.68f, 5.79f, 1};   // eight wavefronts of 64 columns
 // Pieces of K are joined by a launch of its own; a plan with one is only taken where it saves a twentieth
-constexpr float kJoin = 2.77f, kJoinGated = 1.7f, kJoinMb = 0.302f, kSplitBias = 1.06f;
+constexpr float kJoin = 2.71f, kJoinGated = 1.66f, kJoinMb = 0.308f, kSplitBias = 1.06f;
 
 // The kernel that joins K inside the workgroup: the wait for a first step, a step, a CU's 100 KB of codes, the weights,
 // a workgroup's rest
@@ -96,8 +97,8 @@ struct ThinCost {
   int tm, nw, wv;
   float t0, first, step, kb, tb_s, rest;
 };
-constexpr ThinCost kThin[] = {{1, 1, 4, 2.7f, 0.785f, 0.139f, 2.31f, 5.96f, 0.926f}, {1, 2, 16, 1.78f, 4.47f, 0.0909f, 2.35f, 5.81f, 2.89f}, {2, 1, 16, 2.87f, 3.14f, 0.f, 2.53f, 5.44f, 1.95f},
-                              {2, 2, 8, 1.86f, 0.39f, 0.627f, 2.16f, 5.57f, 2.63f}, {4, 1, 8, 1.82f, 3.37f, 0.176f, 2.36f, 7.08f, 2.62f}, {4, 2, 8, 0.f, 6.04f, 0.247f, 2.57f, 5.67f, 4.08f}};
+constexpr ThinCost kThin[] = {{1, 1, 4, 2.66f, 0.615f, 0.0423f, 2.32f, 5.96f, 0.94f}, {1, 2, 16, 1.74f, 4.44f, 0.129f, 2.38f, 5.86f, 2.9f}, {2, 1, 16, 2.8f, 3.19f, 0.f, 2.54f, 5.44f, 2.01f},
+                              {2, 2, 8, 1.74f, 2.58f, 0.44f, 2.35f, 5.58f, 2.39f}, {4, 1, 8, 1.95f, 3.18f, 0.203f, 2.36f, 7.28f, 2.52f}, {4, 2, 8, 0.f, 5.55f, 0.56f, 2.58f, 5.68f, 3.97f}};
 
 struct Choice {
   int M, N, kt, row_tiles, bytes;   // bytes: of an output value, its old one read included
@@ -169,7 +170,7 @@ GemmI8Plan gemm_i8_plan(int M, int N, int kt, int epi) {
   for (int tm = 3; tm <= 12; ++tm)
     if (rt > tm ? fewer(tm, 3) : rt > 8 && rt == tm) c.wide(tm <= 4 ? kNarrowLow : kNarrow, tm, 2, 4, false);
   for (int tm = 4; tm <= 16; ++tm) {
-    if (rt > tm && fewer(tm, 4)) c.wide(tm <= 7 ? kCols64Low : kCols64, tm, 4, 4, false);
+    if (rt > tm && fewer(tm, 4)) c.wide(tm <= 7 ? kCols64Low : tm <= 10 ? kCols64 : kCols64High, tm, 4, 4, false);
     if (rt <= tm && rt > 8 && tm % 2 == 0 && rt + 2 > tm) c.wide(kCols64Once, tm, 4, 4, true);
   }
   if (rt > 8)

@@ -57,17 +57,21 @@ def silu(z):
 # (rows, output columns, K) that take the instances of the product's kernels: tile heights, widths, wavefronts, weights
 # read once or more often, K cut or whole, K shared out inside a workgroup
 PLANS = [
-    (1, 1, 248), (1, 4097, 40), (1, 4103, 13218), (1, 4098, 1895), (1, 9067, 19122), (17, 1, 1536),
-    (17, 1, 64), (17, 1, 6144), (17, 1, 640), (18, 10888, 3358), (65, 1, 28), (49, 1, 5012), (33, 1, 460),
-    (1346, 1046, 36), (1539, 1, 8094), (33, 4099, 54), (33, 1, 5964), (39, 4112, 763), (227, 13202, 289),
-    (225, 2207, 16830), (33, 8215, 5778), (130, 16234, 1940), (2305, 1, 7048), (194, 21758, 6000),
-    (195, 4206, 10829), (791, 12340, 839), (200, 8306, 14610), (173, 16343, 3870), (2689, 1, 8084),
-    (2087, 2305, 10), (324, 2730, 16238), (65, 5429, 11580), (2265, 4624, 365), (262, 8294, 14608),
-    (196, 16340, 10420), (2245, 132, 12217), (2507, 2322, 501), (195, 4533, 16942), (2977, 4231, 14),
-    (292, 8194, 14682), (2310, 1544, 178), (2046, 268, 15030), (65, 16404, 5), (72, 5418, 12630),
-    (2635, 2604, 399), (244, 4151, 16985), (97, 8249, 9360), (2906, 5258, 24), (228, 10971, 17061),
-    (2307, 1667, 264), (129, 5489, 6624), (257, 30016, 5681), (264, 4367, 17053), (2890, 5638, 56),
-    (259, 16440, 16499), (2003, 2314, 49), (145, 4123, 13978), (2250, 4125, 1457), (291, 8328, 14291),
-    (129, 8307, 12002), (873, 6491, 126), (162, 4137, 14093), (868, 12864, 984), (337, 8362, 16023),
-    (2702, 2078, 204), (181, 4367, 15882), (2702, 4174, 2256), (178, 8233, 14213), (610, 21699, 1615),
-    (2594, 5180, 5702), (194, 8325, 16105), (1154, 12872, 3766), (727, 21562, 53), (228, 11360, 17800)]
+    (1, 1, 248), (1, 4097, 40), (1, 4101, 11172), (1, 4098, 1895), (1, 16396, 7593), (17, 1, 1600),
+    (17, 1, 64), (17, 1, 6144), (17, 1, 448), (17, 10881, 3436), (65, 1, 28), (49, 1, 4948), (33, 1, 460),
+    (1346, 1032, 50), (1539, 1, 8094), (33, 4101, 52), (33, 1, 5900), (33, 4108, 813), (436, 8259, 865),
+    (65, 5380, 7281), (33, 8215, 5778), (130, 16115, 2067), (2305, 1, 7048), (195, 21603, 5712),
+    (194, 4106, 12028), (792, 12385, 719), (197, 8302, 13867), (163, 16378, 4101), (2689, 1, 8084),
+    (2087, 2305, 10), (329, 2714, 16539), (65, 5440, 10993), (2311, 4740, 283), (261, 8289, 14620),
+    (199, 16313, 8954), (2245, 132, 12217), (777, 7711, 438), (197, 5497, 17244), (2977, 4231, 14),
+    (294, 8299, 16539), (2309, 1537, 192), (2018, 257, 16597), (68, 16530, 358), (71, 5438, 11401),
+    (2835, 2352, 327), (248, 4105, 15147), (97, 8245, 8788), (2896, 5263, 29), (354, 8323, 17151),
+    (2201, 1801, 208), (135, 3209, 16114), (257, 30677, 4016), (257, 4367, 15698), (2902, 5635, 35),
+    (259, 16440, 16499), (2001, 2309, 8), (153, 4097, 13112), (725, 12989, 1596), (291, 4391, 18744),
+    (132, 8330, 11634), (866, 6450, 32), (162, 4396, 14454), (483, 21592, 627), (343, 8236, 14639),
+    (2429, 2309, 204), (177, 5385, 12776), (566, 21691, 543), (354, 9007, 18407), (161, 9005, 14284),
+    (587, 21578, 825), (386, 9332, 17758), (644, 21612, 620), (193, 8798, 15479), (678, 21683, 1251),
+    (722, 21739, 799), (227, 10882, 16461),
+    (1, 32804, 60), (17, 33119, 17), (33, 33616, 64), (67, 33345, 33), (97, 33354, 20), (148, 83564, 50),
+    (165, 90599, 64), (436, 4379, 31400), (201, 89937, 48), (459, 4381, 29230), (482, 4401, 37888),
+    (242, 83836, 63)]

@@ -144,6 +144,22 @@ def test_norm_without_rows_takes_the_first_of_more():
     assert np.array_equal(out.get()[0], U.tile(U.codes_of(x[:4])[0]))
 
 
+def test_norm_rows_that_are_not_finite_or_beyond_fp32():
+    """Infinities, products with the gain that pass fp32, and squares that do (the scale is then 0)."""
+    x = np.ones((5, 192), np.float32)
+    x[0, 7], x[1, 3], x[2, 100], x[3, 5] = np.inf, -np.inf, 3e38, 1e30
+    gb, g = _bf16(np.where(np.arange(192) == 100, 4.0, 1.0))
+    out = Codes(5, 192)
+    xd, gd = _dev(x), _dev(gb.view(np.int16))
+    hxf.op_rmsnorm_i8(xd.data_ptr(), 0, 5, gd.data_ptr(), *out.ptrs(), 5, 192, 1e-5)
+    codes, scale = out.get()
+    y, _ = U.norm_rows(x, None, g, 1e-5)
+    want, _ = U.codes_of(y)
+    assert np.array_equal(codes, U.tile(want))
+    assert np.isnan(scale[:3]).all() and scale[3] == 0 and scale[4] > 0
+    assert want[3, 5] == 127 and not want[:3].any()
+
+
 EPI = {"bf16": hxf.EPI_BF16, "resid": hxf.EPI_RESID, "swiglu": hxf.EPI_SWIGLU, "f32": hxf.EPI_F32}
 
 
@@ -467,6 +483,25 @@ def test_a_captured_block_replays_on_new_inputs():
         t.cuda.synchronize()
         for layer, want in zip(layers, wants):
             assert t.equal(layer.x, want)
+
+
+def test_a_block_on_a_stream_of_its_own():
+    """The calls go to the stream they are given: a block on a side stream gives what one on the default stream does."""
+    t = torch()
+    rng = np.random.default_rng(12)
+    layer = Layer(rng, 50, 512, 1376)
+    x = _dev(rng.standard_normal((50, 512)).astype(np.float32))
+    layer.x.copy_(x)
+    layer.run()
+    want = layer.x.clone()
+    side = t.cuda.Stream()
+    side.wait_stream(t.cuda.current_stream())
+    with t.cuda.stream(side):
+        for _ in range(3):
+            layer.x.copy_(x)
+            layer.run()
+    t.cuda.current_stream().wait_stream(side)
+    assert t.equal(layer.x, want)
 
 
 def test_two_streams_at_once():

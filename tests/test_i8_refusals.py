@@ -123,7 +123,7 @@ def test_plans_report_what_the_shapes_of_the_gpu_test_take():
             kt = -(-k // 64)
             assert piece % 2 == 0 and splits == (1 if thin else -(-kt // piece)) and (thin or (splits - 1) * piece < kt)
             seen.add((tm, nw, wv, once, thin, splits > 1))
-    assert len(seen) >= 70
+    assert len(seen) >= 80
     assert {t[4] for t in seen} == {0, 1} and {t[2] for t in seen if not t[4]} == {4, 8}
     for bad in ((0, 64, 64, 0), (4, 0, 64, 0), (4, 63, 64, hxf.EPI_SWIGLU), (4, 64, 0, 0), (4, 64, 64, 4)):
         with pytest.raises(hxf.HxfError):
