@@ -1,5 +1,11 @@
-// The product of 8-bit codes for one or two row tiles (a decode step of a few sequences) in one launch: the wavefronts
+// The product of 8-bit codes for one to four row tiles (a decode step of a few sequences) in one launch: the wavefronts
 // of a workgroup share out K and join their sums in LDS.
+//
+// The weights' bytes are the bound, and below some tens of MB the latency of the first loads and of a second launch.
+// With 16 or 32 columns a workgroup an output of a few thousand fills the chip without cutting K across workgroups,
+// whose partials take a launch of their own to join (a call, us, this kernel and the other with cut K: 1 x 6144 x 4096
+// 8.0 / 10.5, 64 rows 10.3 / 13.7; 1 x 4096 x 14336 12.9 / 15.7; 1 x 8192 x 28672 37.3 / 39.4, 6.3 TB/s).  But every
+// workgroup reads all activations itself: from 32 rows of long K on the other kernel is ahead (32 x 8192 x 28672 41.4).
 #include "gemm_i8.hpp"
 
 namespace hxf {
