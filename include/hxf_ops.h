@@ -250,7 +250,7 @@ int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_
  * (r, k) is at
  *   ((r/16) * ceil(K/64) + k/64) * 1024 + ((k%64)/16) * 256 + (r%16) * 16 + k%16,
  * the operand order of the 16x16x64 i8 MFMA.  hxf_i8_codes_bytes(R, K) bytes (-1 for sizes the operators refuse),
- * 16-byte aligned.  0 < K < 2^17, so that no sum of products passes 32 bits; 0 <= R < 2^22. */
+ * 16-byte aligned.  0 < K < 2^17, so that no sum of products passes 32 bits; 0 <= R <= 2^22 - 16. */
 int64_t hxf_i8_codes_bytes(int32_t R, int32_t K);
 
 /* Codes and scales of bf16 rows (weights once when they are loaded, activations in each step): x bf16, R rows of
@@ -265,7 +265,7 @@ int hxf_op_quant_i8(const void* x, int64_t x_stride, int32_t R, int32_t K, void*
  * between (rows may be NULL: row r itself).  The codes are those of x * g, formed in fp32, as hxf_op_quant_i8 makes them;
  * scale = max|x g| / 127 / sqrt(mean(x^2) + eps), the sum of squares in fp32 (beyond its range the scale is 0).  A row whose index is not in
  * [0, x_rows) (an empty place of a padded batch) is zeros with the scale 0.  x fp32 [x_rows, d], 16-byte aligned,
- * g bf16 [d], 8-byte aligned, d % 4 == 0, d < 2^17; codes and scale as above, for [n_rows, d]; n_rows < 2^22.
+ * g bf16 [d], 8-byte aligned, d % 4 == 0, d < 2^17; codes and scale as above, for [n_rows, d]; n_rows <= 2^22 - 16.
  * Without rows, n_rows <= x_rows.  No output may overlap another buffer. */
 int hxf_op_rmsnorm_i8(const float* x, const int32_t* rows, int32_t x_rows, const void* g, void* codes, float* scale,
                       int32_t n_rows, int32_t d, float eps, void* stream);
@@ -277,7 +277,7 @@ int hxf_op_rmsnorm_i8(const float* x, const int32_t* rows, int32_t x_rows, const
  *                   C[:, f] = bf16(silu(gate_f) * up_f), silu(z) = z / (1 + e^-z)
  *   HXF_EPI_F32:    C fp32 [M, ldc]            C = y
  * A and B (and B2): codes as above, 16-byte aligned.  B2 and b2_scale are unused but for SwiGLU.  ldc >= N (SwiGLU: F);
- * elements behind a row's columns are left as they are.  M < 2^22, 0 < N < 2^22, 0 < K < 2^17, M * N < 2^34.
+ * elements behind a row's columns are left as they are.  M <= 2^22 - 16, 0 < N <= 2^22 - 16, 0 < K < 2^17, M * N < 2^34.
  * workspace: hxf_op_gemm_i8_workspace_bytes(M, N, K) bytes (enough for every epilogue; may be 0), 16-byte
  * aligned, whose contents need not be kept between calls; calls that may overlap need one each.  No buffer may
  * overlap another. */

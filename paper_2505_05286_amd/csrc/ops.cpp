@@ -579,8 +579,8 @@ int hxf_op_prefill_attention_kv8(const void* q, int64_t q_stride, const hxf_kv8_
 
 namespace {
 
-// (at most 512 threads a row: under 2^32 of them)
-bool i8_matrix_ok(int32_t R, int32_t K) { return R >= 0 && R < (1 << 22) && K > 0 && K < (1 << 17); }
+// (at most 1024 threads a row of the padded matrix: under 2^32 of them)
+bool i8_matrix_ok(int32_t R, int32_t K) { return R >= 0 && R <= (1 << 22) - 16 && K > 0 && K < (1 << 17); }
 
 }  // namespace
 

@@ -30,7 +30,7 @@ def _quant(**k):
 
 
 @pytest.mark.parametrize("bad", [dict(x=None), dict(x=A + 8), dict(stride=120), dict(stride=132), dict(R=-1),
-                                 dict(R=1 << 22), dict(K=0), dict(K=-8), dict(K=100), dict(K=1 << 17, stride=1 << 17),
+                                 dict(R=(1 << 22) - 15), dict(K=0), dict(K=-8), dict(K=100), dict(K=1 << 17, stride=1 << 17),
                                  dict(codes=None), dict(codes=A + 8), dict(scale=None)])
 def test_quant_refuses(bad):
     _refused(hxf.EINVAL, _quant, **bad)
@@ -44,7 +44,7 @@ def _norm(**k):
 
 @pytest.mark.parametrize("bad", [dict(x=None), dict(x=A + 4), dict(x_rows=-1), dict(rows=0, x_rows=2), dict(g=None),
                                  dict(g=A + 2), dict(codes=None), dict(codes=A + 4), dict(scale=None), dict(n_rows=-1),
-                                 dict(n_rows=1 << 22), dict(d=0), dict(d=126), dict(d=1 << 17)])
+                                 dict(n_rows=(1 << 22) - 15, x_rows=1 << 23), dict(d=0), dict(d=126), dict(d=1 << 17)])
 def test_norm_refuses(bad):
     _refused(hxf.EINVAL, _norm, **bad)
 
@@ -60,7 +60,7 @@ SW = dict(epi=hxf.EPI_SWIGLU, b2=A, sb2=A, ldc=32)
 
 
 @pytest.mark.parametrize("bad", [dict(a=None), dict(a=A + 8), dict(sa=None), dict(b=None), dict(b=A + 1), dict(sb=None),
-                                 dict(c=None), dict(ldc=63), dict(M=-1), dict(M=1 << 22), dict(N=0), dict(N=-64),
+                                 dict(c=None), dict(ldc=63), dict(M=-1), dict(M=(1 << 22) - 15), dict(N=0), dict(N=-64),
                                  dict(N=1 << 22, ldc=1 << 22), dict(K=0), dict(K=-1), dict(K=1 << 17), dict(epi=-1), dict(epi=4),
                                  dict(epi=hxf.EPI_BF16 | hxf.GEMM_A_PACKED), dict(c=A + 1), dict(c=A + 2, epi=hxf.EPI_F32),
                                  dict(c=A + 2, epi=hxf.EPI_RESID), dict(M=1 << 18, N=1 << 18, ldc=1 << 18),
@@ -73,8 +73,8 @@ def test_sizes_of_buffers():
     assert hxf.i8_codes_bytes(0, 64) == 0
     assert hxf.i8_codes_bytes(1, 1) == 1024 and hxf.i8_codes_bytes(16, 64) == 1024
     assert hxf.i8_codes_bytes(17, 65) == 4096
-    assert hxf.i8_codes_bytes((1 << 22) - 1, (1 << 17) - 1) == 1 << 39
-    for bad in ((-1, 64), (1 << 22, 64), (4, 0), (4, 1 << 17)):
+    assert hxf.i8_codes_bytes((1 << 22) - 16, (1 << 17) - 1) == (1 << 39) - (1 << 21)
+    for bad in ((-1, 64), ((1 << 22) - 15, 64), (4, 0), (4, 1 << 17)):
         assert hxf.i8_codes_bytes(*bad) == -1
     for bad in ((-1, 64, 64), (4, 0, 64), (4, 64, 0), (4, 64, 1 << 17), (1 << 18, 1 << 18, 64)):
         assert hxf.op_gemm_i8_workspace_bytes(*bad) == -1
