@@ -10,10 +10,10 @@
 // the norm of 2080 x 5120), and the rows' pieces are neighbours in the tile.  A row's values stay in registers between
 // the maximum and the codes (read twice instead: 2080 x 28672 in 57 us where two rows in registers take 46).
 //
-// ROWS = 4 up to K of 8192, 2048 with the norm, where a workgroup is small; 2 up to 16384, 8192 with the norm, and 1
+// ROWS = 4 up to K of 8192, 2048 with the norm, where a workgroup is small; 2 up to 16384, 4096 with the norm, and 1
 // above, where more rows would fill a CU's registers and none is loaded while another is written (us with 4, 2 and 1 rows,
 // wavefronts chosen for each: 2080 x 28672 48.5 / 46.1 / 40.8, 64 x 28672 9.9 / 6.5 / 5.6, 2080 x 14336 25.8 / 22.8 /
-// 23.4; the norm of 2080 x 14336 45.2 / 41.0 / 35.1, of 2080 x 8192 25.9 / 22.1 / 22.2, of 256 x 8192 8.1 / 6.1 / 6.0;
+// 23.4; the norm of 2080 x 14336 45.2 / 41.0 / 35.1, of 2080 x 5120 16.3 / 15.7 / 14.9, of 256 x 8192 8.1 / 6.1 / 6.0;
 // but 16000 x 512 7.5 / 9.9, 28672 x 8192 124 / 135 and 2080 x 8192 15.1 / 15.4 / 15.6).
 #include "common.hpp"
 #include "gemm_util.hpp"
@@ -254,7 +254,7 @@ hipError_t rmsnorm_i8_launch(const float* x, const int32_t* rows, int x_rows, co
                        x, rows, x_rows, g, codes, scale, n_rows, d, eps);                                           \
     return hipGetLastError();                                                                                       \
   }
-  HXF_N(4, 4, 1) HXF_N(4, 8, 1) HXF_N(2, 8, 1) HXF_N(2, 16, 1) HXF_N(1, 16, 1) HXF_N(1, 16, 2) HXF_N(2, 16, 0)
+  HXF_N(4, 4, 1) HXF_N(4, 8, 1) HXF_N(2, 8, 1) HXF_N(1, 8, 1) HXF_N(1, 16, 1) HXF_N(1, 16, 2) HXF_N(2, 16, 0)
   return hipErrorInvalidValue;
 #undef HXF_N
 #undef ROWS_K
