@@ -81,14 +81,22 @@ struct WideCost {
   float t0, start, store, i0, i1, fetch[3], a_share, tb_s, gated;
   int resident;
 };
-constexpr WideCost kNarrowOnce{2.17f, 0.753f, 0.0348f, 0.192f, 0.033f, {0.37f, 0.33f, 0.3f}, 0.792f, 5.95f, 6.74f, 1};   // 32 columns a wavefront, one row of tiles
-constexpr WideCost kNarrowLow{3.22f, 0.f, 0.0426f, 0.112f, 0.0194f, {0.35f, 0.278f, 0.226f}, 0.64f, 6.f, 5.37f, 3};   // 32 columns, up to 4 row tiles a workgroup
-constexpr WideCost kNarrow{3.4f, 0.f, 0.0425f, 0.0314f, 0.0505f, {0.209f, 0.204f, 0.173f}, 1.55f, 4.24f, 6.25f, 2};   // 32 columns, more
-constexpr WideCost kCols64Once{2.94f, 0.f, 0.0299f, 0.f, 0.0449f, {0.335f, 0.33f, 0.3f}, 0.781f, 6.08f, 9.39f, 1};   // 64 columns, one row of tiles
-constexpr WideCost kCols64Low{3.27f, 0.f, 0.0392f, 0.12f, 0.0335f, {0.35f, 0.135f, 0.115f}, 4.7f, 4.1f, 4.94f, 2};   // 64 columns, up to 7 row tiles: two workgroups a CU
-constexpr WideCost kCols64{0.f, 4.11f, 0.0292f, 0.0925f, 0.036f, {0.35f, 0.133f, 0.115f}, 2.19f, 6.f, 5.68f, 1};   // 64 columns, 8 to 10
-constexpr WideCost kCols64High{2.27f, 2.77f, 0.0301f, 0.f, 0.0413f, {0.35f, 0.33f, 0.3f}, 0.5f, 6.f, 4.42f, 1};   // 64 columns, more
-constexpr WideCost kEight{0.f, 3.16f, 0.0241f, 0.263f, 0.0276f, {0.275f, 0.255f, 0.237f}, 0.795f, 3.68f, 5.79f, 1};   // eight wavefronts of 64 columns
+// 32 columns a wavefront, one row of tiles
+constexpr WideCost kNarrowOnce{2.17f, 0.753f, 0.0348f, 0.192f, 0.033f, {0.37f, 0.33f, 0.3f}, 0.792f, 5.95f, 6.74f, 1};
+// 32 columns, up to 4 row tiles a workgroup
+constexpr WideCost kNarrowLow{3.22f, 0.f, 0.0426f, 0.112f, 0.0194f, {0.35f, 0.278f, 0.226f}, 0.64f, 6.f, 5.37f, 3};
+// 32 columns, more
+constexpr WideCost kNarrow{3.4f, 0.f, 0.0425f, 0.0314f, 0.0505f, {0.209f, 0.204f, 0.173f}, 1.55f, 4.24f, 6.25f, 2};
+// 64 columns, one row of tiles
+constexpr WideCost kCols64Once{2.94f, 0.f, 0.0299f, 0.f, 0.0449f, {0.335f, 0.33f, 0.3f}, 0.781f, 6.08f, 9.39f, 1};
+// 64 columns, up to 7 row tiles: two workgroups a CU
+constexpr WideCost kCols64Low{3.27f, 0.f, 0.0392f, 0.12f, 0.0335f, {0.35f, 0.135f, 0.115f}, 4.7f, 4.1f, 4.94f, 2};
+// 64 columns, 8 to 10
+constexpr WideCost kCols64{0.f, 4.11f, 0.0292f, 0.0925f, 0.036f, {0.35f, 0.133f, 0.115f}, 2.19f, 6.f, 5.68f, 1};
+// 64 columns, more
+constexpr WideCost kCols64High{2.27f, 2.77f, 0.0301f, 0.f, 0.0413f, {0.35f, 0.33f, 0.3f}, 0.5f, 6.f, 4.42f, 1};
+// eight wavefronts of 64 columns
+constexpr WideCost kEight{0.f, 3.16f, 0.0241f, 0.263f, 0.0276f, {0.275f, 0.255f, 0.237f}, 0.795f, 3.68f, 5.79f, 1};
 // Pieces of K are joined by a launch of its own; a plan with one is only taken where it saves a twentieth
 constexpr float kJoin = 2.71f, kJoinGated = 1.66f, kJoinMb = 0.308f, kSplitBias = 1.06f;
 
@@ -98,8 +106,13 @@ struct ThinCost {
   int tm, nw, wv;
   float t0, first, step, kb, tb_s, rest;
 };
-constexpr ThinCost kThin[] = {{1, 1, 4, 2.66f, 0.615f, 0.0423f, 2.32f, 5.96f, 0.94f}, {1, 2, 16, 1.74f, 4.44f, 0.129f, 2.38f, 5.86f, 2.9f}, {2, 1, 16, 2.8f, 3.19f, 0.f, 2.54f, 5.44f, 2.01f},
-                              {2, 2, 8, 1.74f, 2.58f, 0.44f, 2.35f, 5.58f, 2.39f}, {4, 1, 8, 1.95f, 3.18f, 0.203f, 2.36f, 7.28f, 2.52f}, {4, 2, 8, 0.f, 5.55f, 0.56f, 2.58f, 5.68f, 3.97f}};
+constexpr ThinCost kThin[] = {
+    {1, 1, 4, 2.66f, 0.615f, 0.0423f, 2.32f, 5.96f, 0.94f},
+    {1, 2, 16, 1.74f, 4.44f, 0.129f, 2.38f, 5.86f, 2.9f},
+    {2, 1, 16, 2.8f, 3.19f, 0.f, 2.54f, 5.44f, 2.01f},
+    {2, 2, 8, 1.74f, 2.58f, 0.44f, 2.35f, 5.58f, 2.39f},
+    {4, 1, 8, 1.95f, 3.18f, 0.203f, 2.36f, 7.28f, 2.52f},
+    {4, 2, 8, 0.f, 5.55f, 0.56f, 2.58f, 5.68f, 3.97f}};
 
 struct Choice {
   int M, N, kt, row_tiles, bytes;   // bytes: of an output value, its old one read included
