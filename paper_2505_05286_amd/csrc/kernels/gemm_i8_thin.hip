@@ -58,14 +58,17 @@ __global__ __launch_bounds__(64 * WV) void gemm_i8_thin_kernel(GemmI8Args a) {
 #pragma unroll
     for (int j = 0; j < NW; ++j) part[w][i * NW + j][lane] = acc[i][j];
   __syncthreads();
+  // reads in flight: with all sixteen parts of two gate and two up tiles the kernel would need scratch memory
+  // (1 x 28672 x 4096 27.8 us instead of 25.9)
+  constexpr int AHEAD = NW * WV > 32 ? 8 : WV;
   for (int t = w; t < TM * HALF; t += WV) {
     const int i = t / HALF, j = t % HALF;
     const int row = i * 16 + (lane & 15), col = c0 + j * 16 + (lane >> 4) * 4;
     if (row >= a.M || col >= a.N) continue;
     auto sum = [&](int tile) {
-      i32x4 s = part[0][tile][lane];
-#pragma unroll
-      for (int v = 1; v < WV; ++v) s += part[v][tile][lane];
+      i32x4 s = {0, 0, 0, 0};
+#pragma unroll AHEAD
+      for (int v = 0; v < WV; ++v) s += part[v][tile][lane];
       return s;
     };
     const float sa = a.sa[row];
