@@ -32,9 +32,7 @@ __global__ __launch_bounds__(256) void gemm_i8_join_kernel(GemmI8Args a, int S) 
   const float sa = a.sa[row];
   f32x4 y = scaled(sum(col), sa, load_scales(a.sb, col, a.N));
   if constexpr (SW) {
-    const f32x4 u = scaled(sum(a.N + col), sa, load_scales(a.sb2, col, a.N));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = swiglu(y[e], u[e]);
+    y = swiglu(y, scaled(sum(a.N + col), sa, load_scales(a.sb2, col, a.N)));
   }
   store4<EPI>(a, row, col, y);
 }

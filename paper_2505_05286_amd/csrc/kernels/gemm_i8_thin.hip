@@ -74,9 +74,7 @@ __global__ __launch_bounds__(64 * WV) void gemm_i8_thin_kernel(GemmI8Args a) {
     const float sa = a.sa[row];
     f32x4 y = scaled(sum(i * NW + j), sa, load_scales(a.sb, col, a.N));
     if constexpr (SW) {
-      const f32x4 u = scaled(sum(i * NW + HALF + j), sa, load_scales(a.sb2, col, a.N));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = swiglu(y[e], u[e]);
+      y = swiglu(y, scaled(sum(i * NW + HALF + j), sa, load_scales(a.sb2, col, a.N)));
     }
     store4<EPI>(a, row, col, y);
   }

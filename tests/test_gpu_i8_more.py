@@ -1,0 +1,47 @@
+"""Linear layers in 8-bit integers on the GPU: values at the ends of the number formats."""
+import numpy as np
+import pytest
+
+from paper_2505_05286_amd import hxf
+
+from . import i8_util as U
+from ._lib import ensure_built
+from .gpu_util import torch
+from .test_gpu_i8 import U32, UB16, Product, _dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _built():
+    ensure_built()
+
+
+# in the kernel that shares K out in a workgroup, in those with whole K and with cut K and its join
+@pytest.mark.parametrize("M,F,K,thin,cut", [(20, 600, 1600, 1, False), (3, 200, 64, 0, False), (150, 202, 192, 0, False),
+                                            (66, 2706, 7248, 0, True)])
+def test_swiglu_at_gates_far_below_zero(M, F, K, thin, cut):
+    """silu(z) is a normal bf16 value down to z = -91.9, and times a large up value further down: gates from -112 to -60
+    and a few near and above zero, up values from 2^-7 to 2^100."""
+    p = Product(np.random.default_rng(M), M, 2 * F, K, "swiglu")
+    plan = hxf.op_gemm_i8_plan(M, 2 * F, K, hxf.EPI_SWIGLU)
+    assert plan[6] == thin and (plan[4] > 1) == cut
+    z = np.linspace(-112, -60, F)
+    z[::17] = np.linspace(-3, 90, len(z[::17]))
+    p.a[:], p.b[:], p.b2[:] = 0, 0, 0
+    p.a[:, 0] = 1 + np.arange(M) % 3
+    p.b[:, 0], p.b2[:, 0] = -100, 127
+    p.sa[:] = 1 / (1 + np.arange(M) % 3).astype(np.float32)
+    p.sb[:] = z / -100
+    p.sb2[:] = np.array([2.0 ** -14, 2.0 ** -3, 2.0 ** 53, 2.0 ** 93], np.float32)[np.arange(F) % 4]
+    p.dev = [_dev(v) for v in (U.tile(p.a), p.sa, U.tile(p.b), p.sb, U.tile(p.b2), p.sb2)]
+    p.call()
+    got = p.c.float().cpu().numpy()[:M * p.ldc].reshape(M, p.ldc)[:, :F].astype(np.float64)
+    y, up = U.product(p.a, p.sa, p.b, p.sb), U.product(p.a, p.sa, p.b2, p.sb2)
+    want = U.silu(y) * up
+    # relative: two half steps of the gate and two of e^-z's exponent, times |z|; a few each of the exponential, the sum,
+    # the reciprocal, the products and up; then bf16's.  Below the normal numbers half a step of silu (times up) and of
+    # the product in fp32, and of bf16.
+    tol = ((6 * np.abs(y) + 16) * U32 + UB16) * np.abs(want) + 2.0 ** -149 * (np.abs(up) + 1) + 2.0 ** -134
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (int(bad.sum()), [(y[i, j], up[i, j], got[i, j], want[i, j]) for i, j in np.argwhere(bad)[:4]])
