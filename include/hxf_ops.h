@@ -263,10 +263,11 @@ int hxf_op_quant_i8(const void* x, int64_t x_stride, int32_t R, int32_t K, void*
 
 /* RMSNorm into codes: row r is y = x[rows[r]] * g / sqrt(mean(x[rows[r]]^2) + eps), without a rounding to bf16 in
  * between (rows may be NULL: row r itself).  The codes are those of x * g, formed in fp32, as hxf_op_quant_i8 makes them;
- * scale = max|x g| / 127 / sqrt(mean(x^2) + eps), the sum of squares in fp32 (beyond its range the scale is 0).  A row whose index is not in
- * [0, x_rows) (an empty place of a padded batch) is zeros with the scale 0.  x fp32 [x_rows, d], 16-byte aligned,
- * g bf16 [d], 8-byte aligned, d % 4 == 0, d < 2^17; codes and scale as above, for [n_rows, d]; n_rows <= 2^22 - 16.
- * Without rows, n_rows <= x_rows.  No output may overlap another buffer. */
+ * scale = max|x g| / 127 / sqrt(mean(x^2) + eps), the sum of squares in fp32 (beyond its range the scale is 0; eps >= 0, and
+ * where mean(x^2) + eps is below 2^-100 the scale of a row that has codes is undefined).  A row with max|x g| < 2^-119,
+ * or whose index is not in [0, x_rows) (an empty place of a padded batch), is zeros with the scale 0, with eps 0 too.
+ * x fp32 [x_rows, d], 16-byte aligned, g bf16 [d], 8-byte aligned, d % 4 == 0, d < 2^17; codes and scale as above, for
+ * [n_rows, d]; n_rows <= 2^22 - 16.  Without rows, n_rows <= x_rows.  No output may overlap another buffer. */
 int hxf_op_rmsnorm_i8(const float* x, const int32_t* rows, int32_t x_rows, const void* g, void* codes, float* scale,
                       int32_t n_rows, int32_t d, float eps, void* stream);
 

@@ -227,7 +227,7 @@ __global__ __launch_bounds__(64 * NWV) void rmsnorm_i8_kernel(const float* x, co
     }
   }
   if (r < n_rows && w == 0 && (lane & (LPR - 1)) == 0)
-    scale[r] = live ? q.unit * rsqrtf(ss / (float)d + eps) : 0.f;
+    scale[r] = q.unit == 0.f ? 0.f : q.unit * rsqrtf(ss / (float)d + eps);   // (a row of zeros may be divided by zero)
 }
 
 }  // namespace

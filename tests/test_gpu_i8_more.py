@@ -7,7 +7,7 @@ from paper_2505_05286_amd import hxf
 from . import i8_util as U
 from ._lib import ensure_built
 from .gpu_util import torch
-from .test_gpu_i8 import U32, UB16, Product, _dev
+from .test_gpu_i8 import U32, UB16, Codes, Product, _bf16, _dev
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +45,29 @@ def test_swiglu_at_gates_far_below_zero(M, F, K, thin, cut):
     tol = ((6 * np.abs(y) + 16) * U32 + UB16) * np.abs(want) + 2.0 ** -149 * (np.abs(up) + 1) + 2.0 ** -134
     bad = ~(np.abs(got - want) <= tol)
     assert not bad.any(), (int(bad.sum()), [(y[i, j], up[i, j], got[i, j], want[i, j]) for i, j in np.argwhere(bad)[:4]])
+
+
+@pytest.mark.parametrize("d", [128, 1000, 3000, 8000, 20000, 33000])
+def test_norm_without_eps(d):
+    """eps 0: rows of zeros, and those too small for codes, have the scale 0, like rows that are quantised without a norm;
+    small rows that have codes are as good as others; a row that is not finite stays NaN."""
+    rng = np.random.default_rng(d)
+    x = rng.standard_normal((37, d)).astype(np.float32)
+    x[::5] = 0
+    x[3] *= np.float32(2.0 ** -125)
+    x[6] *= np.float32(2.0 ** -45)
+    x[8, d // 2] = np.nan
+    gb, g = _bf16(1 + rng.uniform(-0.5, 0.5, d))
+    out = Codes(37, d)
+    xd, gd = _dev(x), _dev(gb.view(np.int16))
+    hxf.op_rmsnorm_i8(xd.data_ptr(), 0, 37, gd.data_ptr(), *out.ptrs(), 37, d, 0.0)
+    codes, scale = out.get()
+    y, r = U.norm_rows(x, None, g, 0.0)
+    want, unit = U.codes_of(y)
+    assert np.array_equal(codes, U.tile(want))
+    zero = unit == 0
+    assert zero[::5].all() and zero[3] and not scale[zero].any()
+    assert np.isnan(scale[8]) and np.isnan(unit).sum() == 1
+    ok = unit > 0
+    tol = ((d / 64 + 16) / 2 + 8) * U32      # as with eps: the chain of the sum, halved by the root, and a few steps more
+    assert ok[6] and (np.abs(scale[ok] - unit[ok] * r[ok]) <= tol * unit[ok] * r[ok]).all()
