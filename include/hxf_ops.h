@@ -279,9 +279,11 @@ int hxf_op_rmsnorm_i8(const float* x, const int32_t* rows, int32_t x_rows, const
  *   HXF_EPI_F32:    C fp32 [M, ldc]            C = y
  * A and B (and B2): codes as above, 16-byte aligned.  B2 and b2_scale are unused but for SwiGLU.  ldc >= N (SwiGLU: F);
  * elements behind a row's columns are left as they are.  M <= 2^22 - 16, 0 < N <= 2^22 - 16, 0 < K < 2^17, M * N < 2^34.
- * workspace: hxf_op_gemm_i8_workspace_bytes(M, N, K) bytes (enough for every epilogue; may be 0), 16-byte
- * aligned, whose contents need not be kept between calls; calls that may overlap need one each.  No buffer may
- * overlap another. */
+ * workspace: hxf_op_gemm_i8_workspace_bytes(M, N, K) bytes are enough for every epilogue and every product of at most M rows,
+ * N columns and K (may be 0; never more than HXF_GEMM_I8_MAX_WORKSPACE, which is enough for any), 16-byte aligned, whose
+ * contents need not be kept between calls; calls that may overlap need one each.  HXF_ENOMEM (nothing enqueued) only where
+ * the pieces of K that this product is cut into, 4 M N bytes each, do not fit.  No buffer may overlap another. */
+#define HXF_GEMM_I8_MAX_WORKSPACE (72LL << 20)
 int64_t hxf_op_gemm_i8_workspace_bytes(int32_t M, int32_t N, int32_t K);
 /* Introspection (host only, no device work): the plan hxf_op_gemm_i8 takes for these sizes:
  * plan = {row tiles of 16, column tiles of 16 per wavefront, wavefronts, 1 if the weights are fetched as read once,

@@ -97,6 +97,9 @@ constexpr WideCost kCols64High{2.27f, 2.77f, 0.0301f, 0.f, 0.0413f, {0.35f, 0.33
 constexpr WideCost kEight{0.f, 3.16f, 0.0241f, 0.263f, 0.0276f, {0.275f, 0.255f, 0.237f}, 0.795f, 3.68f, 5.79f, 1};
 // Pieces of K are joined by a launch of its own; a plan with one is only taken where it saves a twentieth
 constexpr float kJoin = 2.71f, kJoinGated = 1.66f, kJoinMb = 0.308f, kSplitBias = 1.06f;
+// and only where all pieces of all tiles run at once, one a CU
+constexpr int kMaxPieces = 8, kPieceSteps = 12;
+constexpr int kMaxTile = 9 * 4 * 8 * 256;   // the most sums a workgroup holds, both halves of a gated one counted
 
 // The kernel that joins K inside the workgroup: the wait for a first step, a step, a CU's 100 KB of codes, the weights,
 // a workgroup's rest
@@ -124,7 +127,7 @@ struct Choice {
     const int64_t tiles = (int64_t)tiles_m * ((N + cols - 1) / cols);
     const float unit = tm * nw * wv / 16.f, ways = (nw * wv + c.a_share * tm) / 16.f;
     const float step = std::max(c.i0 + c.i1 * unit, c.fetch[tiles_m == 1 ? 0 : tiles_m <= 3 ? 1 : 2] * ways);
-    for (int s = 1; s <= 8 && (s == 1 || (kt >= 12 * s && tiles * s <= 256)); ++s) {
+    for (int s = 1; s <= kMaxPieces && (s == 1 || (kt >= kPieceSteps * s && tiles * s <= kCus)); ++s) {
       const int piece = ((kt + s - 1) / s + 1) / 2 * 2;
       if (s > 1 && (kt + piece - 1) / piece != s) continue;
       const float a_value = s > 1 ? (gated ? 8.f : 4.f) : gated ? c.gated : bytes;
@@ -199,15 +202,11 @@ int64_t partial_bytes(const GemmI8Plan& p, int M, int N, int epi) {
 
 }  // namespace
 
+// For every plan of at most these sizes.  What one plan needs goes up and down with its rows (4096 x 14336: 14.7 MB at 448
+// rows, 8.4 at 256, none at 2080), and a caller keeps one buffer for batches of any size up to its largest.
 int64_t gemm_i8_ws_bytes(int M, int N, int K) {
-  if (M == 0) return 0;
-  int64_t need = 0;
-  for (int epi : {EPI_BF16, EPI_RESID, EPI_F32, EPI_SWIGLU}) {
-    if (epi == EPI_SWIGLU && N % 2) continue;
-    const int n = epi == EPI_SWIGLU ? N / 2 : N;
-    need = std::max(need, partial_bytes(gemm_i8_plan(M, n, (K + 63) / 64, epi), M, n, epi));
-  }
-  return need;
+  const int pieces = std::min(kMaxPieces, (K + 63) / 64 / kPieceSteps);
+  return pieces < 2 ? 0 : std::min((int64_t)pieces * M * N * 4, (int64_t)kCus * kMaxTile * 4);
 }
 
 hipError_t gemm_i8_launch(const GemmI8Args& a, int epi, int64_t ws_bytes, hipStream_t st) {

@@ -117,7 +117,7 @@ hipError_t gemm_i8_f32(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st)
 hipError_t gemm_i8_split(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
 hipError_t gemm_i8_thin(const GemmI8Args& a, int epi, const GemmI8Plan& p, hipStream_t st);
 hipError_t gemm_i8_split_swiglu(const GemmI8Args& a, const GemmI8Plan& p, hipStream_t st);
-int64_t gemm_i8_ws_bytes(int M, int N, int K);   // N as the caller counts it (SwiGLU: 2F)
+int64_t gemm_i8_ws_bytes(int M, int N, int K);   // up to these sizes; N as the caller counts it (SwiGLU: 2F)
 // hipErrorOutOfMemory (nothing enqueued) where the plan's partials need more than ws_bytes
 hipError_t gemm_i8_launch(const GemmI8Args& a, int epi, int64_t ws_bytes, hipStream_t st);
 

@@ -444,6 +444,7 @@ def op_gemm(A, lda, B, B2, Cp, ldc, M, N, K, epi, ws=0, ws_bytes=0, stream=0):
 
 
 GEMM_NOALLOC_MAX_BYTES = 16 << 20
+GEMM_I8_MAX_WORKSPACE = 72 << 20
 
 
 def op_gemm_noalloc(A, lda, B, B2, Cp, ldc, M, N, K, epi, stream=0):
@@ -616,6 +617,7 @@ def op_rmsnorm_i8(x, rows, x_rows, g, codes, scale, n_rows, d, eps, stream=0):
 
 
 def op_gemm_i8_workspace_bytes(M, N, K):
+    """Enough for op_gemm_i8 of at most M rows, N columns and K, any epilogue."""
     return lib().hxf_op_gemm_i8_workspace_bytes(M, N, K)
 
 

@@ -7,7 +7,7 @@ from paper_2505_05286_amd import hxf
 from . import i8_util as U
 from ._lib import ensure_built
 from .gpu_util import torch
-from .test_gpu_i8 import U32, UB16, Codes, Product, _bf16, _dev
+from .test_gpu_i8 import DEV, GUARD, U32, UB16, Codes, Product, _bf16, _dev
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +71,19 @@ def test_norm_without_eps(d):
     ok = unit > 0
     tol = ((d / 64 + 16) / 2 + 8) * U32      # as with eps: the chain of the sum, halved by the root, and a few steps more
     assert ok[6] and (np.abs(scale[ok] - unit[ok] * r[ok]) <= tol * unit[ok] * r[ok]).all()
+
+
+def test_a_workspace_for_the_largest_batch_serves_smaller_ones():
+    """One buffer, sized once for a batch whose K is whole, for batches whose K is cut."""
+    t = torch()
+    rng = np.random.default_rng(23)
+    N, K = 1024, 4096
+    n = hxf.op_gemm_i8_workspace_bytes(2080, N, K)
+    ws = t.full((n + GUARD,), 0x5A, dtype=t.uint8, device=DEV)
+    assert hxf.op_gemm_i8_plan(2080, N, K, hxf.EPI_RESID)[4] == 1
+    assert all(hxf.op_gemm_i8_plan(m, N, K, hxf.EPI_RESID)[4] > 1 for m in (300, 129))
+    for m in (2080, 300, 129, 33):
+        p = Product(rng, m, N, K, "resid")
+        p.ws = ws
+        p.call()
+        p.check()
