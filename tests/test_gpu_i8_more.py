@@ -4,10 +4,11 @@ import pytest
 
 from paper_2505_05286_amd import hxf
 
+from . import i8_instances
 from . import i8_util as U
 from ._lib import ensure_built
 from .gpu_util import torch
-from .test_gpu_i8 import DEV, GUARD, U32, UB16, Codes, Product, _bf16, _dev
+from .test_gpu_i8 import DEV, GUARD, U32, UB16, Codes, Product, _bf16, _dev, _tile_dev
 
 pytestmark = pytest.mark.gpu
 
@@ -87,3 +88,42 @@ def test_a_workspace_for_the_largest_batch_serves_smaller_ones():
         p.ws = ws
         p.call()
         p.check()
+
+
+@pytest.mark.parametrize("M,N,K,epi", i8_instances.MORE)
+def test_gemm_in_the_instances_of_one_epilogue(M, N, K, epi):
+    """With the other list's, every compiled instance of the kernels; whole numbers by products in 64 bits (exact below
+    2^53), rows of outputs a column apart, the buffers' ends guarded."""
+    t = torch()
+    cols, gated, wide = (2 * N if epi == "swiglu" else N), epi == "swiglu", epi in ("resid", "f32")
+    print(i8_instances.instance(M, N, K, epi), flush=True)
+    g = t.Generator(device=DEV)
+    g.manual_seed(M * 7 + N)
+    rand = lambda n: t.randint(-127, 128, (n, K), generator=g, device=DEV, dtype=t.int8)   # noqa: E731
+    a, b, b2 = rand(M), rand(N), rand(N if gated else 1)
+    sa = t.rand(M, generator=g, device=DEV) + 0.5
+    sb, sb2 = ((t.rand(len(w), generator=g, device=DEV) + 0.5) / (5000 * K ** 0.5) for w in (b, b2))
+    dev = [_tile_dev(v) for v in (a, b, b2)]
+    c = t.full((M * (N + 1) + GUARD,), 3.0, device=DEV, dtype=t.float32 if wide else t.bfloat16)
+    view = c[:M * (N + 1)].view(M, N + 1)
+    if epi == "resid":
+        view[:, :N] = t.randn(M, N, generator=g, device=DEV)
+    old = view[:, :N].double()
+    n = hxf.op_gemm_i8_workspace_bytes(M, cols, K)
+    ws = t.full((n + GUARD,), 0x5A, dtype=t.uint8, device=DEV)
+    hxf.op_gemm_i8(dev[0].data_ptr(), sa.data_ptr(), dev[1].data_ptr(), sb.data_ptr(), dev[2].data_ptr() if gated else 0,
+                   sb2.data_ptr() if gated else 0, c.data_ptr(), N + 1, M, cols, K, i8_instances.EPILOGUES[epi], ws.data_ptr(), n)
+    t.cuda.synchronize()
+    assert bool((ws[n:] == 0x5A).all()) and bool((view[:, N] == 3.0).all()) and bool((c[M * (N + 1):] == 3.0).all())
+    y = ((a.double() @ b.double().T) * sa.double()[:, None]) * sb.double()
+    rel = 3.001 * U32           # float(acc) and two products
+    if gated:
+        want = y * t.sigmoid(y) * (((a.double() @ b2.double().T) * sa.double()[:, None]) * sb2.double())
+        tol = (UB16 + (6 * y.abs() + 16) * U32) * want.abs() + 2.0 ** -134
+    elif epi == "resid":
+        want = y + old
+        tol = rel * y.abs() + 1.001 * U32 * (want.abs() + rel * y.abs())
+    else:
+        want, tol = y, (rel + (0 if wide else UB16 + rel)) * y.abs()
+    bad = ~((view[:, :N].double() - want).abs() <= tol)
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist())

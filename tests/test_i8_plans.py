@@ -5,6 +5,7 @@ import pytest
 
 from paper_2505_05286_amd import hxf
 
+from . import i8_instances
 from ._lib import ensure_built
 
 EPILOGUES = (hxf.EPI_BF16, hxf.EPI_RESID, hxf.EPI_SWIGLU, hxf.EPI_F32)
@@ -47,3 +48,11 @@ def test_the_workspace_covers_smaller_products_of_any_size():
     assert cut > 1000
     assert hxf.op_gemm_i8_workspace_bytes(100000, 100000, 131071) == hxf.GEMM_I8_MAX_WORKSPACE
     assert hxf.op_gemm_i8_workspace_bytes(0, 4096, 14336) == 0
+
+
+def test_every_compiled_instance_is_taken_by_a_tested_product():
+    """With its epilogue: the instances are compiled for each of them."""
+    taken = {i8_instances.instance(*p) for p in i8_instances.products()}
+    every = i8_instances.compiled()
+    assert len(every) == 41 * 6 + 6 * 4
+    assert taken == every, (sorted(every - taken), sorted(taken - every))
