@@ -1,4 +1,5 @@
-"""Linear layers in 8-bit integers on the GPU: values at the ends of the number formats."""
+"""Linear layers in 8-bit integers on the GPU: values at the ends of the number formats, every instance of the product,
+cut K in batches, on streams and in graphs."""
 import numpy as np
 import pytest
 
@@ -8,7 +9,7 @@ from . import i8_instances
 from . import i8_util as U
 from ._lib import ensure_built
 from .gpu_util import torch
-from .test_gpu_i8 import DEV, GUARD, U32, UB16, Codes, Product, _bf16, _dev, _tile_dev
+from .test_gpu_i8 import DEV, GUARD, U32, UB16, Codes, Layer, Product, _bf16, _dev, _tile_dev
 
 pytestmark = pytest.mark.gpu
 
@@ -127,3 +128,117 @@ def test_gemm_in_the_instances_of_one_epilogue(M, N, K, epi):
         want, tol = y, (rel + (0 if wide else UB16 + rel)) * y.abs()
     bad = ~((view[:, :N].double() - want).abs() <= tol)
     assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist())
+
+
+def _cut(m, n, k, epi):
+    """The product is cut into pieces of K: partials in the workspace and a second launch."""
+    assert hxf.op_gemm_i8_plan(m, n, k, i8_instances.EPILOGUES[epi])[4] > 1
+
+
+def test_products_with_cut_k_on_two_streams_at_once():
+    """A workspace each, other operands, outputs and workspaces filled with something else before each call."""
+    t = torch()
+    rng = np.random.default_rng(19)
+    ps = [Product(rng, 33, 1024, 8192, "f32"), Product(rng, 300, 512, 4096, "f32")]
+    for p in ps:
+        _cut(p.M, p.N, p.K, p.epi)
+    streams = [t.cuda.Stream() for _ in ps]
+    t.cuda.synchronize()
+    seen = [[], []]
+    for _ in range(8):
+        for p, s, out in zip(ps, streams, seen):
+            with t.cuda.stream(s):
+                p.c[:p.M * p.ldc].fill_(float("nan"))
+                p.ws[:-GUARD].fill_(0x33)
+                p.call(stream=s.cuda_stream)
+                out.append(p.c.clone())
+    t.cuda.synchronize()
+    for p, out in zip(ps, seen):
+        p.check()
+        assert all(t.equal(c, p.c) for c in out)
+
+
+def _layers(rng):
+    """Blocks whose gate and up projections, or whose down projection, are cut."""
+    _cut(70, 2 * 1408, 4096, "swiglu")
+    _cut(33, 1024, 8192, "resid")
+    return [Layer(rng, 70, 4096, 1408), Layer(rng, 33, 1024, 8192)]
+
+
+def _eager(layer, x):
+    layer.ws.fill_(0x33)
+    layer.x.copy_(x)
+    layer.run()
+    return layer.x.clone()
+
+
+def test_blocks_with_cut_k_step_by_step():
+    """Each step from what the step before it left: codes to the bit, scales and products within their roundings."""
+    rng = np.random.default_rng(20)
+    for layer in _layers(rng):
+        x = rng.standard_normal((layer.T, layer.d)).astype(np.float32)
+        got = _eager(layer, _dev(x)).cpu().numpy().astype(np.float64)
+        (gate, sg), (up, su), (down, sd) = (U.codes_of(w) for w in layer.wv)
+        y, r = U.norm_rows(x, None, layer.g, np.float32(1e-5))
+        a, unit = U.codes_of(y)
+        codes, sa = layer.cx.get()
+        assert np.array_equal(codes, U.tile(a))
+        assert (np.abs(sa - unit * r) <= ((layer.d / 64 + 16) / 2 + 8) * U32 * unit * r).all()
+        h = layer.h.float().cpu().numpy()
+        z = U.product(a, sa, gate, sg)
+        want = U.silu(z) * U.product(a, sa, up, su)
+        assert (np.abs(h - want) <= (UB16 + (6 * np.abs(z) + 16) * U32) * np.abs(want) + 2.0 ** -134).all()
+        a, unit = U.codes_of(h)
+        codes, sa = layer.ch.get()
+        assert np.array_equal(codes, U.tile(a)) and np.array_equal(sa, unit)
+        v = U.product(a, sa, down, sd)
+        rel = 3.001 * U32
+        assert (np.abs(got - (x + v)) <= rel * np.abs(v) + 1.001 * U32 * (np.abs(x + v) + rel * np.abs(v))).all()
+
+
+def test_blocks_with_cut_k_on_streams_of_their_own():
+    t = torch()
+    rng = np.random.default_rng(21)
+    layers = _layers(rng)
+    xs = [_dev(rng.standard_normal((v.T, v.d)).astype(np.float32)) for v in layers]
+    wants = [_eager(v, x) for v, x in zip(layers, xs)]
+    streams = [t.cuda.Stream() for _ in layers]
+    t.cuda.synchronize()
+    gots = [[], []]
+    for _ in range(4):
+        for layer, x, s, out in zip(layers, xs, streams, gots):
+            with t.cuda.stream(s):
+                layer.h.zero_()
+                out.append(_eager(layer, x))
+    t.cuda.synchronize()
+    for want, out in zip(wants, gots):
+        assert all(t.equal(v, want) for v in out)
+
+
+def test_captured_blocks_with_cut_k_replay_on_new_inputs():
+    """Two graphs with a workspace each, replayed at once on two streams; eager calls and waits between the replays."""
+    t = torch()
+    rng = np.random.default_rng(22)
+    layers = _layers(rng)
+    graphs, streams = [], [t.cuda.Stream() for _ in layers]
+    for layer in layers:
+        layer.run()
+        t.cuda.synchronize()
+        graph = t.cuda.CUDAGraph()
+        with t.cuda.graph(graph):
+            layer.run()
+        graphs.append(graph)
+    for k in range(4):
+        xs = [_dev(rng.standard_normal((v.T, v.d)).astype(np.float32)) for v in layers]
+        wants = [_eager(v, x) for v, x in zip(layers, xs)]
+        for layer, x in zip(layers, xs):
+            layer.x.copy_(x)
+            layer.ws.fill_(0x33)
+            layer.h.zero_()
+        t.cuda.synchronize()
+        for graph, s in zip(graphs, streams):
+            with t.cuda.stream(s):
+                graph.replay()
+        t.cuda.synchronize()
+        for layer, want in zip(layers, wants):
+            assert t.equal(layer.x, want)
