@@ -74,7 +74,10 @@ namespace {
 // `resident` workgroups at once, which share its time but wait each by itself (start).  The weights come at tb_s at best.
 //
 // Fitted to 190,000 launches of 4,900 shapes (1 to 3,000 rows, half of them projections of d 4096-8192), weights not
-// in the caches, in graphs: the choice is 2.2% slower than the best plan on average, 28% at the worst hundredth.
+// in the caches, in graphs: the choice is 2.2% slower than the best plan on average, 28% at the worst hundredth.  Among the
+// worst are some batches of model shapes, where two estimates lie closer than the times (us, the choice and the best plan):
+// 1-16 rows of 28672 x 4096 SwiGLU 25.7 / 20.8, 17-32 of 8192 x 28672 45 / 39, 82 68 / 48, 130 of 4096 x 4096 15.0 / 11.5,
+// 192 14.0 / 11.7, 440 of 5120 x 27648 108 / 72.
 struct WideCost {
   float t0, start, store, i0, i1, fetch[3], a_share, tb_s, gated;
   int resident;

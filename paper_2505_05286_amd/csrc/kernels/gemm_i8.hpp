@@ -87,11 +87,12 @@ __device__ __forceinline__ void store4(const GemmI8Args& a, int row, int col, f3
 // K: the weights go straight from memory to registers, R steps of 64 of K ahead, and only the activations pass
 // through LDS, stages of 128 of K by buffer DMA, NS in flight.  Steps past the end of K multiply weights of zero, so
 // what the activations hold there does not matter.
-// Up to ~128 rows the weights' bytes are the bound (64 rows of 28672 x 4096 SwiGLU 20.1 us, 5.8 TB/s; weights that one row
-// of tiles reads are fetched with the non-temporal hint); with 2080 rows the power (57344 x 8192 714 us, 2.74 P/s at
-// 1.6-1.9 GHz, MFMAs busy 60-68% of the time) and, in products of one round of tiles, the instructions between the MFMAs of
-// a wavefront that is alone on its SIMD (4096 x 14336 112 us, 2.18 P/s).  32x32x32 MFMAs in this scheme are 7% slower
-// (831 us against 774), eight stages of activations or weights eight steps ahead gain nothing (0-2%).
+// Up to ~128 rows the weights' bytes are the bound (64 rows of 28672 x 4096 SwiGLU 21.3 us, 5.6 TB/s; weights that one row
+// of tiles reads are fetched with the non-temporal hint); with 2080 rows the power (57344 x 8192 709 us, 2.76 P/s at
+// 1.7 GHz, MFMAs busy 73% of the time; 692 to 735 us from run to run) and, in products of one round of tiles, the
+// instructions between the MFMAs of a wavefront that is alone on its SIMD (4096 x 14336 112 us, 2.18 P/s, MFMAs busy 50%).
+// 32x32x32 MFMAs in this scheme were 7% slower (831 us against 774, before loads were spread as below), eight stages of
+// activations or weights eight steps ahead gained nothing (0-2%).
 // SwiGLU: half of a wavefront's column tiles are gate and half the same columns of up, so one lane holds both.
 // Weights are the first MFMA operand: a lane ends up with 4 consecutive columns of one row.
 // SPLIT: grid.y cuts K into pieces of a.piece steps (even); each writes its int32 partial [M][N] (SwiGLU: gate, then

@@ -3,9 +3,11 @@
 //
 // The weights' bytes are the bound, and below some tens of MB the latency of the first loads and of a second launch.
 // With 16 or 32 columns a workgroup an output of a few thousand fills the chip without cutting K across workgroups,
-// whose partials take a launch of their own to join (a call, us, this kernel and the other with cut K: 1 x 6144 x 4096
-// 8.0 / 10.5, 64 rows 10.3 / 13.7; 1 x 4096 x 14336 12.9 / 15.7; 1 x 8192 x 28672 37.3 / 39.4, 6.3 TB/s).  But every
-// workgroup reads all activations itself: from 32 rows of long K on the other kernel is ahead (32 x 8192 x 28672 41.4).
+// whose partials take a launch of their own to join (a call in a graph, us, this kernel and the other's best plan, with cut
+// K: 1 x 6144 x 4096 8.0 / 10.0, 64 rows 10.8 / 13.8; 1 x 4096 x 14336 13.5 / 15.5; 1 x 8192 x 28672 39 / 38.2, 6.0 TB/s).
+// But every workgroup reads all activations itself, and with a gate twice the weights wait in two rounds of workgroups: there
+// the other kernel is ahead, while the plan's estimate, a few percent off, still takes this one (17 and 32 rows of 8192 x 28672
+// 45 / 39; 1 to 16 rows of 28672 x 4096 SwiGLU 25.7 / 20.8, whole K; from 33 rows of 8192 x 28672 on it takes the other).
 #include "gemm_i8.hpp"
 
 namespace hxf {

@@ -14,7 +14,10 @@
 // above, where more rows would fill a CU's registers and none is loaded while another is written (us with 4, 2 and 1 rows,
 // wavefronts chosen for each: 2080 x 28672 48.5 / 46.1 / 40.8, 64 x 28672 9.9 / 6.5 / 5.6, 2080 x 14336 25.8 / 22.8 /
 // 23.4; the norm of 2080 x 14336 45.2 / 41.0 / 35.1, of 2080 x 5120 16.3 / 15.7 / 14.9, of 256 x 8192 8.1 / 6.1 / 6.0;
-// but 16000 x 512 7.5 / 9.9, 28672 x 8192 124 / 135 and 2080 x 8192 15.1 / 15.4 / 15.6).
+// but 16000 x 512 7.5 / 9.9, 28672 x 8192 124 / 135 and 2080 x 8192 15.1 / 15.4 / 15.6).  Rows above 32768 fit no workgroup's
+// registers and are read twice, two a workgroup (us with 4, 2 and 1 rows: 2080 x 40000 85 / 82 / 75, 64 x 40000 14.2 / 8.7 /
+// 6.1, 2080 x 131064 353 / 366 / 348, 300 x 131064 67 / 48 / 54; the norm of them 160 / 144 / 132, 28 / 16 / 10, 609 / 640 /
+// 628, 131 / 92 / 101): the longest rows of few take least with two, the rest with one.
 #include "common.hpp"
 #include "gemm_util.hpp"
 #include "kernels.hpp"
